@@ -343,6 +343,90 @@ qe_status qe_outliers_csr(const float* H, int64_t q, int64_t p, const int64_t* s
                           const int64_t* nnz, int64_t cap, int64_t* rowptr, int32_t* cols,
                           float* vals, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Key/value cache in 4 bits, for decoders whose layers this library quantizes.
+ * The paper covers weights only; grid and layout are this library's.
+ *
+ * Grid.  The dim channels of a token's key (or value) in one head are cut into
+ * groups of `group` consecutive channels.  A group x gets, in fp32,
+ *   lo = min(0, min x), hi = max(0, max x),
+ *   s = max((hi - lo) / 15, 2^-126), its bit pattern rounded to a multiple of 16,
+ *   z = rint(-lo * (1 / s)),  n = clamp(rint(x * (1 / s)) + z, 0, 15),
+ * and is held as the codes n and one word, the bit pattern of s with z in its low
+ * four bits; it stands for s (n - z), each element within s / 2 of x (up to rounding).  A
+ * group that holds a NaN or an infinity, or whose hi - lo passes the largest fp32
+ * number, has a NaN scale: it reads back as NaN, and so does every attention row
+ * that sees it.
+ *
+ * Layout.  dim is a multiple of 8, at most 256; group is 32, 64 or 128; a page
+ * holds `page` tokens (a multiple of 32).  The cache is num_pages pages, in each of
+ * them kv_heads x page / 32 records of 32 consecutive tokens of one head (pages 16-byte
+ * aligned, qe_kv_page_bytes each).  With Dp = dim rounded up to 64, 96, 128, 192 or
+ * 256 (channels past dim hold 0), NC = Dp / 32 and NG = ceil(Dp / group), a record is
+ *   - 32 key rows of 4 NC words: word j NC + c holds channels 8 (4 c + j) .. + 7,
+ *     the lowest channel in the lowest four bits;
+ *   - NG x 32 words: the groups' s and z, group-major;
+ *   - Dp / 4 x 32 half-words: channels 4 u .. + 3 of the tokens' values;
+ *   - NG x 32 words: the value groups' s and z.
+ * A token's slot is page number * page + its place in the page.
+ *
+ * dtype of K, V, Q, out: QE_F32, QE_F16 or QE_BF16; a head's dim channels are
+ * contiguous, tokens and heads lie at the given strides (in elements; an output's
+ * elements must not overlap).
+ * ------------------------------------------------------------------------ */
+#define QE_F32  0
+#define QE_F16  1
+#define QE_BF16 2
+
+/* Bytes of one page; 0 where the sizes are not supported. */
+int64_t qe_kv_page_bytes(int kv_heads, int dim, int group, int page);
+
+/* Quantizes K and V (tokens x kv_heads x dim) into the slots (device int64, one
+ * per token; the slots of a call that are not negative must differ).  A negative slot skips
+ * its token; so does one past the cache, which also sets QE_ERR_ARG in `status` (NULL, or a
+ * device int that the call never clears).  Other tokens of the cache keep their bits.
+ * tokens = 0: nothing is done. */
+qe_status qe_kv_write(const void* K, const void* V, int dtype, int64_t tokens, int kv_heads, int dim,
+                      int64_t k_stride, int64_t k_head_stride, int64_t v_stride, int64_t v_head_stride,
+                      const int64_t* slots, int group, void* pages, int64_t num_pages, int page,
+                      int* status, void* stream);
+
+/* The values s (n - z) that the cache holds at the slots, rounded once to dtype.
+ * Any slots, in any order; a negative one, or one past the cache (QE_ERR_ARG in
+ * `status`), gives zeros. */
+qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64_t* slots, int64_t tokens,
+                     int kv_heads, int dim, int group, void* K, void* V, int dtype, int64_t k_stride,
+                     int64_t k_head_stride, int64_t v_stride, int64_t v_head_stride, int* status,
+                     void* stream);
+
+/* Attention over the cache.  Sequence b has lengths[b] cached tokens, token t in
+ * page table[b * width + t / page], and the queries q_start[b] .. q_start[b + 1] - 1
+ * of the `total` rows of Q (total x heads x dim); with q_start NULL the queries
+ * b max_q .. b max_q + max_q - 1.  Its i-th of nq queries stands at token
+ * pos = lengths[b] - nq + i, so new tokens are written before the call.  Query head h
+ * uses key/value head h / (heads / kv_heads).  The query sees the tokens
+ *   t < lengths[b];  causal: t <= pos;  window > 0 (causal only): t > pos - window,
+ * and out = sum_t p_t v_t, p the softmax over them of
+ *   scale q . k_t + slopes[h] (t - pos)       (slopes NULL: without the last term;
+ *                                              causal only).
+ * A row that sees no token is 0, its lse -infinity.  lse: NULL or total x heads floats
+ * (device): the natural logarithm of the softmax's denominator.
+ * Products run on the fp16 matrix cores: codes are exact there, a query row is
+ * scaled by a power of two and rounded to fp16 (exact for fp16 and bf16 inputs up to
+ * 2^-25 of the row's largest value; fp32 rows and their probabilities are split into two
+ * fp16 parts each), probabilities are rounded to fp16; statistics and sums are fp32.
+ * max_q: at least every nq.  Lengths past width * page, queries past `total` or max_q and
+ * page numbers outside of the cache set QE_ERR_ARG in the workspace's status word (which
+ * this call never clears; qe_sync_status does) and count as absent. */
+size_t qe_kv_attn_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads,
+                                 int dim);
+qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                     int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                     const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                     const int32_t* table, int64_t width, const int32_t* lengths, float scale,
+                     int causal, int window, const float* slopes, void* out, int64_t o_stride,
+                     int64_t o_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -3,6 +3,7 @@
 #include <cmath>
 #include <mutex>
 
+#include "kv.h"
 #include "qe_internal.h"
 
 using namespace qe;
@@ -83,6 +84,23 @@ qe_status scratch_on_stream(hipStream_t s, void** out)
     }
     *out = g_scratch_ptr[dev];
     return QE_OK;
+}
+
+// Sizes of a key/value cache: supported, and record numbers fit 32 bits.
+bool bad_kv(int64_t num_pages, int page, int kv_heads, int dim, int group)
+{
+    if (kv_heads < 1 || kv_heads > (1 << 20) || dim < 8 || dim > 256 || dim % 8) return true;
+    if (group != 32 && group != 64 && group != 128) return true;
+    if (page < kKvTok || page % kKvTok || page > (1 << 30)) return true;
+    return num_pages < 1 || num_pages > ((int64_t(1) << 32) - 1) / (page / kKvTok);
+}
+bool bad_dtype(int dtype) { return dtype != QE_F32 && dtype != QE_F16 && dtype != QE_BF16; }
+bool misaligned(const void* p, int bytes) { return (uintptr_t)p % bytes != 0; }
+int dtype_bytes(int dtype) { return dtype == QE_F32 ? 4 : 2; }
+
+KvCache kv_cache(const void* pages, int64_t num_pages, int page, int kv_heads, int dim)
+{
+    return {static_cast<uint8_t*>(const_cast<void*>(pages)), num_pages * page, (uint32_t)(page / kKvTok), kv_heads, dim};
 }
 
 __global__ void status_copy_kernel(const int* from, int* to)
@@ -335,6 +353,90 @@ qe_status qei_lambda_max_polls(const float* Sigma, int64_t p, int max_iters, flo
     hipStream_t s = as_stream(stream);
     if (clear_status(ws, s) != QE_OK) return QE_ERR_HIP;
     return launch_lambda(Sigma, p, max_iters, tol, lambda_out, ws, max_polls, s);
+}
+
+// ------------------------------------------------------------------ key/value cache
+int64_t qe_kv_page_bytes(int kv_heads, int dim, int group, int page)
+{
+    if (bad_kv(1, page, kv_heads, dim, group)) return 0;
+    return kv_record_bytes(kv_dp(dim), group) * kv_heads * (page / kKvTok);
+}
+
+qe_status qe_kv_write(const void* K, const void* V, int dtype, int64_t tokens, int kv_heads, int dim,
+                      int64_t k_stride, int64_t k_head_stride, int64_t v_stride, int64_t v_head_stride,
+                      const int64_t* slots, int group, void* pages, int64_t num_pages, int page,
+                      int* status, void* stream)
+{
+    if (bad_dtype(dtype) || tokens < 0 || bad_kv(num_pages, page, kv_heads, dim, group)) return QE_ERR_ARG;
+    if (tokens == 0) return QE_OK;
+    if (!K || !V || !slots || !pages || misaligned(pages, 16)) return QE_ERR_ARG;
+    if (misaligned(K, dtype_bytes(dtype)) || misaligned(V, dtype_bytes(dtype))) return QE_ERR_ARG;
+    const int64_t strides[4] = {k_stride, k_head_stride, v_stride, v_head_stride};
+    return launch_kv_write(K, V, dtype, strides, slots, tokens, kv_cache(pages, num_pages, page, kv_heads, dim), group,
+                           status, as_stream(stream));
+}
+
+qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64_t* slots, int64_t tokens,
+                     int kv_heads, int dim, int group, void* K, void* V, int dtype, int64_t k_stride,
+                     int64_t k_head_stride, int64_t v_stride, int64_t v_head_stride, int* status, void* stream)
+{
+    if (bad_dtype(dtype) || tokens < 0 || bad_kv(num_pages, page, kv_heads, dim, group)) return QE_ERR_ARG;
+    if (tokens == 0) return QE_OK;
+    if (!K || !V || !slots || !pages || misaligned(pages, 16)) return QE_ERR_ARG;
+    if (misaligned(K, dtype_bytes(dtype)) || misaligned(V, dtype_bytes(dtype))) return QE_ERR_ARG;
+    const int64_t strides[4] = {k_stride, k_head_stride, v_stride, v_head_stride};
+    return launch_kv_read(kv_cache(pages, num_pages, page, kv_heads, dim), group, slots, tokens, K, V, dtype, strides,
+                          status, as_stream(stream));
+}
+
+size_t qe_kv_attn_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim)
+{
+    if (total < 0 || batch < 0 || max_q < 0 || bad_kv(1, kKvTok, kv_heads, dim, 32)) return 0;
+    if (heads < 1 || heads % kv_heads) return 0;
+    return kv_attn_ws_bytes(std::min(batch, total), std::min(max_q, total), heads, kv_heads, dim);
+}
+
+qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                     int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                     const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                     const int32_t* table, int64_t width, const int32_t* lengths, float scale, int causal,
+                     int window, const float* slopes, void* out, int64_t o_stride, int64_t o_head_stride,
+                     float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    if (bad_dtype(dtype) || bad_kv(num_pages, page, kv_heads, dim, group)) return QE_ERR_ARG;
+    if (heads < 1 || heads % kv_heads || heads > (1 << 20)) return QE_ERR_ARG;
+    if (total < 0 || total > 0x7fffffff || batch < 0 || batch > 0x7fffffff || max_q < 0 || width < 0) return QE_ERR_ARG;
+    if (!std::isfinite(scale) || window < 0 || (!causal && (window || slopes))) return QE_ERR_ARG;
+    if (!q_start && total != batch * max_q) return QE_ERR_ARG;
+    if (total == 0 || batch == 0 || max_q == 0) return QE_OK;
+    if (!Q || !pages || !lengths || !out || (width > 0 && !table) || misaligned(pages, 16)) return QE_ERR_ARG;
+    if (misaligned(Q, dtype_bytes(dtype)) || misaligned(out, dtype_bytes(dtype))) return QE_ERR_ARG;
+    if (!ws || ws_bytes < qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim)) return QE_ERR_WORKSPACE;
+    KvAttn a{};
+    a.c = kv_cache(pages, num_pages, page, kv_heads, dim);
+    a.q = Q;
+    a.out = out;
+    a.lse = lse;
+    a.qt = q_stride;
+    a.qh = q_head_stride;
+    a.ot = o_stride;
+    a.oh = o_head_stride;
+    a.q_start = q_start;
+    a.total = total;
+    a.max_q = std::min(max_q, total);
+    a.width = width;
+    a.batch = (int32_t)batch;
+    a.heads = heads;
+    a.table = table;
+    a.lengths = lengths;
+    a.scale = scale;
+    a.causal = causal ? 1 : 0;
+    a.window = window;
+    a.slopes = slopes;
+    a.dtype = dtype;
+    a.group = group;
+    a.status = static_cast<int*>(ws);
+    return launch_kv_attn(a, ws, as_stream(stream));
 }
 
 }  // extern "C"

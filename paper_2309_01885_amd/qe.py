@@ -42,6 +42,10 @@ QE_CD_DENSE = 0x10000
 QE_DEBUG_CHECKS = 0x40
 QE_OBJ_IN = 0x80
 
+QE_F32 = 0
+QE_F16 = 1
+QE_BF16 = 2
+
 
 def QE_RELAX_PERIOD(k: int) -> int:
     """Flag bits for relaxed sweeps every k-th sweep of a call (qe.h)."""
@@ -81,6 +85,15 @@ SIGNATURES = {
     "qe_objective": (_int, [_vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
     "qe_lambda_workspace_size": (_sz, [_i64]),
     "qe_lambda_max": (_int, [_vp, _i64, _int, _f32, ctypes.POINTER(_f32), _vp, _sz, _vp]),
+    "qe_kv_page_bytes": (_i64, [_int, _int, _int, _int]),
+    "qe_kv_write": (_int, [_vp, _vp, _int, _i64, _int, _int, _i64, _i64, _i64, _i64, _vp, _int, _vp, _i64,
+                           _int, _vp, _vp]),
+    "qe_kv_read": (_int, [_vp, _i64, _int, _vp, _i64, _int, _int, _int, _vp, _vp, _int, _i64, _i64, _i64,
+                          _i64, _vp, _vp]),
+    "qe_kv_attn_workspace_size": (_sz, [_i64, _i64, _i64, _int, _int, _int]),
+    "qe_kv_attn": (_int, [_vp, _int, _i64, _int, _int, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _int, _int,
+                          _int, _vp, _i64, _vp, _f32, _int, _int, _vp, _vp, _i64, _i64, _vp, _vp, _sz,
+                          _vp]),
 }
 
 _lib = None
@@ -371,3 +384,138 @@ def lambda_max(Sigma: torch.Tensor, max_iters: int = 500, tol: float = 1e-7,
                              float(tol), ctypes.byref(out), _vp(ws.data_ptr()), ws.numel(),
                              _stream(stream)), "qe_lambda_max")
     return float(out.value)
+
+
+# ---------------------------------------------------------------------------- key/value cache in 4 bits
+_DTYPES = {torch.float32: QE_F32, torch.float16: QE_F16, torch.bfloat16: QE_BF16}
+
+
+def _heads(t: torch.Tensor, name: str, shape=None, dtype=None):
+    """A tokens x heads x dim tensor whose channels are contiguous: (pointer, dtype code, strides)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be {dtype or 'float32, float16 or bfloat16'}, got {t.dtype}")
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be {tuple(shape) if shape is not None else 'tokens x heads x dim'}, "
+                         f"got {tuple(t.shape)}")
+    if t.numel() > 0 and t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: the channels of a head must be contiguous")
+    return _vp(t.data_ptr()), _DTYPES[t.dtype], t.stride(0), t.stride(1)
+
+
+def _pages(pages: torch.Tensor, dim: int, group: int):
+    """Checks a cache made by kv_pages: (pointer, pages, tokens of a page, kv heads)."""
+    if pages.dim() != 4:
+        raise ValueError("pages must be pages x kv_heads x page / 32 x record bytes (kv_pages)")
+    num, kv, per, rec = pages.shape
+    need = load().qe_kv_page_bytes(kv, dim, group, 32 * per)
+    if need == 0 or need != kv * per * rec:
+        raise ValueError(f"pages do not fit dim {dim} and group {group}")
+    return _ptr(pages, torch.uint8, "pages"), num, 32 * per, kv
+
+
+def _same_device(ref: torch.Tensor, **others):
+    for name, t in others.items():
+        if t is not None and t.device != ref.device:
+            raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+
+
+def kv_page_bytes(kv_heads: int, dim: int, group: int = 64, page: int = 64) -> int:
+    return int(load().qe_kv_page_bytes(kv_heads, dim, group, page))
+
+
+def kv_pages(num_pages: int, kv_heads: int, dim: int, group: int = 64, page: int = 64,
+             device="cuda") -> torch.Tensor:
+    """An empty 4-bit key/value cache: uint8, pages x kv_heads x page / 32 x record bytes (qe.h)."""
+    nbytes = kv_page_bytes(kv_heads, dim, group, page)
+    if nbytes == 0 or num_pages < 1:
+        raise ValueError("dim must be a multiple of 8 up to 256, group 32, 64 or 128, page a multiple of 32")
+    return torch.zeros((num_pages, kv_heads, page // 32, nbytes // kv_heads // (page // 32)),
+                       dtype=torch.uint8, device=device)
+
+
+def kv_write(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, group: int = 64,
+             status: Optional[torch.Tensor] = None, stream=None):
+    """Quantizes K and V (tokens x kv_heads x dim; any token and head strides) into the
+    slots (int64) of the cache (qe_kv_write).  status: None or an int32 device tensor of one element,
+    set to QE_ERR_ARG by a slot past the cache (never cleared)."""
+    lib = load()
+    if pages.dim() != 4 or K.dim() != 3:
+        raise ValueError("K must be tokens x kv_heads x dim, pages a cache of kv_pages")
+    n, kv, dim = K.shape
+    pp, num, page, heads = _pages(pages, dim, group)
+    kp, dt, kt, kh = _heads(K, "K", (n, heads, dim))
+    vp, _, vt, vh = _heads(V, "V", (n, heads, dim), K.dtype)
+    _same_device(pages, K=K, V=V, slots=slots, status=status)
+    _check(lib.qe_kv_write(kp, vp, dt, n, heads, dim, kt, kh, vt, vh, _ptr(slots, torch.int64, "slots", n), group,
+                           pp, num, page, _ptr(status, torch.int32, "status", 1), _stream(stream)), "qe_kv_write")
+    return pages
+
+
+def kv_read(pages: torch.Tensor, slots: torch.Tensor, dim: int, group: int = 64, dtype=torch.float32,
+            K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None,
+            status: Optional[torch.Tensor] = None, stream=None):
+    """The keys and values (tokens x kv_heads x dim) that the cache holds at the slots
+    (qe_kv_read); into K and V where given."""
+    lib = load()
+    pp, num, page, heads = _pages(pages, dim, group)
+    n = slots.numel()
+    if K is None:
+        K = torch.empty((n, heads, dim), dtype=dtype, device=pages.device)
+    if V is None:
+        V = torch.empty((n, heads, dim), dtype=K.dtype, device=pages.device)
+    kp, dt, kt, kh = _heads(K, "K", (n, heads, dim))
+    vp, _, vt, vh = _heads(V, "V", (n, heads, dim), K.dtype)
+    _same_device(pages, K=K, V=V, slots=slots, status=status)
+    _check(lib.qe_kv_read(pp, num, page, _ptr(slots, torch.int64, "slots"), n, heads, dim, group, kp, vp, dt, kt,
+                          kh, vt, vh, _ptr(status, torch.int32, "status", 1), _stream(stream)), "qe_kv_read")
+    return K, V
+
+
+def kv_attn_workspace_size(total: int, batch: int, max_q: int, heads: int, kv_heads: int, dim: int) -> int:
+    return int(load().qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim))
+
+
+def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+            group: int = 64, q_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None,
+            scale: Optional[float] = None, causal: bool = True, window: int = 0,
+            slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+            lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, check: bool = False,
+            stream=None) -> torch.Tensor:
+    """Attention of Q (total x heads x dim) over the 4-bit cache (qe_kv_attn).
+
+    table (int32, sequences x pages) and lengths (int32) describe the sequences; q_start (int32,
+    sequences + 1) and max_q their queries, without them total / sequences queries each.
+    scale: 1 / sqrt(dim) unless given.  lse: None or float32, total x heads, written.  The call does
+    not wait for the device; check=True does, and raises if it met a bad page number, length or
+    query range (sync_status(ws) tells later otherwise)."""
+    lib = load()
+    if Q.dim() != 3 or table.dim() != 2:
+        raise ValueError("Q must be total x heads x dim, table sequences x pages")
+    total, heads, dim = Q.shape
+    batch, width = table.shape
+    pp, num, page, kv = _pages(pages, dim, group)
+    if q_start is None:
+        if max_q is None:
+            max_q = total // batch if batch else 0
+        if total != batch * max_q:
+            raise ValueError(f"{total} queries are not {max_q} for each of {batch} sequences: give q_start")
+    elif max_q is None:
+        raise ValueError("q_start needs max_q, the largest number of queries of a sequence")
+    if out is None:
+        out = torch.empty((total, heads, dim), dtype=Q.dtype, device=Q.device)
+    qp, dt, qt, qh = _heads(Q, "Q")
+    op, _, ot, oh = _heads(out, "out", (total, heads, dim), Q.dtype)
+    if ws is None:
+        ws = workspace(kv_attn_workspace_size(total, batch, max_q, heads, kv, dim), Q.device)
+    _same_device(pages, Q=Q, table=table, lengths=lengths, q_start=q_start, slopes=slopes, out=out, lse=lse, ws=ws)
+    _check(lib.qe_kv_attn(qp, dt, total, heads, dim, qt, qh,
+                          _ptr(q_start, torch.int32, "q_start", batch + 1), batch, max_q, pp, num, page, kv, group,
+                          _ptr(table, torch.int32, "table"), width, _ptr(lengths, torch.int32, "lengths", batch),
+                          1.0 / dim ** 0.5 if scale is None else float(scale), 1 if causal else 0, int(window),
+                          _ptr(slopes, torch.float32, "slopes", heads), op, ot, oh,
+                          _ptr(lse, torch.float32, "lse", total * heads), _vp(ws.data_ptr()), ws.numel(),
+                          _stream(stream)), "qe_kv_attn")
+    _finish(ws, check, "qe_kv_attn", stream)
+    return out
