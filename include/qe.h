@@ -414,7 +414,9 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  * Products run on the fp16 matrix cores: codes are exact there, a query row is
  * scaled by a power of two and rounded to fp16 (exact for fp16 and bf16 inputs up to
  * 2^-25 of the row's largest value; fp32 rows and their probabilities are split into two
- * fp16 parts each), probabilities are rounded to fp16; statistics and sums are fp32.
+ * fp16 parts each), probabilities times value scales are rounded to fp16 (to 2^-11 of
+ * themselves, or 2^-35 of the largest such product where that is more); statistics and
+ * sums are fp32.
  * max_q: at least every nq.  Lengths past width * page, queries past `total` or max_q and
  * page numbers outside of the cache set QE_ERR_ARG in the workspace's status word (which
  * this call never clears; qe_sync_status does) and count as absent. */

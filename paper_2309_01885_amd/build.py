@@ -4,6 +4,8 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -12,7 +14,7 @@ LIB = os.path.join(HERE, "libqe.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Wall", "-Wno-unused-result",
     # keep the compiler from forming packed fp32 instructions (v_pk_*_f32)
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -28,9 +30,8 @@ PEAK_SRC = os.path.join(HERE, "peak", "peak.hip")
 PEAK_LIB = os.path.join(HERE, "libqe_peak.so")
 
 
-def _hipcc(srcs, out, verbose):
-    tmp = out + ".tmp"
-    cmd = [HIPCC] + FLAGS + srcs + ["-o", tmp]
+def _run(args, what, verbose):
+    cmd = [HIPCC] + FLAGS + args
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -38,10 +39,20 @@ def _hipcc(srcs, out, verbose):
     err = "\n".join(l for l in (r.stderr or "").splitlines() if noise not in l)
     if r.returncode != 0:
         sys.stderr.write(err + "\n")
-        raise RuntimeError(f"hipcc failed building {os.path.basename(out)}")
+        raise RuntimeError(f"hipcc failed building {what}")
     if verbose and err.strip():
         sys.stderr.write(err + "\n")
-    os.replace(tmp, out)
+
+
+def _hipcc(srcs, out, verbose):
+    """Compiles the sources side by side (at most 8 at a time) and links them."""
+    with tempfile.TemporaryDirectory(prefix="qe_build_") as tmp:
+        objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in srcs]
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: _run(["-c", so[0], "-o", so[1]], os.path.basename(so[0]), verbose),
+                          zip(srcs, objs)))
+        _run(["-shared"] + objs + ["-o", out + ".tmp"], os.path.basename(out), verbose)
+    os.replace(out + ".tmp", out)
     return out
 
 

@@ -393,7 +393,7 @@ size_t qe_kv_attn_workspace_size(int64_t total, int64_t batch, int64_t max_q, in
 {
     if (total < 0 || batch < 0 || max_q < 0 || bad_kv(1, kKvTok, kv_heads, dim, 32)) return 0;
     if (heads < 1 || heads % kv_heads) return 0;
-    return kv_attn_ws_bytes(std::min(batch, total), std::min(max_q, total), heads, kv_heads, dim);
+    return kv_attn_ws_bytes(batch, std::min(max_q, total), heads, kv_heads, dim);
 }
 
 qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,

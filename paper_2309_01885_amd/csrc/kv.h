@@ -98,6 +98,7 @@ struct KvAttn {
     int32_t causal, window;
     const float* slopes;           // or null
     int32_t dtype, group;
+    bool vec_q;                    // 16-byte loads of Q
     int* status;
 };
 

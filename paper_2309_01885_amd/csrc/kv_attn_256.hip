@@ -1,0 +1,6 @@
+// Attention over the 4-bit cache: heads padded to 256 channels.
+#include "kv_attn.h"
+
+namespace qe {
+template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
+}
