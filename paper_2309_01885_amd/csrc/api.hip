@@ -408,6 +408,7 @@ qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim
     if (total < 0 || total > 0x7fffffff || batch < 0 || batch > 0x7fffffff || max_q < 0 || width < 0) return QE_ERR_ARG;
     if (!std::isfinite(scale) || window < 0 || (!causal && (window || slopes))) return QE_ERR_ARG;
     if (!q_start && total != batch * max_q) return QE_ERR_ARG;
+    if (std::min(max_q, total) * (heads / kv_heads) > 0x7fffffff - 1024) return QE_ERR_ARG;   // query rows of a sequence and key head
     if (total == 0 || batch == 0 || max_q == 0) return QE_OK;
     if (!Q || !pages || !lengths || !out || (width > 0 && !table) || misaligned(pages, 16)) return QE_ERR_ARG;
     if (misaligned(Q, dtype_bytes(dtype)) || misaligned(out, dtype_bytes(dtype))) return QE_ERR_ARG;

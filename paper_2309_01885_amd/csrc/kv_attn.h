@@ -29,7 +29,7 @@ constexpr float kLog2e = 1.44269504088896341f;
 // heads per key head + head in the group) of one sequence and key head; each unit has
 // nsplit workgroups along the tokens, whose results kv_join_kernel joins.
 struct KvPlan {
-    int64_t row_tiles;                      // units of a sequence and key head
+    int64_t row_tiles, units;               // units of a sequence and key head; of the call
     int nsplit, rows;
     float* part;                            // nsplit > 1: (unit, split, row, DP) sums relative to the maximum
     float* stat;                            // (unit, split, row, 2): maximum (log2) and mass
@@ -37,50 +37,54 @@ struct KvPlan {
 
 // What a workgroup works on; the join recomputes it.
 struct KvUnit {
-    int64_t first, pos0, len;               // first row of Q, position of query 0, cached tokens
-    int nq, rec0, rec1, splits;             // queries; records that any row of the unit sees; splits in use
+    int64_t unit, first, pos0;              // first row of Q, position of query 0
+    int b, kvh, per, tile_row, rows;        // per: heads of a key head; the unit's first row; rows of the sequence
+    int len, nq, rec0, rec1, splits;        // cached tokens, queries; records that some row sees; splits in use
 };
 
 // Records a split has at least (a workgroup's waves take them in turn).
 constexpr int kKvMinRecords = 4;
 
-__device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t b, int64_t tile, bool report)
+__device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit, bool report)
 {
     KvUnit u;
+    const int64_t bh = unit / p.row_tiles, tile = unit - bh * p.row_tiles;
+    u.unit = unit;
+    u.b = (int)(bh / a.c.heads);
+    u.kvh = (int)(bh - (int64_t)u.b * a.c.heads);
+    u.per = a.heads / a.c.heads;
     bool bad = false;
-    u.first = b * a.max_q;
+    u.first = u.b * a.max_q;
     int64_t nq = a.max_q;
     if (a.q_start) {
-        u.first = a.q_start[b];
-        nq = (int64_t)a.q_start[b + 1] - u.first;
+        u.first = a.q_start[u.b];
+        nq = (int64_t)a.q_start[u.b + 1] - u.first;
         bad = u.first < 0 || nq < 0 || nq > a.max_q || u.first + nq > a.total;
         u.first = u.first < 0 ? 0 : u.first;
-        nq = min(min(nq, a.max_q), a.total - u.first);
+        nq = max((int64_t)0, min(min(nq, a.max_q), a.total - u.first));
     }
     const int64_t room = a.width * (int64_t)a.c.per * kKvTok;
-    u.len = a.lengths[b];
-    bad = bad || u.len < 0 || u.len > room;
-    u.len = u.len < 0 ? 0 : min(u.len, room);
-    if (bad && report) set_status(a.status, QE_ERR_ARG);
-    u.nq = nq < 0 ? 0 : (int)nq;
-    u.pos0 = u.len - u.nq;
-    // the rows of the unit are queries i0 .. i1
-    const int per = a.heads / a.c.heads;
-    const int64_t i0 = tile * p.rows / per, i1 = min((int64_t)u.nq, (tile * p.rows + p.rows + per - 1) / per) - 1;
-    int64_t end = a.causal ? min(u.len, u.pos0 + i1 + 1) : u.len;
-    int64_t begin = a.window ? max((int64_t)0, u.pos0 + i0 - a.window + 1) : 0;
-    if (i0 >= u.nq || end < begin) end = begin = 0;
+    int64_t len = a.lengths[u.b];
+    bad = bad || len < 0 || len > room;
+    len = len < 0 ? 0 : min(len, room);
+    if (bad && report && tile == 0 && u.kvh == 0) set_status(a.status, QE_ERR_ARG);
+    u.len = (int)len;
+    u.nq = (int)nq;
+    u.pos0 = len - nq;
+    const int64_t r0 = tile * p.rows, rows = nq * u.per;
+    u.tile_row = (int)min(r0, rows);        // (rows of a sequence: below 2^31, checked on the host)
+    u.rows = (int)rows;
+    // the unit's queries i0 .. i1
+    const int64_t i0 = r0 / u.per, i1 = min(nq, (r0 + p.rows + u.per - 1) / u.per) - 1;
+    int64_t end = a.causal ? min(len, u.pos0 + i1 + 1) : len;
+    const int64_t begin = a.window ? max((int64_t)0, u.pos0 + i0 - a.window + 1) : 0;
+    if (r0 >= rows || end < begin) end = begin;
     u.rec0 = (int)(begin / kKvTok);
-    u.rec1 = (int)((end + kKvTok - 1) / kKvTok);
+    u.rec1 = end > begin ? (int)((end + kKvTok - 1) / kKvTok) : u.rec0;
     u.splits = max(1, min(p.nsplit, (u.rec1 - u.rec0) / kKvMinRecords));
     return u;
 }
 
-__device__ inline float kv_q_elem(const KvAttn& a, int64_t at)
-{
-    return a.dtype == QE_F32 ? static_cast<const float*>(a.q)[at]
-         : a.dtype == QE_F16 ? (float)static_cast<const _Float16*>(a.q)[at] : (float)static_cast<const __bf16*>(a.q)[at];
-}
 __device__ inline void kv_q8(const KvAttn& a, int64_t at, float* x)
 {
     if (a.dtype == QE_F32) kv_load8(static_cast<const float*>(a.q) + at, a.vec_q, x);
@@ -150,153 +154,333 @@ __device__ inline float kv_sum4(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// NT tiles of 16 query rows per wave.  ROWS: the workgroup's waves have rows of their own
-// and see the same tokens; else they share the rows and take the records in turn.
-// PARTS: fp16 parts of a query and of a probability (2 for fp32 calls).
-template <int DP, int GROUP, int NT, int PARTS, bool ROWS>
-__global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttn a, KvPlan plan)
-{
+// Channels a lane's words are made of.  A key word is an octet: row `token`, octet 4 c + j.  A
+// value word is a unit of 4 channels of two tokens; a unit tile is 16 units (one channel
+// class of theirs is a product's 16 rows), with groups of 32 it is 8 (two classes are).
+template <int DP, int GROUP> struct KvTiles {
     using R = KvRec<DP, GROUP>;
-    constexpr int NC = R::NC, NG = R::NG;
-    constexpr int CPG = GROUP / 32;                      // 32-channel products of a key group
-    // products of a record's values: a lane's unit is 4 channels; groups of 32 pair two
-    // classes of 8 units, wider ones one class of 16
-    constexpr bool kHalf = GROUP == 32;
-    constexpr int UT = kHalf ? DP / 32 : (DP + 63) / 64; // unit tiles
-    constexpr int CL = kHalf ? 2 : 4;                    // channel classes of a unit tile
-    const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int split = (int)(wg % plan.nsplit);
-    const int64_t unit = wg / plan.nsplit, bh = unit / plan.row_tiles, tile = unit - bh * plan.row_tiles;
-    const int64_t b = bh / a.c.heads;
-    if (b >= a.batch) return;
-    const int kvh = (int)(bh - b * a.c.heads);
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int i = tid & 15, j = (tid & 63) >> 4;
-    const KvUnit u = kv_unit(a, plan, b, tile, tid == 0 && split == 0 && tile == 0 && kvh == 0);
-    if (split >= u.splits) return;
-    const int per = a.heads / a.c.heads;
-    const int64_t rows = (int64_t)u.nq * per;
-    const int64_t row0 = tile * plan.rows + (ROWS ? wave * (16 * NT) : 0);
-    if ((ROWS ? row0 : tile * plan.rows) >= rows) return;
+    static constexpr int NC = R::NC, NG = R::NG;
+    static constexpr int CPG = GROUP / 32;                       // 32-channel products of a key group
+    static constexpr bool kHalf = GROUP == 32;
+    static constexpr int UT = kHalf ? DP / 32 : (DP + 63) / 64;  // unit tiles
+    static constexpr int CL = kHalf ? 2 : 4;                     // classes of a unit tile
+    // token (of the record) whose key row is row i of half h
+    __device__ static int key_token(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+    __device__ static int unit(int t, int i)
+    {
+        const int u = kHalf ? 8 * t + (i & 7) : 16 * t + i;
+        return DP % 64 == 0 || kHalf ? u : min(u, DP / 4 - 1);   // (rows past the last unit give channels past DP)
+    }
+    static constexpr int group_of(int t) { return (kHalf ? 32 * t : 64 * t) / GROUP; }
+    __device__ static int channel(int t, int k, int row) { return kHalf ? 32 * t + 4 * (row & 7) + k + 2 * (row >> 3) : 64 * t + 4 * row + k; }
+    static constexpr bool kWhole = DP % 64 == 0 || kHalf;        // every channel() is below DP
+};
 
-    // ---- the query rows: scaled by 2^e to a largest element in [2^14, 2^15), rounded to fp16
+// The zero points of a key row as the pairs kv_code_pair takes.
+__device__ inline void kv_key_zero(uint32_t word, uint32_t& lo, uint32_t& hi)
+{
+    const uint32_t z = word & 15u, z2 = z << 16 | z;
+    lo = z2 | 0xE400E400u;
+    hi = z2 << 4 | 0xE400E400u;
+}
+// Of two tokens' value words.
+__device__ inline void kv_value_zero(uint32_t w0, uint32_t w1, uint32_t& lo, uint32_t& hi)
+{
+    const uint32_t z2 = __builtin_amdgcn_perm(w1, w0, 0x05040100u) & 0x000F000Fu;
+    lo = z2 | 0xE400E400u;
+    hi = z2 << 4 | 0xE400E400u;
+}
+__device__ inline f16x8 kv_key_frag(uint32_t w, uint32_t lo, uint32_t hi)
+{
+    const uint32_t w8 = w >> 8;
+    return kv_frag(kv_code_pair(w, false, lo), kv_code_pair(w, true, hi), kv_code_pair(w8, false, lo), kv_code_pair(w8, true, hi));
+}
+
+// A wave's query rows, 16 a tile, and what they see.
+template <int NC, int NT, int PARTS> struct KvRows {
     f16x8 q[PARTS][NT][NC];
-    float cq[NT], slope[NT];
-    int64_t lo[NT], hi[NT];                              // the tokens that the lane's row sees
-    int64_t all_lo = 0, all_hi = u.len;                  // that every row of the wave sees
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int64_t row = row0 + 16 * n + i;
-        const bool have = row < rows;
-        const int qi = have ? (int)(row / per) : 0, head = kvh * per + (have ? (int)(row - (int64_t)qi * per) : 0);
-        float x[NC][8];
-        float top = 0.f;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[c][e] = 0.f;
-            const int d = 8 * (4 * c + j);
-            if (have && d < a.c.dim) kv_q8(a, (u.first + qi) * a.qt + head * a.qh + d, x[c]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[c][e]));
-        }
-        top = kv_max4(top);
-        // (a row of zeros, NaN or infinities keeps its values)
-        const int e2 = top > 0.f && top <= 3.402823466e38f ? max(-100, min(100, 15 - (int)((__float_as_uint(top) >> 23) - 126))) : 0;
-        const float mul = __uint_as_float((uint32_t)(127 + e2) << 23) * (a.scale < 0.f ? -1.f : 1.f);
-        cq[n] = fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e2) << 23);
-        slope[n] = a.slopes && have ? a.slopes[head] * kLog2e : 0.f;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            // (channels 1, 3, 5, 7 meet codes in bits 4-7, 16 times as large)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[c][e] *= mul;
-            uint32_t h[4], m[4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const float f = p & 1 ? 0.0625f : 1.f;
-                const _Float16 h0 = (_Float16)(x[c][p] * f), h1 = (_Float16)(x[c][p + 4] * f);
-                const f16x2 hv = {h0, h1};
-                h[p] = __builtin_bit_cast(uint32_t, hv);
-                if constexpr (PARTS == 2) {
-                    const _Float16 m0 = (_Float16)(x[c][p] * f - (float)h0), m1 = (_Float16)(x[c][p + 4] * f - (float)h1);
-                    const f16x2 mv = {m0, m1};
-                    m[p] = __builtin_bit_cast(uint32_t, mv);
-                }
-            }
-            q[0][n][c] = kv_frag(h[0], h[1], h[2], h[3]);
-            if constexpr (PARTS == 2) q[1][n][c] = kv_frag(m[0], m[1], m[2], m[3]);
-        }
-        const int64_t pos = u.pos0 + qi;
-        hi[n] = !have ? u.len : a.causal ? min(u.len, pos + 1) : u.len;
-        lo[n] = have && a.window ? pos - a.window + 1 : 0;
-    }
-    int64_t any_lo = 0, any_hi = u.len;                  // that some row of the wave sees
-    if (a.causal) {
-        // the first and the last row of the wave bound the others
-        const int64_t last = min(rows, row0 + 16 * NT) - 1;
-        all_hi = min(u.len, u.pos0 + row0 / per + 1);
-        any_hi = min(u.len, u.pos0 + last / per + 1);
-        if (a.window) {
-            all_lo = u.pos0 + last / per - a.window + 1;
-            any_lo = u.pos0 + row0 / per - a.window + 1;
-        }
-    }
+    float c[NT], slope[NT];                 // score of a product: c s + slope (t - pos), in powers of two
+    int lo[NT], hi[NT];                     // the tokens that the lane's row sees
+    int all_lo, all_hi, any_lo, any_hi;     // that every row and that some row of the wave sees
 
-    // ---- the sums
+    // A row is scaled by 2^e to a largest element in [2^14, 2^15) and rounded to fp16.
+    __device__ void load(const KvAttn& a, const KvUnit& u, int row0)
+    {
+        const int i = threadIdx.x & 15, j = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int row = row0 + 16 * n + i;
+            const bool have = row < u.rows;
+            const int qi = have ? row / u.per : 0, head = u.kvh * u.per + (have ? row - qi * u.per : 0);
+            float x[NC][8], top = 0.f;
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[k][e] = 0.f;
+                const int d = 8 * (4 * k + j);
+                if (have && d < a.c.dim) kv_q8(a, (u.first + qi) * a.qt + head * a.qh + d, x[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[k][e]));
+            }
+            top = kv_max4(top);
+            // (a row of zeros, NaN or infinities keeps its values)
+            const int e2 = top > 0.f && top <= 3.402823466e38f ? max(-100, min(100, 141 - (int)(__float_as_uint(top) >> 23))) : 0;
+            const float mul = __uint_as_float((uint32_t)(127 + e2) << 23) * (a.scale < 0.f ? -1.f : 1.f);
+            c[n] = fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e2) << 23);
+            slope[n] = a.slopes && have ? a.slopes[head] * kLog2e : 0.f;
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                uint32_t h[4], m[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    // (channels 1, 3, 5, 7 meet 16 times their codes)
+                    const float f = p & 1 ? 0.0625f * mul : mul, x0 = x[k][p] * f, x1 = x[k][p + 4] * f;
+                    const f16x2 hv = {(_Float16)x0, (_Float16)x1};
+                    h[p] = __builtin_bit_cast(uint32_t, hv);
+                    if constexpr (PARTS == 2) m[p] = kv_pack(x0 - (float)hv[0], x1 - (float)hv[1]);
+                }
+                q[0][n][k] = kv_frag(h[0], h[1], h[2], h[3]);
+                if constexpr (PARTS == 2) q[1][n][k] = kv_frag(m[0], m[1], m[2], m[3]);
+            }
+            const int64_t pos = u.pos0 + qi;
+            hi[n] = have && a.causal ? (int)max((int64_t)0, pos + 1) : u.len;
+            lo[n] = have && a.window ? (int)max((int64_t)0, pos - a.window + 1) : 0;
+        }
+        all_lo = any_lo = 0;
+        all_hi = any_hi = u.len;
+        if (a.causal) {
+            // the first and the last row bound the others
+            const int64_t p0 = u.pos0 + row0 / u.per, p1 = u.pos0 + (min(u.rows, row0 + 16 * NT) - 1) / u.per;
+            all_hi = (int)max((int64_t)0, p0 + 1);
+            any_hi = (int)max((int64_t)0, p1 + 1);
+            if (a.window) {
+                any_lo = (int)max((int64_t)0, p0 - a.window + 1);
+                all_lo = (int)max((int64_t)0, p1 - a.window + 1);
+            }
+        }
+    }
+    __device__ bool masked(int t0) const { return t0 > all_hi - kKvTok || t0 < all_lo; }
+};
+
+// The running softmax and the weighted sums of a wave's rows, o[t][k][n][e]: channel(t, k, 4 j + e).
+// Probabilities are kept as p 2^shift, shift one number for all rows that brings the product with
+// the largest value scale so far to [2^10, 2^11): 2^15 at most, since p reaches 2^4 before the
+// maximum moves.  It drops out of o / mass.
+template <int UT, int CL, int NT> struct KvSums {
     f32x4 o[UT][CL][NT];
     float top[NT], mass[NT];
-    float limit[NG], norm[NG];                           // largest value scale allowed; 2^10 / its power of two
+    float shift, limit;                     // limit: the largest value scale that fits shift
+
+    __device__ void clear()
+    {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int t = 0; t < UT; ++t)
+#pragma unroll
+                for (int k = 0; k < CL; ++k) o[t][k][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            top[n] = -kKvInf;
+            mass[n] = 0.f;
+        }
+        shift = 0.f;
+        limit = 0.f;
+    }
+    __device__ void scale_row(int n, float f)
+    {
+        mass[n] *= f;
 #pragma unroll
         for (int t = 0; t < UT; ++t)
 #pragma unroll
-            for (int c = 0; c < CL; ++c) o[t][c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        top[n] = -kKvInf;
-        mass[n] = 0.f;
-    }
+            for (int k = 0; k < CL; ++k)
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-        limit[g] = 0.f;
-        norm[g] = 1.f;
+                for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
     }
+    // big: a lane's largest value scale
+    __device__ void fit(float big)
+    {
+        if (!__any(big > limit)) return;
+        big = kv_max4(big);
+        const uint32_t ex = max(__builtin_amdgcn_readfirstlane(__float_as_uint(big)) >> 23, 77u);   // (shift at most 60)
+        const float to = (float)(137 - (int)ex), f = limit == 0.f ? 1.f : __builtin_amdgcn_exp2f(to - shift);
+        limit = __uint_as_float(ex << 23 | 0x7fffffu);
+        shift = to;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) scale_row(n, f);
+    }
+    // s: the products times their key scales; on return p 2^shift (0 where the row sees nothing)
+    template <int NC, int PARTS> __device__ void weigh(float (&s)[NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, int t0, bool masked)
+    {
+        const int t = t0 + 8 * ((threadIdx.x & 63) >> 4);
+        float c[NT], big[NT];
+        uint32_t vis[NT];
+        bool move = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            c[n] = r.c[n];
+            if (slopes) {
+                const float base = r.slope[n] * (float)(t - (r.hi[n] - 1));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[n][e] = fmaf(s[n][e], c[n], fmaf(r.slope[n], (float)e, base));
+                c[n] = 1.f;
+            }
+            vis[n] = 0xffu;
+            if (masked) {
+                big[n] = -kKvInf;
+                vis[n] = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool see = t + e >= r.lo[n] && t + e < r.hi[n];
+                    vis[n] |= (see ? 1u : 0u) << e;
+                    big[n] = see ? fmaxf(big[n], s[n][e]) : big[n];
+                }
+            } else {
+                big[n] = fmaxf(fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])), fmaxf(fmaxf(s[n][4], s[n][5]), fmaxf(s[n][6], s[n][7])));
+            }
+            big[n] *= c[n];
+            move = move || big[n] > top[n] + 4.f;
+        }
+        if (__any(move)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float m = kv_max4(fmaxf(top[n], big[n]));
+                const float f = m == top[n] ? 1.f : __builtin_amdgcn_exp2f(top[n] - m);
+                top[n] = m;
+                scale_row(n, f);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float off = shift - top[n];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c[n], off));
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[n][e] = vis[n] >> e & 1u ? s[n][e] : 0.f;
+            }
+            mass[n] += ((s[n][0] + s[n][1]) + (s[n][2] + s[n][3])) + ((s[n][4] + s[n][5]) + (s[n][6] + s[n][7]));
+        }
+    }
+    // the products' fp16 weights p s' of a group
+    template <int PARTS> __device__ static void weights(const float (&s)[NT][8], const float (&sv)[8], bool masked, f16x8 (&pr)[PARTS][NT])
+    {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            uint32_t h[4], m[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
+                if (masked) {                            // (a NaN scale of a token that the row does not see)
+                    x0 = s[n][2 * p] == 0.f ? 0.f : x0;
+                    x1 = s[n][2 * p + 1] == 0.f ? 0.f : x1;
+                }
+                h[p] = kv_pack(x0, x1);
+                if constexpr (PARTS == 2) {
+                    const f16x2 hv = __builtin_bit_cast(f16x2, h[p]);
+                    m[p] = kv_pack(x0 - (float)hv[0], x1 - (float)hv[1]);
+                }
+            }
+            pr[0][n] = kv_frag(h[0], h[1], h[2], h[3]);
+            if constexpr (PARTS == 2) pr[1][n] = kv_frag(m[0], m[1], m[2], m[3]);
+        }
+    }
+    // after the last record: plain sums (odd classes were 16 times as large), the rows' masses.  What is
+    // left of shift is a factor of both.
+    __device__ void finish()
+    {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            mass[n] = kv_sum4(mass[n]);
+#pragma unroll
+            for (int t = 0; t < UT; ++t)
+#pragma unroll
+                for (int k = 1; k < CL; k += 2)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][k][n][e] *= 0.0625f;
+        }
+    }
+};
 
+__device__ inline float kv_lse(float top, float mass) { return mass == 0.f ? -kKvInf : (top + __builtin_amdgcn_logf(mass)) / kLog2e; }
+
+// ---------------------------------------------------------------- few rows
+// A workgroup's waves share the rows of a unit (16 NT) and take its records in turn, each on its
+// own, with the next record's loads in flight; at the end they are joined through LDS.
+template <int DP, int GROUP, int NT, int PARTS>
+__global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
+{
+    using R = KvRec<DP, GROUP>;
+    using T = KvTiles<DP, GROUP>;
+    constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
+    const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t unit = wg / plan.nsplit;
+    const int split = (int)(wg - unit * plan.nsplit);
+    if (unit >= plan.units) return;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int i = tid & 15, j = (tid & 63) >> 4;
+    const KvUnit u = kv_unit(a, plan, unit, tid == 0 && split == 0);
+    if (split >= u.splits || u.tile_row >= u.rows) return;
     const int count = u.rec1 - u.rec0;
-    const int r0 = u.rec0 + (int)((int64_t)count * split / u.splits), r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
+    const int r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
+    int r = u.rec0 + (int)((int64_t)count * split / u.splits) + wave;
+
+    struct Raw {
+        uint32_t k[2][NC], v[UT][4], kw[NG][8], vw[NG][8], kz[2][NG];
+    };
+    constexpr bool kAll = 2 * NC + 4 * UT + 18 * NG <= 52;       // whether the words fit in flight besides the codes
     const int64_t pages = a.c.slots / ((int64_t)a.c.per * kKvTok);
-    for (int r = r0 + (ROWS ? 0 : wave); r < r1; r += ROWS ? 1 : kKvWaves) {
-        const int64_t t0 = (int64_t)r * kKvTok;
-        if (ROWS && (t0 >= any_hi || t0 + kKvTok <= any_lo)) continue;
-        const uint32_t pg = (uint32_t)r / a.c.per;
-        const int64_t id = a.table[b * a.width + pg];
-        if (id < 0 || id >= pages) {
+    const int32_t* table = a.table + u.b * a.width;
+    const int per = (int)a.c.per;
+    int pg = r / per, rem = r - pg * per;
+    int id = r < r1 ? table[pg] : 0;
+    const uint8_t* rec = nullptr;                                // of the record loaded last
+    auto codes = [&](Raw& w) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) kv_words<NC>(rec + T::key_token(i, h) * R::kKeyRow + j * (4 * NC), w.k[h]);
+#pragma unroll
+        for (int t = 0; t < UT; ++t) kv_words<4>(rec + R::kVal + T::unit(t, i) * (2 * kKvTok) + 16 * j, w.v[t]);
+    };
+    auto words = [&](const uint8_t* at, Raw& w) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const uint8_t* kp = at + R::kKeyWords + g * (4 * kKvTok);
+            kv_words<8>(kp + 32 * j, w.kw[g]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w.kz[h][g] = *reinterpret_cast<const uint32_t*>(kp + 4 * T::key_token(i, h));
+            kv_words<8>(at + R::kValWords + g * (4 * kKvTok) + 32 * j, w.vw[g]);
+        }
+    };
+    // Starts the loads of record r (its page number was read before); false where there is no such page.
+    auto start = [&](Raw& w) {
+        const bool ok = id >= 0 && id < pages;
+        if (ok) {
+            rec = a.c.pages + (((int64_t)id * a.c.heads + u.kvh) * per + rem) * R::kBytes;
+            codes(w);
+            if (kAll) words(rec, w);
+        } else if (r < r1) {
             set_status(a.status, QE_ERR_ARG);
-            continue;
         }
-        const uint8_t* rec = a.c.pages + ((id * a.c.heads + kvh) * a.c.per + ((uint32_t)r - pg * a.c.per)) * R::kBytes;
-        uint32_t kraw[2][NC], vraw[UT][4], kw[NG][8], vw[NG][8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) kv_words<NC>(rec + (8 * (i >> 2) + 4 * h + (i & 3)) * R::kKeyRow + j * (4 * NC), kraw[h]);
-#pragma unroll
-        for (int g = 0; g < NG; ++g) kv_words<8>(rec + R::kKeyWords + g * (4 * kKvTok) + 32 * j, kw[g]);
-#pragma unroll
-        for (int t = 0; t < UT; ++t) {
-            int unit4 = kHalf ? 8 * t + (i & 7) : 16 * t + i;
-            if (DP % 64 != 0 && !kHalf) unit4 = min(unit4, DP / 4 - 1);      // (the lanes past the last unit give nothing)
-            kv_words<4>(rec + R::kVal + unit4 * (2 * kKvTok) + 16 * j, vraw[t]);
+        rem += kKvWaves;
+        while (rem >= per) {
+            rem -= per;
+            ++pg;
         }
-#pragma unroll
-        for (int g = 0; g < NG; ++g) kv_words<8>(rec + R::kValWords + g * (4 * kKvTok) + 32 * j, vw[g]);
+        if (r + kKvWaves < r1) id = table[pg];
+        return ok;
+    };
 
-        uint32_t kz[2][NG];                              // zero points of the tokens whose codes the lane holds
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-                kz[h][g] = reinterpret_cast<const uint32_t*>(rec + R::kKeyWords)[g * kKvTok + 8 * (i >> 2) + 4 * h + (i & 3)] & 15u;
+    Raw now, next;
+    bool ok = false;
+    if (r < r1) ok = start(now);
+    const uint8_t* at = rec;
+    KvRows<NC, NT, PARTS> rows;
+    rows.load(a, u, u.tile_row);
+    KvSums<UT, CL, NT> sums;
+    sums.clear();
 
-        // ---- scores
+    auto work = [&](Raw& w, const uint8_t* base) {
+        const int t0 = r * kKvTok;
+        if (!kAll) words(base, w);
+        const bool masked = rows.masked(t0);
         float s[NT][8];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -306,262 +490,380 @@ __global__ __launch_bounds__(256, 2) void kv_attn_kernel(KvAttn a, KvPlan plan)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = g * CPG; c < (g + 1) * CPG && c < NC; ++c)
+            for (int h = 0; h < 2; ++h) {
+                uint32_t lo, hi;
+                kv_key_zero(w.kz[h][g], lo, hi);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t w = kraw[h][c], w8 = w >> 8;
-                    const uint32_t lo = kz[h][g] * 0x10001u | 0xE400E400u, hi = kz[h][g] * 0x100010u | 0xE400E400u;
-                    const f16x8 f = kv_frag(kv_code_pair(w, false, lo), kv_code_pair(w, true, hi),
-                                            kv_code_pair(w8, false, lo), kv_code_pair(w8, true, hi));
+                for (int k = g * T::CPG; k < (g + 1) * T::CPG && k < NC; ++k) {
+                    const f16x8 f = kv_key_frag(w.k[h][k], lo, hi);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, q[p][n][c], acc[n][h]);
+                        for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][k], acc[n][h]);
                 }
+            }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int e = 0; e < 8; ++e) {
+                const float sc = kv_scale(w.kw[g][e]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float sc = kv_scale(kw[g][e]), v = acc[n][e >> 2][e & 3];
+                for (int n = 0; n < NT; ++n) {
+                    const float v = acc[n][e >> 2][e & 3];
                     s[n][e] = g == 0 ? sc * v : fmaf(sc, v, s[n][e]);
                 }
+            }
         }
-
-        // ---- probabilities
-        const bool masked = t0 + kKvTok > all_hi || t0 < all_lo;
-        uint32_t seen = 0xffu;                           // tokens of the lane that lie before the sequence's end
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float c = cq[n];
-            if (a.slopes) {
-                const float base = slope[n] * (float)(int)(t0 + 8 * j - (hi[n] - 1));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[n][e] = fmaf(s[n][e], c, fmaf(slope[n], (float)e, base));
-                c = 1.f;
-            }
-            uint32_t vis = 0xffu;
-            float big;
-            if (masked) {
-                big = -kKvInf;
-                vis = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int64_t t = t0 + 8 * j + e;
-                    const bool see = t >= lo[n] && t < hi[n];
-                    vis |= (see ? 1u : 0u) << e;
-                    big = see ? fmaxf(big, s[n][e]) : big;
-                }
-            } else {
-                big = fmaxf(fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])), fmaxf(fmaxf(s[n][4], s[n][5]), fmaxf(s[n][6], s[n][7])));
-            }
-            big *= c;
-            // the maximum moves only when it has to: probabilities reach 2^4 before
-            if (__any(big > top[n] + 4.f)) {
-                const float m = kv_max4(fmaxf(top[n], big));
-                const float f = m == top[n] ? 1.f : __builtin_amdgcn_exp2f(top[n] - m);
-                top[n] = m;
-                mass[n] *= f;
-#pragma unroll
-                for (int t = 0; t < UT; ++t)
-#pragma unroll
-                    for (int k = 0; k < CL; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c, -top[n]));
-            if (masked) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[n][e] = vis >> e & 1u ? s[n][e] : 0.f;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mass[n] += s[n][e];
-        }
-        if (t0 + kKvTok > u.len) {
+        if (t0 > u.len - kKvTok) {
             // words past the sequence's end are anything: no scale of theirs may meet a 0
 #pragma unroll
-            for (int e = 0; e < 8; ++e) seen &= t0 + 8 * j + e < u.len ? ~0u : ~(1u << e);
+            for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int g = 0; g < NG; ++g)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) vw[g][e] = seen >> e & 1u ? vw[g][e] : 0u;
+                for (int g = 0; g < NG; ++g) w.vw[g][e] = t0 + 8 * j + e < u.len ? w.vw[g][e] : 0u;
         }
-
-        // ---- weighted sum of the values
+        float big = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) big = fmaxf(big, kv_scale(w.vw[g][e]));
+        sums.fit(big);
+        sums.weigh(s, rows, a.slopes != nullptr, t0, masked);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             float sv[8];
-            float big = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                sv[e] = kv_scale(vw[g][e]);
-                big = fmaxf(big, sv[e]);
-            }
-            // p s' stays below 2^15: s' is the scale over the largest one's power of two, times 2^10
-            if (__any(big > limit[g])) {
-                big = kv_max4(big);
-                big = fmaxf(big, __shfl_xor(big, 1));
-                const uint32_t ex = max(__float_as_uint(big) >> 23, 20u);
-                limit[g] = __uint_as_float(ex << 23 | 0x7fffffu);
-                const float to = __uint_as_float((264u - ex) << 23), f = to / norm[g];
-                norm[g] = to;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                    for (int t = 0; t < UT; ++t)
-                        if ((kHalf ? 32 * t : 64 * t) / GROUP == g)
-#pragma unroll
-                            for (int k = 0; k < CL; ++k)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sv[e] *= norm[g];
+            for (int e = 0; e < 8; ++e) sv[e] = kv_scale(w.vw[g][e]);
             f16x8 pr[PARTS][NT];
+            sums.template weights<PARTS>(s, sv, masked, pr);
+            uint32_t lo[4], hi[4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                uint32_t h[4], m[4];
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
-                    if (masked) {                        // (a NaN scale of a token that the row does not see)
-                        x0 = s[n][2 * p] == 0.f ? 0.f : x0;
-                        x1 = s[n][2 * p + 1] == 0.f ? 0.f : x1;
-                    }
-                    h[p] = kv_pack(x0, x1);
-                    if constexpr (PARTS == 2) {
-                        const f16x2 hv = __builtin_bit_cast(f16x2, h[p]);
-                        m[p] = kv_pack(x0 - (float)hv[0], x1 - (float)hv[1]);
-                    }
-                }
-                pr[0][n] = kv_frag(h[0], h[1], h[2], h[3]);
-                if constexpr (PARTS == 2) pr[1][n] = kv_frag(m[0], m[1], m[2], m[3]);
-            }
-            uint32_t z[4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) z[p] = __builtin_amdgcn_perm(vw[g][2 * p + 1], vw[g][2 * p], 0x05040100u) & 0x000F000Fu;
+            for (int p = 0; p < 4; ++p) kv_value_zero(w.vw[g][2 * p], w.vw[g][2 * p + 1], lo[p], hi[p]);
 #pragma unroll
             for (int t = 0; t < UT; ++t) {
-                if ((kHalf ? 32 * t : 64 * t) / GROUP != g) continue;
-                uint32_t w[4];
+                if (T::group_of(t) != g) continue;
+                uint32_t v[4];
 #pragma unroll
-                for (int p = 0; p < 4; ++p) w[p] = kHalf ? vraw[t][p] >> (i & 8) : vraw[t][p];
+                for (int p = 0; p < 4; ++p) v[p] = T::kHalf ? w.v[t][p] >> (i & 8) : w.v[t][p];
 #pragma unroll
                 for (int k = 0; k < CL; ++k) {
-                    uint32_t v[4];
+                    uint32_t x[4];
 #pragma unroll
-                    for (int p = 0; p < 4; ++p)
-                        v[p] = kv_code_pair(w[p] >> (k >= 2 ? 8 : 0), k & 1, (k & 1 ? z[p] << 4 : z[p]) | 0xE400E400u);
-                    const f16x8 f = kv_frag(v[0], v[1], v[2], v[3]);
+                    for (int p = 0; p < 4; ++p) x[p] = kv_code_pair(v[p] >> (k >= 2 ? 8 : 0), k & 1, k & 1 ? hi[p] : lo[p]);
+                    const f16x8 f = kv_frag(x[0], x[1], x[2], x[3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) o[t][k][n] = kv_mfma(f, pr[p][n], o[t][k][n]);
+                        for (int p = 0; p < PARTS; ++p) sums.o[t][k][n] = kv_mfma(f, pr[p][n], sums.o[t][k][n]);
                 }
             }
         }
+    };
+    while (r < r1) {
+        bool ok2 = false;
+        r += kKvWaves;
+        if (r < r1) ok2 = start(next);
+        r -= kKvWaves;
+        const uint8_t* at2 = rec;
+        if (ok) work(now, at);
+        r += kKvWaves;
+        if (r >= r1) break;
+        ok = false;
+        r += kKvWaves;
+        if (r < r1) ok = start(now);
+        r -= kKvWaves;
+        at = rec;
+        if (ok2) work(next, at2);
+        r += kKvWaves;
     }
+    sums.finish();
 
-    // ---- to plain sums relative to the maximum: o[t][k][n][e] is channel `channel(t, k, 4 j + e)`
+    // every wave to the common maximum (and shift), then sums over the waves
+    __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT];
+    __shared__ float acc[kKvWaves][16 * NT][DP + 1];
+    const float back = __builtin_amdgcn_exp2f(-sums.shift);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+        if (j == 0) {
+            wtop[wave][16 * n + i] = sums.top[n];
+            wmass[wave][16 * n + i] = sums.mass[n] * back;
+        }
+    __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        mass[n] = kv_sum4(mass[n]);
+        float m = wtop[0][16 * n + i];
 #pragma unroll
-        for (int t = 0; t < UT; ++t) {
-            const int g = (kHalf ? 32 * t : 64 * t) / GROUP;
-            const float f = 1.f / norm[g];
+        for (int w = 1; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][16 * n + i]);
+        const float f = m == sums.top[n] ? back : __builtin_amdgcn_exp2f(sums.top[n] - m) * back;
+#pragma unroll
+        for (int t = 0; t < UT; ++t)
 #pragma unroll
             for (int k = 0; k < CL; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[t][k][n][e] *= k & 1 ? 0.0625f * f : f;
+                for (int e = 0; e < 4; ++e) {
+                    const int d = T::channel(t, k, 4 * j + e);
+                    if (T::kWhole || d < DP) acc[wave][16 * n + i][d] = sums.o[t][k][n][e] * f;
+                }
+    }
+    __syncthreads();
+    for (int x = tid; x < 16 * NT * DP; x += 256) {
+        const int rr = x / DP, d = x - rr * DP, row = u.tile_row + rr;
+        if (row >= u.rows) break;
+        float m = -kKvInf, l = 0.f, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][rr]);
+#pragma unroll
+        for (int w = 0; w < kKvWaves; ++w) {
+            l += wtop[w][rr] == m ? wmass[w][rr] : wmass[w][rr] * __builtin_amdgcn_exp2f(wtop[w][rr] - m);
+            sum += acc[w][rr][d];
+        }
+        if (u.splits > 1) {
+            const int64_t slot = (unit * plan.nsplit + split) * plan.rows + rr;
+            plan.part[slot * DP + d] = sum;
+            if (d == 0) {
+                plan.stat[2 * slot] = m;
+                plan.stat[2 * slot + 1] = l;
+            }
+        } else {
+            const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
+            if (d < a.c.dim) kv_out(a, (u.first + qi) * a.ot + head * a.oh + d, l == 0.f ? 0.f : sum / l);
+            if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
         }
     }
+}
 
-    if constexpr (!ROWS) {
-        // join the waves: every wave to the common maximum, then sums over the waves through LDS
-        __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT];
-        __shared__ float acc[kKvWaves][16 * NT][DP + 1];
+// ---------------------------------------------------------------- many rows
+// Every wave has 16 NT rows of its own and the workgroup goes through the records together.  A record's
+// codes are turned into fp16 once, each wave a quarter of them, and reach the others through LDS as
+// the products' operands (1 KB each, in lane order); while record r is multiplied, r + 1 is
+// converted and r + 2 is on its way.
+template <int DP, int GROUP, int NT, int PARTS>
+__global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
+{
+    using R = KvRec<DP, GROUP>;
+    using T = KvTiles<DP, GROUP>;
+    constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
+    constexpr int CW = (NC + 1) / 2;                             // key products a wave converts
+    constexpr int VW = T::kHalf ? (UT + 1) / 2 : UT;             // value products
+    struct Stage {
+        f16x8 k[2][NC][64], v[UT][CL][64];
+        float ks[NG][kKvTok], vs[NG][kKvTok];
+        float top[NG];                                           // the largest of vs
+    };
+    __shared__ Stage stage[2];
+    // workgroups of an XCD (every eighth) get a contiguous stretch of units: rows of the same keys
+    // share its L2
+    const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t total = plan.units * plan.nsplit, q8 = total / 8, r8 = total % 8, x8 = wg & 7;
+    if (wg >= total) return;
+    const int64_t mine = x8 * q8 + (x8 < r8 ? x8 : r8) + (wg >> 3);
+    const int64_t unit = mine / plan.nsplit;
+    const int split = (int)(mine - unit * plan.nsplit);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int i = tid & 15, j = lane >> 4;
+    const KvUnit u = kv_unit(a, plan, unit, tid == 0 && split == 0);
+    if (split >= u.splits || u.tile_row >= u.rows) return;
+    const int count = u.rec1 - u.rec0;
+    const int r0 = u.rec0 + (int)((int64_t)count * split / u.splits), r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
+    const int row0 = u.tile_row + wave * (16 * NT);
+
+    const int64_t pages = a.c.slots / ((int64_t)a.c.per * kKvTok);
+    const int32_t* table = a.table + u.b * a.width;
+    const int per = (int)a.c.per;
+    int pg = r0 / per, rem = r0 - pg * per;
+    int id = r0 < r1 ? table[pg] : 0;
+
+    // what the wave converts of a record
+    const int kh = wave & 1, kc = (wave >> 1) * CW;              // half and first channel block of the keys
+    const int vk = T::kHalf ? wave & 1 : wave, vt = T::kHalf ? wave >> 1 : 0;   // class; first unit tile (every second)
+    uint32_t k[CW], kz[NG], v[VW][4], vw[NG][8], word[(NG + 3) / 4];
+    bool have = false;
+    auto start = [&](int r) {
+        have = id >= 0 && id < pages;
+        if (have) {
+            const uint8_t* rec = a.c.pages + (((int64_t)id * a.c.heads + u.kvh) * per + rem) * R::kBytes;
+            const int token = T::key_token(i, kh);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-            if (j == 0) {
-                wtop[wave][16 * n + i] = top[n];
-                wmass[wave][16 * n + i] = mass[n];
+            for (int x = 0; x < CW; ++x)
+                k[x] = *reinterpret_cast<const uint32_t*>(rec + token * R::kKeyRow + j * (4 * NC) + 4 * min(kc + x, NC - 1));
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                kz[g] = *reinterpret_cast<const uint32_t*>(rec + R::kKeyWords + g * (4 * kKvTok) + 4 * token);
+                kv_words<8>(rec + R::kValWords + g * (4 * kKvTok) + 32 * j, vw[g]);
             }
-        __syncthreads();
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float m = wtop[0][16 * n + i];
+            for (int x = 0; x < VW; ++x)
+                kv_words<4>(rec + R::kVal + T::unit(T::kHalf ? min(vt + 2 * x, UT - 1) : x, i) * (2 * kKvTok) + 16 * j, v[x]);
+            // a wave's lanes: 32 key words, 32 value words of a group
 #pragma unroll
-            for (int w = 1; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][16 * n + i]);
-            const float f = m == top[n] ? 1.f : __builtin_amdgcn_exp2f(top[n] - m);
-#pragma unroll
-            for (int t = 0; t < UT; ++t)
-#pragma unroll
-                for (int k = 0; k < CL; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int rho = 4 * j + e;
-                        const int d = kHalf ? 32 * t + 4 * (rho & 7) + k + 2 * (rho >> 3) : 64 * t + 4 * rho + k;
-                        if (DP % 64 == 0 || kHalf || d < DP) acc[wave][16 * n + i][d] = o[t][k][n][e] * f;
-                    }
+            for (int x = 0; x < (NG + 3) / 4; ++x)
+                word[x] = *reinterpret_cast<const uint32_t*>(rec + (lane < 32 ? R::kKeyWords : R::kValWords) + min(wave + 4 * x, NG - 1) * (4 * kKvTok) + 4 * (lane & 31));
+        } else if (tid == 0) {
+            set_status(a.status, QE_ERR_ARG);
         }
-        __syncthreads();
-        for (int at = tid; at < 16 * NT * DP; at += 256) {
-            const int rr = at / DP, d = at - rr * DP;
-            const int64_t row = row0 + rr;
-            if (row >= rows) break;
-            float m = -kKvInf, l = 0.f, x = 0.f;
+        if (++rem == per) {
+            rem = 0;
+            ++pg;
+        }
+        if (r + 1 < r1) id = table[pg];
+    };
+    auto convert = [&](Stage& st, int r) {
+        if (!have) return;
 #pragma unroll
-            for (int w = 0; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][rr]);
+        for (int x = 0; x < CW; ++x) {
+            if (kc + x >= NC) continue;
+            uint32_t lo, hi;
+            if constexpr (NG == 1) kv_key_zero(kz[0], lo, hi);
+            else {
+                uint32_t z = kz[0];
 #pragma unroll
-            for (int w = 0; w < kKvWaves; ++w) {
-                l += wtop[w][rr] == m ? wmass[w][rr] : wmass[w][rr] * __builtin_amdgcn_exp2f(wtop[w][rr] - m);
-                x += acc[w][rr][d];
+                for (int g = 1; g < NG; ++g) z = (kc + x) / T::CPG == g ? kz[g] : z;
+                kv_key_zero(z, lo, hi);
             }
-            if (u.splits > 1) {
-                const int64_t slot = (unit * plan.nsplit + split) * plan.rows + rr;
-                plan.part[slot * DP + d] = x;
-                if (d == 0) {
-                    plan.stat[2 * slot] = m;
-                    plan.stat[2 * slot + 1] = l;
+            st.k[kh][kc + x][lane] = kv_key_frag(k[x], lo, hi);
+        }
+#pragma unroll
+        for (int x = 0; x < VW; ++x) {
+            const int t = T::kHalf ? vt + 2 * x : x;
+            if (t >= UT) continue;
+            uint32_t f[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                uint32_t w0 = vw[0][2 * p], w1 = vw[0][2 * p + 1];
+#pragma unroll
+                for (int g = 1; g < NG; ++g) {
+                    w0 = T::group_of(t) == g ? vw[g][2 * p] : w0;
+                    w1 = T::group_of(t) == g ? vw[g][2 * p + 1] : w1;
                 }
-            } else {
-                const int64_t qi = row / per;
-                const int head = kvh * per + (int)(row - qi * per);
-                if (d < a.c.dim) kv_out(a, (u.first + qi) * a.ot + head * a.oh + d, l == 0.f ? 0.f : x / l);
-                if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = l == 0.f ? -kKvInf : (m + __builtin_amdgcn_logf(l)) / kLog2e;
+                uint32_t lo, hi;
+                kv_value_zero(w0, w1, lo, hi);
+                const uint32_t w = T::kHalf ? v[x][p] >> (i & 8) : v[x][p] >> (vk & 2 ? 8 : 0);
+                f[p] = vk & 1 ? kv_code_pair(w, true, hi) : kv_code_pair(w, false, lo);
+            }
+            st.v[t][vk][lane] = kv_frag(f[0], f[1], f[2], f[3]);
+        }
+#pragma unroll
+        for (int x = 0; x < (NG + 3) / 4; ++x) {
+            const int g = wave + 4 * x;
+            if (g >= NG) continue;
+            float s = kv_scale(word[x]);
+            // (words past the sequence's end are anything: no scale of theirs may meet a 0)
+            if (lane >= 32 && r * kKvTok + (lane - 32) >= u.len) s = 0.f;
+            float m = lane < 32 ? 0.f : s;
+#pragma unroll
+            for (int y = 1; y < 32; y *= 2) m = fmaxf(m, __shfl_xor(m, y));
+            if (lane < 32) st.ks[g][lane] = s;
+            else st.vs[g][lane - 32] = s;
+            if (lane == 32) st.top[g] = m;
+        }
+    };
+
+    bool ok = false;
+    if (r0 < r1) {
+        start(r0);
+        convert(stage[0], r0);
+        ok = have;
+    }
+    KvRows<NC, NT, PARTS> rows;
+    rows.load(a, u, min(row0, u.rows - 1));
+    const bool idle = row0 >= u.rows;
+    KvSums<UT, CL, NT> sums;
+    sums.clear();
+    if (r0 + 1 < r1) start(r0 + 1);
+    __syncthreads();
+    for (int r = r0; r < r1; ++r) {
+        bool ok2 = false;
+        if (r + 1 < r1) {
+            convert(stage[r + 1 - r0 & 1], r + 1);
+            ok2 = have;
+            if (r + 2 < r1) start(r + 2);
+        }
+        const int t0 = r * kKvTok;
+        if (ok && !idle && t0 < rows.any_hi && t0 + kKvTok > rows.any_lo) {
+            const Stage& st = stage[r - r0 & 1];
+            const bool masked = rows.masked(t0);
+            float s[NT][8];
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                f32x4 acc[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = g * T::CPG; k < (g + 1) * T::CPG && k < NC; ++k)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f16x8 f = st.k[h][k][lane];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][k], acc[n][h]);
+                    }
+                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j + 4]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
+                        s[n][e] = g == 0 ? sc * x : fmaf(sc, x, s[n][e]);
+                    }
+            }
+            float big = st.top[0];
+#pragma unroll
+            for (int g = 1; g < NG; ++g) big = fmaxf(big, st.top[g]);
+            sums.fit(big);
+            sums.weigh(s, rows, a.slopes != nullptr, t0, masked);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j + 4]);
+                float sv[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sv[e] = e < 4 ? s0[e] : s1[e - 4];
+                f16x8 pr[PARTS][NT];
+                sums.template weights<PARTS>(s, sv, masked, pr);
+#pragma unroll
+                for (int t = 0; t < UT; ++t) {
+                    if (T::group_of(t) != g) continue;
+#pragma unroll
+                    for (int k = 0; k < CL; ++k) {
+                        const f16x8 f = st.v[t][k][lane];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int p = 0; p < PARTS; ++p) sums.o[t][k][n] = kv_mfma(f, pr[p][n], sums.o[t][k][n]);
+                    }
+                }
             }
         }
-    } else {
+        ok = ok2;
+        __syncthreads();
+    }
+    if (idle) return;
+    sums.finish();
+    const float back = __builtin_amdgcn_exp2f(-sums.shift);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int64_t row = row0 + 16 * n + i;
-            if (row >= rows) continue;
-            const int64_t qi = row / per;
-            const int head = kvh * per + (int)(row - qi * per);
-            const int64_t slot = (unit * plan.nsplit + split) * plan.rows + (row - tile * plan.rows);
-            const float inv = mass[n] == 0.f ? 0.f : 1.f / mass[n];
+    for (int n = 0; n < NT; ++n) {
+        const int row = row0 + 16 * n + i;
+        if (row >= u.rows) continue;
+        const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
+        const int64_t slot = (unit * plan.nsplit + split) * plan.rows + (row - u.tile_row);
+        const float f = u.splits > 1 ? back : sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n];
 #pragma unroll
-            for (int t = 0; t < UT; ++t)
+        for (int t = 0; t < UT; ++t)
 #pragma unroll
-                for (int k = 0; k < CL; ++k)
+            for (int k = 0; k < CL; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int rho = 4 * j + e;
-                        const int d = kHalf ? 32 * t + 4 * (rho & 7) + k + 2 * (rho >> 3) : 64 * t + 4 * rho + k;
-                        if (u.splits > 1) {
-                            if (DP % 64 == 0 || kHalf || d < DP) plan.part[slot * DP + d] = o[t][k][n][e];
-                        } else if (d < a.c.dim)
-                            kv_out(a, (u.first + qi) * a.ot + head * a.oh + d, mass[n] == 0.f ? 0.f : o[t][k][n][e] * inv);
-                    }
-            if (j == 0) {
-                if (u.splits > 1) {
-                    plan.stat[2 * slot] = top[n];
-                    plan.stat[2 * slot + 1] = mass[n];
-                } else if (a.lse)
-                    a.lse[(u.first + qi) * a.heads + head] = mass[n] == 0.f ? -kKvInf : (top[n] + __builtin_amdgcn_logf(mass[n])) / kLog2e;
-            }
+                for (int e = 0; e < 4; ++e) {
+                    const int d = T::channel(t, k, 4 * j + e);
+                    if (u.splits > 1) {
+                        if (T::kWhole || d < DP) plan.part[slot * DP + d] = sums.o[t][k][n][e] * f;
+                    } else if (d < a.c.dim)
+                        kv_out(a, (u.first + qi) * a.ot + head * a.oh + d, sums.mass[n] == 0.f ? 0.f : sums.o[t][k][n][e] * f);
+                }
+        if (j == 0) {
+            if (u.splits > 1) {
+                plan.stat[2 * slot] = sums.top[n];
+                plan.stat[2 * slot + 1] = sums.mass[n] * back;
+            } else if (a.lse)
+                a.lse[(u.first + qi) * a.heads + head] = kv_lse(sums.top[n] - sums.shift, sums.mass[n]);
         }
     }
 }
@@ -571,64 +873,57 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a
 {
     const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
-    const int64_t unit = at / plan.rows, rr = at - unit * plan.rows, bh = unit / plan.row_tiles, tile = unit - bh * plan.row_tiles;
-    const int64_t b = bh / a.c.heads;
-    if (b >= a.batch) return;
-    const int kvh = (int)(bh - b * a.c.heads), per = a.heads / a.c.heads;
-    const KvUnit u = kv_unit(a, plan, b, tile, false);
-    const int64_t row = tile * plan.rows + rr;
-    if (u.splits <= 1 || row >= (int64_t)u.nq * per) return;
+    const int64_t unit = at / plan.rows;
+    const int rr = (int)(at - unit * plan.rows);
+    if (unit >= plan.units) return;
+    const KvUnit u = kv_unit(a, plan, unit, false);
+    const int row = u.tile_row + rr;
+    if (u.splits <= 1 || row >= u.rows) return;
     const int64_t slot = unit * plan.nsplit * plan.rows + rr;
     float m = -kKvInf;
     for (int s = lane; s < u.splits; s += 64) m = fmaxf(m, plan.stat[2 * (slot + (int64_t)s * plan.rows)]);
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-    float l = 0.f, x[DP / 64 + (DP % 64 != 0)] = {};
+    constexpr int C = (DP + 63) / 64;
+    float l = 0.f, x[C] = {};
     for (int s = 0; s < u.splits; ++s) {
         const int64_t k = slot + (int64_t)s * plan.rows;
         const float t = plan.stat[2 * k], f = t == m ? 1.f : __builtin_amdgcn_exp2f(t - m);
         l = fmaf(plan.stat[2 * k + 1], f, l);
 #pragma unroll
-        for (int c = 0; c < (DP + 63) / 64; ++c)
+        for (int c = 0; c < C; ++c)
             if (DP % 64 == 0 || 64 * c + lane < DP) x[c] = fmaf(plan.part[k * DP + 64 * c + lane], f, x[c]);
     }
-    const int64_t qi = row / per;
-    const int head = kvh * per + (int)(row - qi * per);
+    const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
 #pragma unroll
-    for (int c = 0; c < (DP + 63) / 64; ++c)
+    for (int c = 0; c < C; ++c)
         if (64 * c + lane < a.c.dim) kv_out(a, (u.first + qi) * a.ot + head * a.oh + 64 * c + lane, l == 0.f ? 0.f : x[c] / l);
-    if (a.lse && lane == 0) a.lse[(u.first + qi) * a.heads + head] = l == 0.f ? -kKvInf : (m + __builtin_amdgcn_logf(l)) / kLog2e;
+    if (a.lse && lane == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
 }
 
-// The form of a call: rows of a wave in tiles of 16, and whether waves have rows of their own.
-struct KvForm { int nt; bool rows; };
+// The form of a call: many rows or few, and a wave's tiles of 16 rows.
+struct KvForm { bool many; int nt; };
 
-template <int DP, int GROUP, int NT, int PARTS, bool ROWS>
-void kv_attn_start(const KvAttn& a, const KvPlan& plan, dim3 grid, hipStream_t s)
-{
-    hipLaunchKernelGGL((kv_attn_kernel<DP, GROUP, NT, PARTS, ROWS>), grid, dim3(256), 0, s, a, plan);
-}
-
-// Query tiles of a wave in the ROWS form: what the registers hold.
-template <int DP, int PARTS> constexpr int kRowsNT = DP <= 128 ? (PARTS == 1 ? 2 : 1) : 1;
+// Tiles of a wave with many rows: what the registers hold.
+constexpr int kv_many_nt(int dp, bool f32) { return dp <= 128 && !f32 ? 2 : 1; }
 
 template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm form, dim3 grid, hipStream_t s)
 {
     kv_dispatch_group<DP>(a.group, [&](auto shape) {
         constexpr int G = decltype(shape)::GROUP;
         if (a.dtype == QE_F32) {
-            if (form.rows) kv_attn_start<DP, G, kRowsNT<DP, 2>, 2, true>(a, plan, grid, s);
-            else kv_attn_start<DP, G, 1, 2, false>(a, plan, grid, s);
+            if (form.many) hipLaunchKernelGGL((kv_many_kernel<DP, G, kv_many_nt(DP, true), 2>), grid, dim3(256), 0, s, a, plan);
+            else hipLaunchKernelGGL((kv_few_kernel<DP, G, 1, 2>), grid, dim3(256), 0, s, a, plan);
+        } else if (form.many) {
+            hipLaunchKernelGGL((kv_many_kernel<DP, G, kv_many_nt(DP, false), 1>), grid, dim3(256), 0, s, a, plan);
+        } else if (DP > 128 || form.nt == 1) {
+            hipLaunchKernelGGL((kv_few_kernel<DP, G, 1, 1>), grid, dim3(256), 0, s, a, plan);
         } else {
-            if (form.rows) kv_attn_start<DP, G, kRowsNT<DP, 1>, 1, true>(a, plan, grid, s);
-            else if (form.nt == 1) kv_attn_start<DP, G, 1, 1, false>(a, plan, grid, s);
-            else kv_attn_start<DP, G, 2, 1, false>(a, plan, grid, s);
+            hipLaunchKernelGGL((kv_few_kernel<DP, G, DP <= 128 ? 2 : 1, 1>), grid, dim3(256), 0, s, a, plan);
         }
     });
-    if (plan.nsplit > 1) {
-        const int64_t rows = (int64_t)a.batch * a.c.heads * plan.row_tiles * plan.rows;
-        hipLaunchKernelGGL(kv_join_kernel<DP>, grid_xy(cdiv(rows, 4), 256), dim3(256), 0, s, a, plan);
-    }
+    if (plan.nsplit > 1)
+        hipLaunchKernelGGL(kv_join_kernel<DP>, grid_xy(cdiv(plan.units * plan.rows, 4), 256), dim3(256), 0, s, a, plan);
 }
 
 }  // namespace qe

@@ -11,13 +11,13 @@ extern template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, di
 
 namespace {
 
-constexpr int kRowsFrom = 128;      // query rows of a sequence and key head from which waves have rows of their own
+constexpr int64_t kManyFrom = 128;  // query rows of a sequence and key head from which waves have rows of their own
 constexpr int64_t kFill = 1024;     // workgroups that fill the chip
 
 KvForm form_of(int64_t rows, int dp, bool f32)
 {
-    if (rows >= kRowsFrom) return {dp <= 128 && !f32 ? 2 : 1, true};
-    return {rows <= 16 || f32 ? 1 : 2, false};
+    if (rows >= kManyFrom) return {true, kv_many_nt(dp, f32)};
+    return {false, rows <= 16 || f32 || dp > 128 ? 1 : 2};
 }
 
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
@@ -37,7 +37,7 @@ Sizes sizes_of(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, b
     Sizes z;
     const int64_t rows = max_q * (heads / kv_heads);
     z.form = form_of(rows, kv_dp(dim), f32);
-    z.rows = 16 * z.form.nt * (z.form.rows ? kKvWaves : 1);
+    z.rows = 16 * z.form.nt * (z.form.many ? kKvWaves : 1);
     z.row_tiles = cdiv(rows, z.rows);
     z.units = batch * kv_heads * z.row_tiles;
     return z;
@@ -69,6 +69,7 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     const Sizes z = sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.dtype == QE_F32);
     KvPlan plan{};
     plan.row_tiles = z.row_tiles;
+    plan.units = z.units;
     plan.rows = z.rows;
     int64_t records = a.width * a.c.per;
     if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
