@@ -98,11 +98,21 @@ __device__ inline void kv_out(const KvAttn& a, int64_t at, float x)
     else static_cast<__bf16*>(a.out)[at] = (__bf16)x;
 }
 
-// A pair of codes of a word (nibbles k and k + 4 of w >> 4 k') less their zero points: `high`: the
-// codes in bits 4-7, times 16.  minus: a pair of -(1024 + z), or of -(1024 + 16 z).
-__device__ inline uint32_t kv_code_pair(uint32_t w, bool high, uint32_t minus)
+// Constants in registers: an instruction takes no two literals, and "and, or" is one instruction
+// with both of them in registers.
+struct KvBits {
+    uint32_t low = 0x000F000Fu, high = 0x00F000F0u, n = 0x64006400u, z = 0xE400E400u;
+    __device__ KvBits()
+    {
+        asm("" : "+s"(low), "+s"(high));
+        asm("" : "+v"(n), "+v"(z));
+    }
+};
+// A pair of codes of a word (nibbles k and k + 4 of w >> 4 k') less their zero points: mask: low, or
+// high for the codes in bits 4-7, times 16.  minus: a pair of -(1024 + z), or of -(1024 + 16 z).
+__device__ inline uint32_t kv_code_pair(uint32_t w, uint32_t mask, uint32_t minus, const KvBits& bits)
 {
-    const uint32_t n = (w & (high ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;
+    const uint32_t n = (w & mask) | bits.n;
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, n) + __builtin_bit_cast(f16x2, minus));
 }
 
@@ -176,24 +186,29 @@ template <int DP, int GROUP> struct KvTiles {
     static constexpr bool kWhole = DP % 64 == 0 || kHalf;        // every channel() is below DP
 };
 
-// The zero points of a key row as the pairs kv_code_pair takes.
-__device__ inline void kv_key_zero(uint32_t word, uint32_t& lo, uint32_t& hi)
+// The zero points of a key row as the pairs kv_code_pair takes, and of two tokens' value words.
+__device__ inline void kv_key_zero(uint32_t word, uint32_t& lo, uint32_t& hi, const KvBits& bits)
 {
     const uint32_t z = word & 15u, z2 = z << 16 | z;
-    lo = z2 | 0xE400E400u;
-    hi = z2 << 4 | 0xE400E400u;
+    lo = z2 | bits.z;
+    hi = z2 << 4 | bits.z;
 }
-// Of two tokens' value words.
-__device__ inline void kv_value_zero(uint32_t w0, uint32_t w1, uint32_t& lo, uint32_t& hi)
+__device__ inline void kv_value_zero(uint32_t w0, uint32_t w1, uint32_t& lo, uint32_t& hi, const KvBits& bits)
 {
-    const uint32_t z2 = __builtin_amdgcn_perm(w1, w0, 0x05040100u) & 0x000F000Fu;
-    lo = z2 | 0xE400E400u;
-    hi = z2 << 4 | 0xE400E400u;
+    const uint32_t w = __builtin_amdgcn_perm(w1, w0, 0x05040100u);
+    lo = (w & bits.low) | bits.z;
+    hi = ((w << 4) & bits.high) | bits.z;
 }
-__device__ inline f16x8 kv_key_frag(uint32_t w, uint32_t lo, uint32_t hi)
+__device__ inline f16x8 kv_key_frag(uint32_t w, uint32_t lo, uint32_t hi, const KvBits& bits)
 {
     const uint32_t w8 = w >> 8;
-    return kv_frag(kv_code_pair(w, false, lo), kv_code_pair(w, true, hi), kv_code_pair(w8, false, lo), kv_code_pair(w8, true, hi));
+    return kv_frag(kv_code_pair(w, bits.low, lo, bits), kv_code_pair(w, bits.high, hi, bits),
+                   kv_code_pair(w8, bits.low, lo, bits), kv_code_pair(w8, bits.high, hi, bits));
+}
+// The largest; NaNs are passed over.
+__device__ inline float kv_max8(const float (&x)[8])
+{
+    return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), x[3]), x[4]), x[5]), x[6]), x[7]);
 }
 
 // A wave's query rows, 16 a tile, and what they see.
@@ -226,7 +241,7 @@ template <int NC, int NT, int PARTS> struct KvRows {
             // (a row of zeros, NaN or infinities keeps its values)
             const int e2 = top > 0.f && top <= 3.402823466e38f ? max(-100, min(100, 141 - (int)(__float_as_uint(top) >> 23))) : 0;
             const float mul = __uint_as_float((uint32_t)(127 + e2) << 23) * (a.scale < 0.f ? -1.f : 1.f);
-            c[n] = fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e2) << 23);
+            c[n] = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e2) << 23), 1e-37f);   // (0 times -inf)
             slope[n] = a.slopes && have ? a.slopes[head] * kLog2e : 0.f;
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
@@ -285,83 +300,70 @@ template <int UT, int CL, int NT> struct KvSums {
         shift = 0.f;
         limit = 0.f;
     }
-    __device__ void scale_row(int n, float f)
+    // Moves the maxima and the shift, and the sums with them, where a row's maximum (at: a lane's) or a
+    // value scale (big: a lane's largest) is out of range.
+    __device__ void move(const float (&at)[NT], float big)
     {
-        mass[n] *= f;
+        bool out = big > limit;
 #pragma unroll
-        for (int t = 0; t < UT; ++t)
-#pragma unroll
-            for (int k = 0; k < CL; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
-    }
-    // big: a lane's largest value scale
-    __device__ void fit(float big)
-    {
-        if (!__any(big > limit)) return;
-        big = kv_max4(big);
-        const uint32_t ex = max(__builtin_amdgcn_readfirstlane(__float_as_uint(big)) >> 23, 77u);   // (shift at most 60)
-        const float to = (float)(137 - (int)ex), f = limit == 0.f ? 1.f : __builtin_amdgcn_exp2f(to - shift);
-        limit = __uint_as_float(ex << 23 | 0x7fffffu);
+        for (int n = 0; n < NT; ++n) out = out || at[n] > top[n] + 4.f;
+        if (!__any(out)) return;
+        big = fmaxf(kv_max4(big), limit);
+        const int e = __builtin_amdgcn_readfirstlane(__float_as_int(big)) >> 23, ex = e < 77 ? 77 : e;   // (shift at most 60)
+        const float to = (float)(137 - ex), g = limit == 0.f ? 1.f : __builtin_amdgcn_exp2f(to - shift);
+        limit = __int_as_float(ex << 23 | 0x7fffff);
         shift = to;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) scale_row(n, f);
+        for (int n = 0; n < NT; ++n) {
+            const float m = kv_max4(fmaxf(top[n], at[n]));
+            const float f = m == top[n] ? g : g * __builtin_amdgcn_exp2f(top[n] - m);
+            top[n] = m;
+            mass[n] *= f;
+#pragma unroll
+            for (int t = 0; t < UT; ++t)
+#pragma unroll
+                for (int k = 0; k < CL; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
+        }
     }
-    // s: the products times their key scales; on return p 2^shift (0 where the row sees nothing)
-    template <int NC, int PARTS> __device__ void weigh(float (&s)[NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, int t0, bool masked)
+    // s: the products times their key scales; on return p 2^shift (0 where the row sees nothing).
+    // masked: some row does not see the whole record.  big: the lane's largest value scale.
+    template <int NC, int PARTS>
+    __device__ void weigh(float (&s)[NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, int t0, bool masked, float big)
     {
-        const int t = t0 + 8 * ((threadIdx.x & 63) >> 4);
-        float c[NT], big[NT];
-        uint32_t vis[NT];
-        bool move = false;
+        float at[NT], c[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             c[n] = r.c[n];
-            if (slopes) {
-                const float base = r.slope[n] * (float)(t - (r.hi[n] - 1));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[n][e] = fmaf(s[n][e], c[n], fmaf(r.slope[n], (float)e, base));
-                c[n] = 1.f;
-            }
-            vis[n] = 0xffu;
-            if (masked) {
-                big[n] = -kKvInf;
-                vis[n] = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool see = t + e >= r.lo[n] && t + e < r.hi[n];
-                    vis[n] |= (see ? 1u : 0u) << e;
-                    big[n] = see ? fmaxf(big[n], s[n][e]) : big[n];
-                }
-            } else {
-                big[n] = fmaxf(fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])), fmaxf(fmaxf(s[n][4], s[n][5]), fmaxf(s[n][6], s[n][7])));
-            }
-            big[n] *= c[n];
-            move = move || big[n] > top[n] + 4.f;
+            at[n] = c[n] * kv_max8(s[n]);
         }
-        if (__any(move)) {
+        if (masked || slopes) {
+            const int t = t0 + 8 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float m = kv_max4(fmaxf(top[n], big[n]));
-                const float f = m == top[n] ? 1.f : __builtin_amdgcn_exp2f(top[n] - m);
-                top[n] = m;
-                scale_row(n, f);
+                const float base = r.slope[n] * (float)(t - (r.hi[n] - 1));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[n][e] = fmaf(s[n][e], c[n], fmaf(r.slope[n], (float)e, base));
+                    s[n][e] = t + e >= r.lo[n] && t + e < r.hi[n] ? s[n][e] : -kKvInf;
+                }
+                c[n] = 1.f;
+                at[n] = kv_max8(s[n]);
             }
         }
+        move(at, big);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float off = shift - top[n];
+            const float off = top[n] == -kKvInf ? 0.f : shift - top[n];     // (nothing seen so far: every s is -inf)
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c[n], off));
-            if (masked) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[n][e] = vis[n] >> e & 1u ? s[n][e] : 0.f;
-            }
             mass[n] += ((s[n][0] + s[n][1]) + (s[n][2] + s[n][3])) + ((s[n][4] + s[n][5]) + (s[n][6] + s[n][7]));
         }
     }
-    // the products' fp16 weights p s' of a group
-    template <int PARTS> __device__ static void weights(const float (&s)[NT][8], const float (&sv)[8], bool masked, f16x8 (&pr)[PARTS][NT])
+    // The products' fp16 weights p s' of a group.  unseen: a token that some row does not see may have
+    // a NaN scale, and 0 is to stay 0.
+    template <int PARTS> __device__ static void weights(const float (&s)[NT][8], const float (&sv)[8], bool unseen, f16x8 (&pr)[PARTS][NT])
     {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -369,7 +371,7 @@ template <int UT, int CL, int NT> struct KvSums {
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
-                if (masked) {                            // (a NaN scale of a token that the row does not see)
+                if (unseen) {
                     x0 = s[n][2 * p] == 0.f ? 0.f : x0;
                     x1 = s[n][2 * p + 1] == 0.f ? 0.f : x1;
                 }
@@ -382,6 +384,26 @@ template <int UT, int CL, int NT> struct KvSums {
             pr[0][n] = kv_frag(h[0], h[1], h[2], h[3]);
             if constexpr (PARTS == 2) pr[1][n] = kv_frag(m[0], m[1], m[2], m[3]);
         }
+    }
+    // Whether a scale of the lane's tokens is a NaN.
+    template <int NG> __device__ static bool has_nan(const float (&sv)[NG][8])
+    {
+        float x = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x += sv[g][e];
+        return __any(x != x);
+    }
+    // Keeps every sum in one place from record to record (the compiler copied half of them otherwise).
+    __device__ void pin()
+    {
+#pragma unroll
+        for (int t = 0; t < UT; ++t)
+#pragma unroll
+            for (int k = 0; k < CL; ++k)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) asm("" : "+v"(o[t][k][n]));
     }
     // after the last record: plain sums (odd classes were 16 times as large), the rows' masses.  What is
     // left of shift is a factor of both.
@@ -423,6 +445,7 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
     const int r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
     int r = u.rec0 + (int)((int64_t)count * split / u.splits) + wave;
 
+    const KvBits bits;
     struct Raw {
         uint32_t k[2][NC], v[UT][4], kw[NG][8], vw[NG][8], kz[2][NG];
     };
@@ -435,25 +458,26 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
     const uint8_t* rec = nullptr;                                // of the record loaded last
     auto codes = [&](Raw& w) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) kv_words<NC>(rec + T::key_token(i, h) * R::kKeyRow + j * (4 * NC), w.k[h]);
+        for (int h = 0; h < 2; ++h) kv_words<NC>(rec + (uint32_t)(T::key_token(i, h) * R::kKeyRow + j * (4 * NC)), w.k[h]);
 #pragma unroll
-        for (int t = 0; t < UT; ++t) kv_words<4>(rec + R::kVal + T::unit(t, i) * (2 * kKvTok) + 16 * j, w.v[t]);
+        for (int t = 0; t < UT; ++t) kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(t, i) * (2 * kKvTok) + 16 * j), w.v[t]);
     };
     auto words = [&](const uint8_t* at, Raw& w) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const uint8_t* kp = at + R::kKeyWords + g * (4 * kKvTok);
-            kv_words<8>(kp + 32 * j, w.kw[g]);
+            const uint32_t kp = R::kKeyWords + g * (4 * kKvTok);
+            kv_words<8>(at + (kp + 32 * j), w.kw[g]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) w.kz[h][g] = *reinterpret_cast<const uint32_t*>(kp + 4 * T::key_token(i, h));
-            kv_words<8>(at + R::kValWords + g * (4 * kKvTok) + 32 * j, w.vw[g]);
+            for (int h = 0; h < 2; ++h) w.kz[h][g] = *reinterpret_cast<const uint32_t*>(at + (kp + 4 * T::key_token(i, h)));
+            kv_words<8>(at + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), w.vw[g]);
         }
     };
     // Starts the loads of record r (its page number was read before); false where there is no such page.
     auto start = [&](Raw& w) {
-        const bool ok = id >= 0 && id < pages;
+        const int page = __builtin_amdgcn_readfirstlane(id);
+        const bool ok = page >= 0 && page < pages;
         if (ok) {
-            rec = a.c.pages + (((int64_t)id * a.c.heads + u.kvh) * per + rem) * R::kBytes;
+            rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
             codes(w);
             if (kAll) words(rec, w);
         } else if (r < r1) {
@@ -464,7 +488,7 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
             rem -= per;
             ++pg;
         }
-        if (r + kKvWaves < r1) id = table[pg];
+        if (r + kKvWaves < r1) id = table[pg];            // (in a vector register until it is needed: a wait for it now would be one for all loads)
         return ok;
     };
 
@@ -479,8 +503,8 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
 
     auto work = [&](Raw& w, const uint8_t* base) {
         const int t0 = r * kKvTok;
-        if (!kAll) words(base, w);
         const bool masked = rows.masked(t0);
+        if (!kAll) words(base, w);
         float s[NT][8];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -492,10 +516,10 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t lo, hi;
-                kv_key_zero(w.kz[h][g], lo, hi);
+                kv_key_zero(w.kz[h][g], lo, hi, bits);
 #pragma unroll
                 for (int k = g * T::CPG; k < (g + 1) * T::CPG && k < NC; ++k) {
-                    const f16x8 f = kv_key_frag(w.k[h][k], lo, hi);
+                    const f16x8 f = kv_key_frag(w.k[h][k], lo, hi, bits);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -519,23 +543,23 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
 #pragma unroll
                 for (int g = 0; g < NG; ++g) w.vw[g][e] = t0 + 8 * j + e < u.len ? w.vw[g][e] : 0u;
         }
-        float big = 0.f;
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) big = fmaxf(big, kv_scale(w.vw[g][e]));
-        sums.fit(big);
-        sums.weigh(s, rows, a.slopes != nullptr, t0, masked);
+        float sv[NG][8], big = 0.f;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            float sv[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sv[e] = kv_scale(w.vw[g][e]);
+            for (int e = 0; e < 8; ++e) sv[g][e] = kv_scale(w.vw[g][e]);
+            big = fmaxf(big, kv_max8(sv[g]));
+        }
+        sums.weigh(s, rows, a.slopes != nullptr, t0, masked, big);
+        const bool unseen = masked && sums.has_nan(sv);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
             f16x8 pr[PARTS][NT];
-            sums.template weights<PARTS>(s, sv, masked, pr);
+            if (unseen) sums.template weights<PARTS>(s, sv[g], true, pr);
+            else sums.template weights<PARTS>(s, sv[g], false, pr);
             uint32_t lo[4], hi[4];
 #pragma unroll
-            for (int p = 0; p < 4; ++p) kv_value_zero(w.vw[g][2 * p], w.vw[g][2 * p + 1], lo[p], hi[p]);
+            for (int p = 0; p < 4; ++p) kv_value_zero(w.vw[g][2 * p], w.vw[g][2 * p + 1], lo[p], hi[p], bits);
 #pragma unroll
             for (int t = 0; t < UT; ++t) {
                 if (T::group_of(t) != g) continue;
@@ -546,7 +570,7 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
                 for (int k = 0; k < CL; ++k) {
                     uint32_t x[4];
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) x[p] = kv_code_pair(v[p] >> (k >= 2 ? 8 : 0), k & 1, k & 1 ? hi[p] : lo[p]);
+                    for (int p = 0; p < 4; ++p) x[p] = kv_code_pair(v[p] >> (k >= 2 ? 8 : 0), k & 1 ? bits.high : bits.low, k & 1 ? hi[p] : lo[p], bits);
                     const f16x8 f = kv_frag(x[0], x[1], x[2], x[3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
@@ -563,6 +587,7 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
         r -= kKvWaves;
         const uint8_t* at2 = rec;
         if (ok) work(now, at);
+        sums.pin();
         r += kKvWaves;
         if (r >= r1) break;
         ok = false;
@@ -571,6 +596,7 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
         r -= kKvWaves;
         at = rec;
         if (ok2) work(next, at2);
+        sums.pin();
         r += kKvWaves;
     }
     sums.finish();
@@ -645,7 +671,6 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     struct Stage {
         f16x8 k[2][NC][64], v[UT][CL][64];
         float ks[NG][kKvTok], vs[NG][kKvTok];
-        float top[NG];                                           // the largest of vs
     };
     __shared__ Stage stage[2];
     // workgroups of an XCD (every eighth) get a contiguous stretch of units: rows of the same keys
@@ -673,28 +698,31 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     // what the wave converts of a record
     const int kh = wave & 1, kc = (wave >> 1) * CW;              // half and first channel block of the keys
     const int vk = T::kHalf ? wave & 1 : wave, vt = T::kHalf ? wave >> 1 : 0;   // class; first unit tile (every second)
+    const KvBits bits;
+    const uint32_t vmask = vk & 1 ? bits.high : bits.low, vshift = vk & 1 ? 4 : 0;
     uint32_t k[CW], kz[NG], v[VW][4], vw[NG][8], word[(NG + 3) / 4];
     bool have = false;
     auto start = [&](int r) {
-        have = id >= 0 && id < pages;
+        const int page = __builtin_amdgcn_readfirstlane(id);
+        have = page >= 0 && page < pages;
         if (have) {
-            const uint8_t* rec = a.c.pages + (((int64_t)id * a.c.heads + u.kvh) * per + rem) * R::kBytes;
+            const uint8_t* rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
             const int token = T::key_token(i, kh);
 #pragma unroll
             for (int x = 0; x < CW; ++x)
-                k[x] = *reinterpret_cast<const uint32_t*>(rec + token * R::kKeyRow + j * (4 * NC) + 4 * min(kc + x, NC - 1));
+                k[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(token * R::kKeyRow + j * (4 * NC)) + 4 * (NC % 2 != 0 ? min(kc + x, NC - 1) : kc + x));
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                kz[g] = *reinterpret_cast<const uint32_t*>(rec + R::kKeyWords + g * (4 * kKvTok) + 4 * token);
-                kv_words<8>(rec + R::kValWords + g * (4 * kKvTok) + 32 * j, vw[g]);
+                kz[g] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(R::kKeyWords + g * (4 * kKvTok) + 4 * token));
+                kv_words<8>(rec + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), vw[g]);
             }
 #pragma unroll
             for (int x = 0; x < VW; ++x)
-                kv_words<4>(rec + R::kVal + T::unit(T::kHalf ? min(vt + 2 * x, UT - 1) : x, i) * (2 * kKvTok) + 16 * j, v[x]);
+                kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(T::kHalf ? min(vt + 2 * x, UT - 1) : x, i) * (2 * kKvTok) + 16 * j), v[x]);
             // a wave's lanes: 32 key words, 32 value words of a group
 #pragma unroll
             for (int x = 0; x < (NG + 3) / 4; ++x)
-                word[x] = *reinterpret_cast<const uint32_t*>(rec + (lane < 32 ? R::kKeyWords : R::kValWords) + min(wave + 4 * x, NG - 1) * (4 * kKvTok) + 4 * (lane & 31));
+                word[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)((lane < 32 ? R::kKeyWords : R::kValWords) + min(wave + 4 * x, NG - 1) * (4 * kKvTok) + 4 * (lane & 31)));
         } else if (tid == 0) {
             set_status(a.status, QE_ERR_ARG);
         }
@@ -702,27 +730,27 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             rem = 0;
             ++pg;
         }
-        if (r + 1 < r1) id = table[pg];
+        if (r + 1 < r1) id = table[pg];          // (in a vector register until it is needed: a wait for it now would be one for all loads)
     };
     auto convert = [&](Stage& st, int r) {
         if (!have) return;
 #pragma unroll
         for (int x = 0; x < CW; ++x) {
-            if (kc + x >= NC) continue;
+            if (NC % 2 != 0 && kc + x >= NC) continue;
             uint32_t lo, hi;
-            if constexpr (NG == 1) kv_key_zero(kz[0], lo, hi);
+            if constexpr (NG == 1) kv_key_zero(kz[0], lo, hi, bits);
             else {
                 uint32_t z = kz[0];
 #pragma unroll
                 for (int g = 1; g < NG; ++g) z = (kc + x) / T::CPG == g ? kz[g] : z;
-                kv_key_zero(z, lo, hi);
+                kv_key_zero(z, lo, hi, bits);
             }
-            st.k[kh][kc + x][lane] = kv_key_frag(k[x], lo, hi);
+            st.k[kh][kc + x][lane] = kv_key_frag(k[x], lo, hi, bits);
         }
 #pragma unroll
         for (int x = 0; x < VW; ++x) {
             const int t = T::kHalf ? vt + 2 * x : x;
-            if (t >= UT) continue;
+            if (T::kHalf && UT % 2 != 0 && t >= UT) continue;
             uint32_t f[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
@@ -732,10 +760,8 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
                     w0 = T::group_of(t) == g ? vw[g][2 * p] : w0;
                     w1 = T::group_of(t) == g ? vw[g][2 * p + 1] : w1;
                 }
-                uint32_t lo, hi;
-                kv_value_zero(w0, w1, lo, hi);
-                const uint32_t w = T::kHalf ? v[x][p] >> (i & 8) : v[x][p] >> (vk & 2 ? 8 : 0);
-                f[p] = vk & 1 ? kv_code_pair(w, true, hi) : kv_code_pair(w, false, lo);
+                const uint32_t z = ((__builtin_amdgcn_perm(w1, w0, 0x05040100u) << vshift) & vmask) | bits.z;
+                f[p] = kv_code_pair(T::kHalf ? v[x][p] >> (i & 8) : v[x][p] >> (vk & 2 ? 8 : 0), vmask, z, bits);
             }
             st.v[t][vk][lane] = kv_frag(f[0], f[1], f[2], f[3]);
         }
@@ -746,12 +772,7 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             float s = kv_scale(word[x]);
             // (words past the sequence's end are anything: no scale of theirs may meet a 0)
             if (lane >= 32 && r * kKvTok + (lane - 32) >= u.len) s = 0.f;
-            float m = lane < 32 ? 0.f : s;
-#pragma unroll
-            for (int y = 1; y < 32; y *= 2) m = fmaxf(m, __shfl_xor(m, y));
-            if (lane < 32) st.ks[g][lane] = s;
-            else st.vs[g][lane - 32] = s;
-            if (lane == 32) st.top[g] = m;
+            (lane < 32 ? st.ks : st.vs)[g][lane & 31] = s;
         }
     };
 
@@ -766,6 +787,64 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     const bool idle = row0 >= u.rows;
     KvSums<UT, CL, NT> sums;
     sums.clear();
+    auto tile = [&](const Stage& st, int t0) {
+        const bool masked = rows.masked(t0);
+        float s[NT][8];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            f32x4 acc[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = g * T::CPG; k < (g + 1) * T::CPG && k < NC; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f16x8 f = st.k[h][k][lane];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][k], acc[n][h]);
+                }
+            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j + 4]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
+                    s[n][e] = g == 0 ? sc * x : fmaf(sc, x, s[n][e]);
+                }
+        }
+        float sv[NG][8], big = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j + 4]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sv[g][e] = e < 4 ? s0[e] : s1[e - 4];
+            big = fmaxf(big, kv_max8(sv[g]));
+        }
+        sums.weigh(s, rows, a.slopes != nullptr, t0, masked, big);
+        const bool unseen = masked && sums.has_nan(sv);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            f16x8 pr[PARTS][NT];
+            if (unseen) sums.template weights<PARTS>(s, sv[g], true, pr);
+            else sums.template weights<PARTS>(s, sv[g], false, pr);
+#pragma unroll
+            for (int t = 0; t < UT; ++t) {
+                if (T::group_of(t) != g) continue;
+#pragma unroll
+                for (int k = 0; k < CL; ++k) {
+                    const f16x8 f = st.v[t][k][lane];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) sums.o[t][k][n] = kv_mfma(f, pr[p][n], sums.o[t][k][n]);
+                }
+            }
+        }
+    };
     if (r0 + 1 < r1) start(r0 + 1);
     __syncthreads();
     for (int r = r0; r < r1; ++r) {
@@ -776,63 +855,8 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             if (r + 2 < r1) start(r + 2);
         }
         const int t0 = r * kKvTok;
-        if (ok && !idle && t0 < rows.any_hi && t0 + kKvTok > rows.any_lo) {
-            const Stage& st = stage[r - r0 & 1];
-            const bool masked = rows.masked(t0);
-            float s[NT][8];
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                f32x4 acc[NT][2];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = g * T::CPG; k < (g + 1) * T::CPG && k < NC; ++k)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const f16x8 f = st.k[h][k][lane];
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][k], acc[n][h]);
-                    }
-                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j + 4]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
-                        s[n][e] = g == 0 ? sc * x : fmaf(sc, x, s[n][e]);
-                    }
-            }
-            float big = st.top[0];
-#pragma unroll
-            for (int g = 1; g < NG; ++g) big = fmaxf(big, st.top[g]);
-            sums.fit(big);
-            sums.weigh(s, rows, a.slopes != nullptr, t0, masked);
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j + 4]);
-                float sv[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sv[e] = e < 4 ? s0[e] : s1[e - 4];
-                f16x8 pr[PARTS][NT];
-                sums.template weights<PARTS>(s, sv, masked, pr);
-#pragma unroll
-                for (int t = 0; t < UT; ++t) {
-                    if (T::group_of(t) != g) continue;
-#pragma unroll
-                    for (int k = 0; k < CL; ++k) {
-                        const f16x8 f = st.v[t][k][lane];
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int p = 0; p < PARTS; ++p) sums.o[t][k][n] = kv_mfma(f, pr[p][n], sums.o[t][k][n]);
-                    }
-                }
-            }
-        }
+        if (ok && !idle && t0 < rows.any_hi && t0 + kKvTok > rows.any_lo) tile(stage[r - r0 & 1], t0);
+        sums.pin();
         ok = ok2;
         __syncthreads();
     }
