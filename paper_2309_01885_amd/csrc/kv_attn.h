@@ -425,10 +425,15 @@ template <int UT, int CL, int NT> struct KvSums {
 __device__ inline float kv_lse(float top, float mass) { return mass == 0.f ? -kKvInf : (top + __builtin_amdgcn_logf(mass)) / kLog2e; }
 
 // ---------------------------------------------------------------- few rows
+// Workgroups of a CU that the registers are to allow.
+constexpr int kv_few_occupancy(int dp, int group, int nt, int parts)
+{
+    return dp <= 128 && group > 32 && nt == 1 ? 3 : dp == 64 && group > 32 ? 3 : 2;
+}
 // A workgroup's waves share the rows of a unit (16 NT) and take its records in turn, each on its
-// own, with the next record's loads in flight; at the end they are joined through LDS.
+// own; at the end they are joined through LDS.
 template <int DP, int GROUP, int NT, int PARTS>
-__global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
+__global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void kv_few_kernel(KvAttn a, KvPlan plan)
 {
     using R = KvRec<DP, GROUP>;
     using T = KvTiles<DP, GROUP>;
@@ -445,66 +450,63 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
     const int r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
     int r = u.rec0 + (int)((int64_t)count * split / u.splits) + wave;
 
+    // A record's words.  The keys' registers are free once the scores are there and take the next
+    // record's keys; the values' likewise after the weighted sum.
     const KvBits bits;
-    struct Raw {
-        uint32_t k[2][NC], v[UT][4], kw[NG][8], vw[NG][8], kz[2][NG];
-    };
-    constexpr bool kAll = 2 * NC + 4 * UT + 18 * NG <= 52;       // whether the words fit in flight besides the codes
+    uint32_t k[2][NC], kw[NG][8], kz[2][NG], v[UT][4], vw[NG][8];
     const int64_t pages = a.c.slots / ((int64_t)a.c.per * kKvTok);
     const int32_t* table = a.table + u.b * a.width;
     const int per = (int)a.c.per;
     int pg = r / per, rem = r - pg * per;
     int id = r < r1 ? table[pg] : 0;
-    const uint8_t* rec = nullptr;                                // of the record loaded last
-    auto codes = [&](Raw& w) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) kv_words<NC>(rec + (uint32_t)(T::key_token(i, h) * R::kKeyRow + j * (4 * NC)), w.k[h]);
-#pragma unroll
-        for (int t = 0; t < UT; ++t) kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(t, i) * (2 * kKvTok) + 16 * j), w.v[t]);
-    };
-    auto words = [&](const uint8_t* at, Raw& w) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            const uint32_t kp = R::kKeyWords + g * (4 * kKvTok);
-            kv_words<8>(at + (kp + 32 * j), w.kw[g]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) w.kz[h][g] = *reinterpret_cast<const uint32_t*>(at + (kp + 4 * T::key_token(i, h)));
-            kv_words<8>(at + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), w.vw[g]);
-        }
-    };
-    // Starts the loads of record r (its page number was read before); false where there is no such page.
-    auto start = [&](Raw& w) {
-        const int page = __builtin_amdgcn_readfirstlane(id);
-        const bool ok = page >= 0 && page < pages;
-        if (ok) {
-            rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
-            codes(w);
-            if (kAll) words(rec, w);
-        } else if (r < r1) {
+    const uint8_t* rec = a.c.pages;
+    bool here = false;                                           // whether the record is there (else any other is read, and not used)
+    // The address of record r, whose page number was read before; reads the one after it.
+    auto find = [&](int r) {
+        int page = __builtin_amdgcn_readfirstlane(id);
+        here = page >= 0 && page < pages;
+        if (!here) {
             set_status(a.status, QE_ERR_ARG);
+            page = 0;
         }
+        rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
         rem += kKvWaves;
         while (rem >= per) {
             rem -= per;
             ++pg;
         }
         if (r + kKvWaves < r1) id = table[pg];            // (in a vector register until it is needed: a wait for it now would be one for all loads)
-        return ok;
     };
-
-    Raw now, next;
-    bool ok = false;
-    if (r < r1) ok = start(now);
-    const uint8_t* at = rec;
+    auto keys = [&] {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) kv_words<NC>(rec + (uint32_t)(T::key_token(i, h) * R::kKeyRow + j * (4 * NC)), k[h]);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const uint32_t kp = R::kKeyWords + g * (4 * kKvTok);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) kz[h][g] = *reinterpret_cast<const uint32_t*>(rec + (kp + 4 * T::key_token(i, h)));
+            kv_words<8>(rec + (kp + 32 * j), kw[g]);
+        }
+    };
+    auto values = [&] {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) kv_words<8>(rec + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), vw[g]);
+#pragma unroll
+        for (int t = 0; t < UT; ++t) kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(t, i) * (2 * kKvTok) + 16 * j), v[t]);
+    };
+    if (r < r1) {
+        find(r);
+        keys();
+        values();
+    }
     KvRows<NC, NT, PARTS> rows;
     rows.load(a, u, u.tile_row);
     KvSums<UT, CL, NT> sums;
     sums.clear();
 
-    auto work = [&](Raw& w, const uint8_t* base) {
-        const int t0 = r * kKvTok;
-        const bool masked = rows.masked(t0);
-        if (!kAll) words(base, w);
+    for (; r < r1; r += kKvWaves) {
+        const int t0 = here ? r * kKvTok : 0x7fffff00;           // (past every sequence's end)
+        const bool masked = rows.masked(t0), more = r + kKvWaves < r1;
         float s[NT][8];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -516,38 +518,42 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t lo, hi;
-                kv_key_zero(w.kz[h][g], lo, hi, bits);
+                kv_key_zero(kz[h][g], lo, hi, bits);
 #pragma unroll
-                for (int k = g * T::CPG; k < (g + 1) * T::CPG && k < NC; ++k) {
-                    const f16x8 f = kv_key_frag(w.k[h][k], lo, hi, bits);
+                for (int c = g * T::CPG; c < (g + 1) * T::CPG && c < NC; ++c) {
+                    const f16x8 f = kv_key_frag(k[h][c], lo, hi, bits);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][k], acc[n][h]);
+                        for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][c], acc[n][h]);
                 }
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float sc = kv_scale(w.kw[g][e]);
+                const float sc = kv_scale(kw[g][e]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const float v = acc[n][e >> 2][e & 3];
-                    s[n][e] = g == 0 ? sc * v : fmaf(sc, v, s[n][e]);
+                    const float x = acc[n][e >> 2][e & 3];
+                    s[n][e] = g == 0 ? sc * x : fmaf(sc, x, s[n][e]);
                 }
             }
+        }
+        if (more) {
+            find(r + kKvWaves);
+            keys();
         }
         if (t0 > u.len - kKvTok) {
             // words past the sequence's end are anything: no scale of theirs may meet a 0
 #pragma unroll
             for (int e = 0; e < 8; ++e)
 #pragma unroll
-                for (int g = 0; g < NG; ++g) w.vw[g][e] = t0 + 8 * j + e < u.len ? w.vw[g][e] : 0u;
+                for (int g = 0; g < NG; ++g) vw[g][e] = t0 + 8 * j + e < u.len ? vw[g][e] : 0u;
         }
         float sv[NG][8], big = 0.f;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sv[g][e] = kv_scale(w.vw[g][e]);
+            for (int e = 0; e < 8; ++e) sv[g][e] = kv_scale(vw[g][e]);
             big = fmaxf(big, kv_max8(sv[g]));
         }
         sums.weigh(s, rows, a.slopes != nullptr, t0, masked, big);
@@ -559,45 +565,28 @@ __global__ __launch_bounds__(256, 2) void kv_few_kernel(KvAttn a, KvPlan plan)
             else sums.template weights<PARTS>(s, sv[g], false, pr);
             uint32_t lo[4], hi[4];
 #pragma unroll
-            for (int p = 0; p < 4; ++p) kv_value_zero(w.vw[g][2 * p], w.vw[g][2 * p + 1], lo[p], hi[p], bits);
+            for (int p = 0; p < 4; ++p) kv_value_zero(vw[g][2 * p], vw[g][2 * p + 1], lo[p], hi[p], bits);
 #pragma unroll
             for (int t = 0; t < UT; ++t) {
                 if (T::group_of(t) != g) continue;
-                uint32_t v[4];
+                uint32_t w[4];
 #pragma unroll
-                for (int p = 0; p < 4; ++p) v[p] = T::kHalf ? w.v[t][p] >> (i & 8) : w.v[t][p];
+                for (int p = 0; p < 4; ++p) w[p] = T::kHalf ? v[t][p] >> (i & 8) : v[t][p];
 #pragma unroll
-                for (int k = 0; k < CL; ++k) {
+                for (int c = 0; c < CL; ++c) {
                     uint32_t x[4];
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) x[p] = kv_code_pair(v[p] >> (k >= 2 ? 8 : 0), k & 1 ? bits.high : bits.low, k & 1 ? hi[p] : lo[p], bits);
+                    for (int p = 0; p < 4; ++p) x[p] = kv_code_pair(w[p] >> (c >= 2 ? 8 : 0), c & 1 ? bits.high : bits.low, c & 1 ? hi[p] : lo[p], bits);
                     const f16x8 f = kv_frag(x[0], x[1], x[2], x[3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) sums.o[t][k][n] = kv_mfma(f, pr[p][n], sums.o[t][k][n]);
+                        for (int p = 0; p < PARTS; ++p) sums.o[t][c][n] = kv_mfma(f, pr[p][n], sums.o[t][c][n]);
                 }
             }
         }
-    };
-    while (r < r1) {
-        bool ok2 = false;
-        r += kKvWaves;
-        if (r < r1) ok2 = start(next);
-        r -= kKvWaves;
-        const uint8_t* at2 = rec;
-        if (ok) work(now, at);
+        if (more) values();
         sums.pin();
-        r += kKvWaves;
-        if (r >= r1) break;
-        ok = false;
-        r += kKvWaves;
-        if (r < r1) ok = start(now);
-        r -= kKvWaves;
-        at = rec;
-        if (ok2) work(next, at2);
-        sums.pin();
-        r += kKvWaves;
     }
     sums.finish();
 
@@ -892,11 +881,14 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     }
 }
 
-// Joins the splits of a row: one wave per row.
-template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a, KvPlan plan)
+// Joins the splits of a row.  ONE: one workgroup per row, whose waves take the splits in turn; else a
+// wave per row (few splits of many rows: a quarter of the workgroups).
+template <int DP, bool ONE> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a, KvPlan plan)
 {
-    const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
+    constexpr int C = (DP + 63) / 64;
+    __shared__ float sum[kKvWaves][DP], mass[kKvWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (ONE ? 1 : kKvWaves) + (ONE ? 0 : wave);
     const int64_t unit = at / plan.rows;
     const int rr = (int)(at - unit * plan.rows);
     if (unit >= plan.units) return;
@@ -908,9 +900,9 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a
     for (int s = lane; s < u.splits; s += 64) m = fmaxf(m, plan.stat[2 * (slot + (int64_t)s * plan.rows)]);
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-    constexpr int C = (DP + 63) / 64;
     float l = 0.f, x[C] = {};
-    for (int s = 0; s < u.splits; ++s) {
+#pragma unroll 4
+    for (int s = ONE ? wave : 0; s < u.splits; s += ONE ? kKvWaves : 1) {
         const int64_t k = slot + (int64_t)s * plan.rows;
         const float t = plan.stat[2 * k], f = t == m ? 1.f : __builtin_amdgcn_exp2f(t - m);
         l = fmaf(plan.stat[2 * k + 1], f, l);
@@ -919,10 +911,21 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a
             if (DP % 64 == 0 || 64 * c + lane < DP) x[c] = fmaf(plan.part[k * DP + 64 * c + lane], f, x[c]);
     }
     const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
+    const int64_t to = (u.first + qi) * a.ot + head * a.oh;
+    if constexpr (ONE) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (64 * c + lane < a.c.dim) kv_out(a, (u.first + qi) * a.ot + head * a.oh + 64 * c + lane, l == 0.f ? 0.f : x[c] / l);
-    if (a.lse && lane == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
+        for (int c = 0; c < C; ++c)
+            if (DP % 64 == 0 || 64 * c + lane < DP) sum[wave][64 * c + lane] = x[c];
+        if (lane == 0) mass[wave] = l;
+        __syncthreads();
+        l = (mass[0] + mass[1]) + (mass[2] + mass[3]);
+        if (tid < a.c.dim) kv_out(a, to + tid, l == 0.f ? 0.f : ((sum[0][tid] + sum[1][tid]) + (sum[2][tid] + sum[3][tid])) / l);
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (64 * c + lane < a.c.dim) kv_out(a, to + 64 * c + lane, l == 0.f ? 0.f : x[c] / l);
+    }
+    if (a.lse && (ONE ? tid : lane) == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
 }
 
 // The form of a call: many rows or few, and a wave's tiles of 16 rows.
@@ -946,8 +949,10 @@ template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm
             hipLaunchKernelGGL((kv_few_kernel<DP, G, DP <= 128 ? 2 : 1, 1>), grid, dim3(256), 0, s, a, plan);
         }
     });
-    if (plan.nsplit > 1)
-        hipLaunchKernelGGL(kv_join_kernel<DP>, grid_xy(cdiv(plan.units * plan.rows, 4), 256), dim3(256), 0, s, a, plan);
+    if (plan.nsplit > 8)
+        hipLaunchKernelGGL((kv_join_kernel<DP, true>), grid_xy(plan.units * plan.rows, 256), dim3(256), 0, s, a, plan);
+    else if (plan.nsplit > 1)
+        hipLaunchKernelGGL((kv_join_kernel<DP, false>), grid_xy(cdiv(plan.units * plan.rows, kKvWaves), 256), dim3(256), 0, s, a, plan);
 }
 
 }  // namespace qe

@@ -12,7 +12,9 @@ extern template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, di
 namespace {
 
 constexpr int64_t kManyFrom = 128;  // query rows of a sequence and key head from which waves have rows of their own
-constexpr int64_t kFill = 1024;     // workgroups that fill the chip
+// Workgroups that fill the chip: two of a CU are resident with many rows; more, with few, even
+// out sequences of different lengths.
+constexpr int64_t kFillMany = 512, kFillFew = 2048;
 
 KvForm form_of(int64_t rows, int dp, bool f32)
 {
@@ -21,9 +23,9 @@ KvForm form_of(int64_t rows, int dp, bool f32)
 }
 
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
-int splits_of(int64_t units, int64_t records)
+int splits_of(bool many, int64_t units, int64_t records)
 {
-    return (int)std::max<int64_t>(1, std::min(kFill / std::max<int64_t>(units, 1), records / kKvMinRecords));
+    return (int)std::max<int64_t>(1, std::min((many ? kFillMany : kFillFew) / std::max<int64_t>(units, 1), records / kKvMinRecords));
 }
 
 struct Sizes {
@@ -53,7 +55,7 @@ size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, i
     size_t need = 0;
     for (int f32 = 0; f32 < 2; ++f32) {
         const Sizes z = sizes_of(batch, max_q, heads, kv_heads, dim, f32 != 0);
-        const int nsplit = splits_of(z.units, INT32_MAX);
+        const int nsplit = splits_of(z.form.many, z.units, INT32_MAX);
         if (nsplit > 1)
             need = std::max(need, align256(part_floats(z, kv_dp(dim), nsplit) * 4) + align256(stat_floats(z, nsplit) * 4));
     }
@@ -73,7 +75,7 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     plan.rows = z.rows;
     int64_t records = a.width * a.c.per;
     if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
-    plan.nsplit = splits_of(z.units, records);
+    plan.nsplit = splits_of(z.form.many, z.units, records);
     plan.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes);
     plan.stat = reinterpret_cast<float*>(reinterpret_cast<char*>(plan.part) + align256(part_floats(z, dp, plan.nsplit) * 4));
     const dim3 grid = grid_xy(z.units * plan.nsplit, 256);
