@@ -42,8 +42,9 @@ struct KvUnit {
     int len, nq, rec0, rec1, splits;        // cached tokens, queries; records that some row sees; splits in use
 };
 
-// Records a split has at least (a workgroup's waves take them in turn).
-constexpr int kKvMinRecords = 4;
+// Records a split has at least (a workgroup's waves take them in turn), and from which splitting gains
+// more than the join costs (a record takes a wave about 1.3 us, the join with its launch 6 us).
+constexpr int kKvMinRecords = 4, kKvSplitFrom = 24;
 
 __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit, bool report)
 {
@@ -81,7 +82,8 @@ __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit,
     if (r0 >= rows || end < begin) end = begin;
     u.rec0 = (int)(begin / kKvTok);
     u.rec1 = end > begin ? (int)((end + kKvTok - 1) / kKvTok) : u.rec0;
-    u.splits = max(1, min(p.nsplit, (u.rec1 - u.rec0) / kKvMinRecords));
+    const int records = u.rec1 - u.rec0;
+    u.splits = records < kKvSplitFrom ? 1 : min(p.nsplit, records / kKvMinRecords);
     return u;
 }
 

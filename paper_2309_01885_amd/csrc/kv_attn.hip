@@ -12,9 +12,9 @@ extern template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, di
 namespace {
 
 constexpr int64_t kManyFrom = 128;  // query rows of a sequence and key head from which waves have rows of their own
-// Workgroups that fill the chip: two of a CU are resident with many rows; more, with few, even
-// out sequences of different lengths.
-constexpr int64_t kFillMany = 512, kFillFew = 2048;
+// Workgroups that fill the chip once: three of a CU with few rows (rounds more than one help only
+// where the sequences' lengths differ), two with many.
+constexpr int64_t kFillMany = 512, kFillFew = 768;
 
 KvForm form_of(int64_t rows, int dp, bool f32)
 {
@@ -25,6 +25,7 @@ KvForm form_of(int64_t rows, int dp, bool f32)
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
 int splits_of(bool many, int64_t units, int64_t records)
 {
+    if (records < kKvSplitFrom) return 1;
     return (int)std::max<int64_t>(1, std::min((many ? kFillMany : kFillFew) / std::max<int64_t>(units, 1), records / kKvMinRecords));
 }
 

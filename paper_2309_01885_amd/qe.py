@@ -387,38 +387,50 @@ def lambda_max(Sigma: torch.Tensor, max_iters: int = 500, tol: float = 1e-7,
 
 
 # ---------------------------------------------------------------------------- key/value cache in 4 bits
+# These calls come once a layer and token, so their checks are kept short: one read of each
+# attribute, plain integers for pointers, the raw stream handle.
 _DTYPES = {torch.float32: QE_F32, torch.float16: QE_F16, torch.bfloat16: QE_BF16}
+_kv_layouts = {}    # (kv_heads, page / 32, record bytes, dim, group) of caches that fit together
 
 
-def _heads(t: torch.Tensor, name: str, shape=None, dtype=None):
-    """A tokens x heads x dim tensor whose channels are contiguous: (pointer, dtype code, strides)."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name} must be {dtype or 'float32, float16 or bfloat16'}, got {t.dtype}")
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{name} must be {tuple(shape) if shape is not None else 'tokens x heads x dim'}, "
-                         f"got {tuple(t.shape)}")
-    if t.numel() > 0 and t.shape[2] > 1 and t.stride(2) != 1:
-        raise ValueError(f"{name}: the channels of a head must be contiguous")
-    return _vp(t.data_ptr()), _DTYPES[t.dtype], t.stride(0), t.stride(1)
+def _bad(name: str, t: torch.Tensor, want: str):
+    raise ValueError(f"{name} must be {want}, got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
 
 
 def _pages(pages: torch.Tensor, dim: int, group: int):
-    """Checks a cache made by kv_pages: (pointer, pages, tokens of a page, kv heads)."""
-    if pages.dim() != 4:
-        raise ValueError("pages must be pages x kv_heads x page / 32 x record bytes (kv_pages)")
-    num, kv, per, rec = pages.shape
-    need = load().qe_kv_page_bytes(kv, dim, group, 32 * per)
-    if need == 0 or need != kv * per * rec:
-        raise ValueError(f"pages do not fit dim {dim} and group {group}")
-    return _ptr(pages, torch.uint8, "pages"), num, 32 * per, kv
+    """Checks a cache made by kv_pages: (pages, tokens of a page, kv heads, device index)."""
+    shape = pages.shape
+    if len(shape) != 4 or pages.dtype != torch.uint8 or not pages.is_cuda or not pages.is_contiguous():
+        _bad("pages", pages, "a contiguous uint8 device tensor, pages x kv_heads x page / 32 x record bytes (kv_pages)")
+    num, kv, per, rec = shape
+    key = (kv, per, rec, dim, group)
+    if key not in _kv_layouts:
+        need = load().qe_kv_page_bytes(kv, dim, group, 32 * per)
+        if need == 0 or need != kv * per * rec:
+            raise ValueError(f"pages {tuple(shape)} do not fit dim {dim} and group {group}")
+        _kv_layouts[key] = True
+    return num, 32 * per, kv, pages.get_device()
 
 
-def _same_device(ref: torch.Tensor, **others):
-    for name, t in others.items():
-        if t is not None and t.device != ref.device:
-            raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+def _heads(t: torch.Tensor, name: str, shape: tuple, dtype, dev: int):
+    """Checks a tokens x heads x dim tensor whose channels are contiguous: (stride of a token, of a head)."""
+    st = t.stride()
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or (st[2] != 1 and shape[2] > 1 and t.numel()):
+        _bad(name, t, f"{shape} {dtype} on GPU {dev} with contiguous channels")
+    return st[0], st[1]
+
+
+def _flat(t: Optional[torch.Tensor], name: str, dtype, dev: int, numel: Optional[int] = None):
+    """Pointer of a contiguous tensor, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != dev or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        _bad(name, t, f"contiguous {dtype}{'' if numel is None else f' of {numel} elements'} on GPU {dev}")
+    return t.data_ptr()
+
+
+def _raw_stream(dev: int, stream):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def kv_page_bytes(kv_heads: int, dim: int, group: int = 64, page: int = 64) -> int:
@@ -440,16 +452,19 @@ def kv_write(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, pages: torch
     """Quantizes K and V (tokens x kv_heads x dim; any token and head strides) into the
     slots (int64) of the cache (qe_kv_write).  status: None or an int32 device tensor of one element,
     set to QE_ERR_ARG by a slot past the cache (never cleared)."""
-    lib = load()
-    if pages.dim() != 4 or K.dim() != 3:
-        raise ValueError("K must be tokens x kv_heads x dim, pages a cache of kv_pages")
-    n, kv, dim = K.shape
-    pp, num, page, heads = _pages(pages, dim, group)
-    kp, dt, kt, kh = _heads(K, "K", (n, heads, dim))
-    vp, _, vt, vh = _heads(V, "V", (n, heads, dim), K.dtype)
-    _same_device(pages, K=K, V=V, slots=slots, status=status)
-    _check(lib.qe_kv_write(kp, vp, dt, n, heads, dim, kt, kh, vt, vh, _ptr(slots, torch.int64, "slots", n), group,
-                           pp, num, page, _ptr(status, torch.int32, "status", 1), _stream(stream)), "qe_kv_write")
+    shape, dtype = K.shape, K.dtype
+    if len(shape) != 3 or dtype not in _DTYPES:
+        _bad("K", K, "tokens x kv_heads x dim in float32, float16 or bfloat16")
+    n, _, dim = shape
+    num, page, heads, dev = _pages(pages, dim, group)
+    shape = (n, heads, dim)
+    kt, kh = _heads(K, "K", shape, dtype, dev)
+    vt, vh = _heads(V, "V", shape, dtype, dev)
+    code = load().qe_kv_write(K.data_ptr(), V.data_ptr(), _DTYPES[dtype], n, heads, dim, kt, kh, vt, vh,
+                              _flat(slots, "slots", torch.int64, dev, n), group, pages.data_ptr(), num, page,
+                              _flat(status, "status", torch.int32, dev, 1), _raw_stream(dev, stream))
+    if code:
+        raise QEError(code, "qe_kv_write")
     return pages
 
 
@@ -458,18 +473,24 @@ def kv_read(pages: torch.Tensor, slots: torch.Tensor, dim: int, group: int = 64,
             status: Optional[torch.Tensor] = None, stream=None):
     """The keys and values (tokens x kv_heads x dim) that the cache holds at the slots
     (qe_kv_read); into K and V where given."""
-    lib = load()
-    pp, num, page, heads = _pages(pages, dim, group)
+    num, page, heads, dev = _pages(pages, dim, group)
     n = slots.numel()
+    shape = (n, heads, dim)
+    if K is not None or V is not None:
+        dtype = (K if K is not None else V).dtype
+    if dtype not in _DTYPES:
+        raise ValueError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
     if K is None:
-        K = torch.empty((n, heads, dim), dtype=dtype, device=pages.device)
+        K = torch.empty(shape, dtype=dtype, device=pages.device)
     if V is None:
-        V = torch.empty((n, heads, dim), dtype=K.dtype, device=pages.device)
-    kp, dt, kt, kh = _heads(K, "K", (n, heads, dim))
-    vp, _, vt, vh = _heads(V, "V", (n, heads, dim), K.dtype)
-    _same_device(pages, K=K, V=V, slots=slots, status=status)
-    _check(lib.qe_kv_read(pp, num, page, _ptr(slots, torch.int64, "slots"), n, heads, dim, group, kp, vp, dt, kt,
-                          kh, vt, vh, _ptr(status, torch.int32, "status", 1), _stream(stream)), "qe_kv_read")
+        V = torch.empty(shape, dtype=dtype, device=pages.device)
+    kt, kh = _heads(K, "K", shape, dtype, dev)
+    vt, vh = _heads(V, "V", shape, dtype, dev)
+    code = load().qe_kv_read(pages.data_ptr(), num, page, _flat(slots, "slots", torch.int64, dev), n, heads, dim, group,
+                             K.data_ptr(), V.data_ptr(), _DTYPES[dtype], kt, kh, vt, vh,
+                             _flat(status, "status", torch.int32, dev, 1), _raw_stream(dev, stream))
+    if code:
+        raise QEError(code, "qe_kv_read")
     return K, V
 
 
@@ -490,12 +511,14 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
     scale: 1 / sqrt(dim) unless given.  lse: None or float32, total x heads, written.  The call does
     not wait for the device; check=True does, and raises if it met a bad page number, length or
     query range (sync_status(ws) tells later otherwise)."""
-    lib = load()
-    if Q.dim() != 3 or table.dim() != 2:
-        raise ValueError("Q must be total x heads x dim, table sequences x pages")
-    total, heads, dim = Q.shape
+    shape, dtype = Q.shape, Q.dtype
+    if len(shape) != 3 or dtype not in _DTYPES:
+        _bad("Q", Q, "total x heads x dim in float32, float16 or bfloat16")
+    if table.dim() != 2:
+        _bad("table", table, "sequences x pages")
+    total, heads, dim = shape
     batch, width = table.shape
-    pp, num, page, kv = _pages(pages, dim, group)
+    num, page, kv, dev = _pages(pages, dim, group)
     if q_start is None:
         if max_q is None:
             max_q = total // batch if batch else 0
@@ -503,19 +526,23 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
             raise ValueError(f"{total} queries are not {max_q} for each of {batch} sequences: give q_start")
     elif max_q is None:
         raise ValueError("q_start needs max_q, the largest number of queries of a sequence")
+    shape = (total, heads, dim)
     if out is None:
-        out = torch.empty((total, heads, dim), dtype=Q.dtype, device=Q.device)
-    qp, dt, qt, qh = _heads(Q, "Q")
-    op, _, ot, oh = _heads(out, "out", (total, heads, dim), Q.dtype)
+        out = torch.empty(shape, dtype=dtype, device=pages.device)
+    qt, qh = _heads(Q, "Q", shape, dtype, dev)
+    ot, oh = _heads(out, "out", shape, dtype, dev)
     if ws is None:
-        ws = workspace(kv_attn_workspace_size(total, batch, max_q, heads, kv, dim), Q.device)
-    _same_device(pages, Q=Q, table=table, lengths=lengths, q_start=q_start, slopes=slopes, out=out, lse=lse, ws=ws)
-    _check(lib.qe_kv_attn(qp, dt, total, heads, dim, qt, qh,
-                          _ptr(q_start, torch.int32, "q_start", batch + 1), batch, max_q, pp, num, page, kv, group,
-                          _ptr(table, torch.int32, "table"), width, _ptr(lengths, torch.int32, "lengths", batch),
-                          1.0 / dim ** 0.5 if scale is None else float(scale), 1 if causal else 0, int(window),
-                          _ptr(slopes, torch.float32, "slopes", heads), op, ot, oh,
-                          _ptr(lse, torch.float32, "lse", total * heads), _vp(ws.data_ptr()), ws.numel(),
-                          _stream(stream)), "qe_kv_attn")
-    _finish(ws, check, "qe_kv_attn", stream)
+        ws = workspace(kv_attn_workspace_size(total, batch, max_q, heads, kv, dim), pages.device)
+    code = load().qe_kv_attn(Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
+                             _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
+                             num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
+                             _flat(lengths, "lengths", torch.int32, dev, batch),
+                             dim ** -0.5 if scale is None else scale, 1 if causal else 0, window,
+                             _flat(slopes, "slopes", torch.float32, dev, heads), out.data_ptr(), ot, oh,
+                             _flat(lse, "lse", torch.float32, dev, total * heads),
+                             _flat(ws, "ws", torch.uint8, dev), ws.numel(), _raw_stream(dev, stream))
+    if code:
+        raise QEError(code, "qe_kv_attn")
+    if check:
+        _finish(ws, check, "qe_kv_attn", stream)
     return out
