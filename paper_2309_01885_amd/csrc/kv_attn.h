@@ -329,29 +329,37 @@ template <int UT, int CL, int NT> struct KvSums {
                     for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
         }
     }
-    // s: the products times their key scales; on return p 2^shift (0 where the row sees nothing).
-    // masked: some row does not see the whole record.  big: the lane's largest value scale.
-    template <int NC, int PARTS>
-    __device__ void weigh(float (&s)[NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, int t0, bool masked, float big)
+    // s: the products times their key scales, of KR records that start at tokens t0; on return p 2^shift
+    // (0 where the row sees nothing).  masked: some row does not see all of them.  big: the lane's
+    // largest value scale.
+    template <int KR, int NC, int PARTS>
+    __device__ void weigh(float (&s)[KR][NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, const int (&t0)[KR], bool masked, float big)
     {
         float at[NT], c[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             c[n] = r.c[n];
-            at[n] = c[n] * kv_max8(s[n]);
+            at[n] = kv_max8(s[0][n]);
+#pragma unroll
+            for (int y = 1; y < KR; ++y) at[n] = fmaxf(at[n], kv_max8(s[y][n]));
+            at[n] *= c[n];
         }
         if (masked || slopes) {
-            const int t = t0 + 8 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float base = r.slope[n] * (float)(t - (r.hi[n] - 1));
+                at[n] = -kKvInf;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[n][e] = fmaf(s[n][e], c[n], fmaf(r.slope[n], (float)e, base));
-                    s[n][e] = t + e >= r.lo[n] && t + e < r.hi[n] ? s[n][e] : -kKvInf;
+                for (int y = 0; y < KR; ++y) {
+                    const int t = t0[y] + 8 * ((threadIdx.x & 63) >> 4);
+                    const float base = r.slope[n] * (float)(t - (r.hi[n] - 1));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        s[y][n][e] = fmaf(s[y][n][e], c[n], fmaf(r.slope[n], (float)e, base));
+                        s[y][n][e] = t + e >= r.lo[n] && t + e < r.hi[n] ? s[y][n][e] : -kKvInf;
+                    }
+                    at[n] = fmaxf(at[n], kv_max8(s[y][n]));
                 }
                 c[n] = 1.f;
-                at[n] = kv_max8(s[n]);
             }
         }
         move(at, big);
@@ -359,8 +367,12 @@ template <int UT, int CL, int NT> struct KvSums {
         for (int n = 0; n < NT; ++n) {
             const float off = top[n] == -kKvInf ? 0.f : shift - top[n];     // (nothing seen so far: every s is -inf)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c[n], off));
-            mass[n] += ((s[n][0] + s[n][1]) + (s[n][2] + s[n][3])) + ((s[n][4] + s[n][5]) + (s[n][6] + s[n][7]));
+            for (int y = 0; y < KR; ++y) {
+                float (&x)[8] = s[y][n];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], c[n], off));
+                mass[n] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+            }
         }
     }
     // The products' fp16 weights p s' of a group.  unseen: a token that some row does not see may have
@@ -509,7 +521,7 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     for (; r < r1; r += kKvWaves) {
         const int t0 = here ? r * kKvTok : 0x7fffff00;           // (past every sequence's end)
         const bool masked = rows.masked(t0), more = r + kKvWaves < r1;
-        float s[NT][8];
+        float s[1][NT][8];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             f32x4 acc[NT][2];
@@ -536,7 +548,7 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float x = acc[n][e >> 2][e & 3];
-                    s[n][e] = g == 0 ? sc * x : fmaf(sc, x, s[n][e]);
+                    s[0][n][e] = g == 0 ? sc * x : fmaf(sc, x, s[0][n][e]);
                 }
             }
         }
@@ -558,13 +570,14 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
             for (int e = 0; e < 8; ++e) sv[g][e] = kv_scale(vw[g][e]);
             big = fmaxf(big, kv_max8(sv[g]));
         }
-        sums.weigh(s, rows, a.slopes != nullptr, t0, masked, big);
+        const int at[1] = {t0};
+        sums.weigh(s, rows, a.slopes != nullptr, at, masked, big);
         const bool unseen = masked && sums.has_nan(sv);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             f16x8 pr[PARTS][NT];
-            if (unseen) sums.template weights<PARTS>(s, sv[g], true, pr);
-            else sums.template weights<PARTS>(s, sv[g], false, pr);
+            if (unseen) sums.template weights<PARTS>(s[0], sv[g], true, pr);
+            else sums.template weights<PARTS>(s[0], sv[g], false, pr);
             uint32_t lo[4], hi[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) kv_value_zero(vw[g][2 * p], vw[g][2 * p + 1], lo[p], hi[p], bits);
@@ -647,21 +660,28 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
 }
 
 // ---------------------------------------------------------------- many rows
-// Every wave has 16 NT rows of its own and the workgroup goes through the records together.  A record's
-// codes are turned into fp16 once, each wave a quarter of them, and reach the others through LDS as
-// the products' operands (1 KB each, in lane order); while record r is multiplied, r + 1 is
-// converted and r + 2 is on its way.
+// Every wave has 16 NT rows of its own and the workgroup goes through the records together, KR at a
+// time.  Codes are turned into fp16 once, by kKvWaves / KR waves a record, and reach the others
+// through LDS as the products' operands (1 KB each, in lane order); while a stage is multiplied,
+// the next is converted and the one after it is on its way.  A stage is straight code, also where a
+// wave's rows see none of it and past the last record: conversion and first products, then
+// exponentials and second products can overlap.
+constexpr int kv_stage_records(int dp) { return dp <= 128 ? 2 : 1; }
+
 template <int DP, int GROUP, int NT, int PARTS>
 __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
 {
     using R = KvRec<DP, GROUP>;
     using T = KvTiles<DP, GROUP>;
     constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
-    constexpr int CW = (NC + 1) / 2;                             // key products a wave converts
-    constexpr int VW = T::kHalf ? (UT + 1) / 2 : UT;             // value products
+    constexpr int KR = kv_stage_records(DP), W = kKvWaves / KR;  // records of a stage, waves that convert one
+    constexpr int CW = KR == 2 ? NC : (NC + 1) / 2;              // key products a wave converts
+    constexpr int VW = T::kHalf ? (UT + 1) / 2 : UT, VK = KR;    // unit tiles and classes
+    constexpr int SW = KR == 2 ? (NG + 1) / 2 : (NG + 3) / 4;    // scales a lane converts
     struct Stage {
-        f16x8 k[2][NC][64], v[UT][CL][64];
-        float ks[NG][kKvTok], vs[NG][kKvTok];
+        f16x8 k[KR][2][NC][64], v[KR][UT][CL][64];
+        float ks[KR][NG][kKvTok], vs[KR][NG][kKvTok];
+        int at[KR];                                              // the records' first tokens
     };
     __shared__ Stage stage[2];
     // workgroups of an XCD (every eighth) get a contiguous stretch of units: rows of the same keys
@@ -680,69 +700,78 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     const int r0 = u.rec0 + (int)((int64_t)count * split / u.splits), r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
     const int row0 = u.tile_row + wave * (16 * NT);
 
+    // what the wave converts: of record `part` of a stage, key half kh from channel block kc on, value
+    // classes vk .. of the unit tiles vt, vt + 2, .. (groups of 32) or all
+    const int part = wave / W, q = wave % W;
+    const int kh = q & 1, kc = KR == 2 ? 0 : (q >> 1) * CW;
+    const int vk = T::kHalf ? (KR == 2 ? 0 : q & 1) : KR == 2 ? 2 * (q & 1) : q;
+    const int vt = T::kHalf ? (KR == 2 ? q & 1 : q >> 1) : 0;
+    const KvBits bits;
+    const uint32_t vmask = vk & 1 ? bits.high : bits.low, vshift = vk & 1 ? 4 : 0;   // (KR == 1)
+    const int token = T::key_token(i, kh);
+    uint32_t k[CW], kz[NG], v[VW][4], vw[NG][8], word[SW];
+
     const int64_t pages = a.c.slots / ((int64_t)a.c.per * kKvTok);
     const int32_t* table = a.table + u.b * a.width;
     const int per = (int)a.c.per;
-    int pg = r0 / per, rem = r0 - pg * per;
+    // the wave's record of the next stage to be loaded, its page's place in the table and its place in the page
+    int next = min(r0 + part, r1 - 1), pg = next / per, rem = next - pg * per;
     int id = r0 < r1 ? table[pg] : 0;
-
-    // what the wave converts of a record
-    const int kh = wave & 1, kc = (wave >> 1) * CW;              // half and first channel block of the keys
-    const int vk = T::kHalf ? wave & 1 : wave, vt = T::kHalf ? wave >> 1 : 0;   // class; first unit tile (every second)
-    const KvBits bits;
-    const uint32_t vmask = vk & 1 ? bits.high : bits.low, vshift = vk & 1 ? 4 : 0;
-    uint32_t k[CW], kz[NG], v[VW][4], vw[NG][8], word[(NG + 3) / 4];
-    bool have = false;
-    auto start = [&](int r) {
-        const int page = __builtin_amdgcn_readfirstlane(id);
-        have = page >= 0 && page < pages;
-        if (have) {
-            const uint8_t* rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
-            const int token = T::key_token(i, kh);
-#pragma unroll
-            for (int x = 0; x < CW; ++x)
-                k[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(token * R::kKeyRow + j * (4 * NC)) + 4 * (NC % 2 != 0 ? min(kc + x, NC - 1) : kc + x));
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                kz[g] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(R::kKeyWords + g * (4 * kKvTok) + 4 * token));
-                kv_words<8>(rec + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), vw[g]);
-            }
-#pragma unroll
-            for (int x = 0; x < VW; ++x)
-                kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(T::kHalf ? min(vt + 2 * x, UT - 1) : x, i) * (2 * kKvTok) + 16 * j), v[x]);
-            // a wave's lanes: 32 key words, 32 value words of a group
-#pragma unroll
-            for (int x = 0; x < (NG + 3) / 4; ++x)
-                word[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)((lane < 32 ? R::kKeyWords : R::kValWords) + min(wave + 4 * x, NG - 1) * (4 * kKvTok) + 4 * (lane & 31)));
-        } else if (tid == 0) {
-            set_status(a.status, QE_ERR_ARG);
+    bool here = false;                                           // whether the record is there (else any other is read, and not used)
+    // Starts the loads of the wave's share of the next stage, whose page number was read before, and reads
+    // the one after it.  Past the last record it is loaded again.
+    auto start = [&] {
+        int page = __builtin_amdgcn_readfirstlane(id);
+        here = page >= 0 && page < pages;
+        if (!here) {
+            if (lane == 0) set_status(a.status, QE_ERR_ARG);
+            page = 0;
         }
-        if (++rem == per) {
-            rem = 0;
+        const uint8_t* rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
+        kv_words<CW>(rec + (uint32_t)(token * R::kKeyRow + j * (4 * NC)) + 4 * kc, k);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            kz[g] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(R::kKeyWords + g * (4 * kKvTok) + 4 * token));
+            kv_words<8>(rec + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), vw[g]);
+        }
+#pragma unroll
+        for (int x = 0; x < VW; ++x)
+            kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(T::kHalf ? min(vt + 2 * x, UT - 1) : x, i) * (2 * kKvTok) + 16 * j), v[x]);
+#pragma unroll
+        for (int x = 0; x < SW; ++x) {
+            const bool key = KR == 2 ? kh == 0 : lane < 32;
+            const int g = KR == 2 ? min((lane >> 5) + 2 * x, NG - 1) : min(q + 4 * x, NG - 1);
+            word[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)((key ? R::kKeyWords : R::kValWords) + g * (4 * kKvTok) + 4 * (lane & 31)));
+        }
+        const int step = min(KR, r1 - 1 - next);
+        next += step;
+        rem += step;
+        while (rem >= per) {
+            rem -= per;
             ++pg;
         }
-        if (r + 1 < r1) id = table[pg];          // (in a vector register until it is needed: a wait for it now would be one for all loads)
+        id = table[pg];                                   // (in a vector register until it is needed: a wait for it now would be one for all loads)
     };
+    // r: the first record of the stage
     auto convert = [&](Stage& st, int r) {
-        if (!have) return;
 #pragma unroll
         for (int x = 0; x < CW; ++x) {
-            if (NC % 2 != 0 && kc + x >= NC) continue;
+            if (KR == 1 && NC % 2 != 0 && kc + x >= NC) continue;
             uint32_t lo, hi;
-            if constexpr (NG == 1) kv_key_zero(kz[0], lo, hi, bits);
+            if constexpr (KR == 2) kv_key_zero(kz[x / T::CPG], lo, hi, bits);
             else {
                 uint32_t z = kz[0];
 #pragma unroll
                 for (int g = 1; g < NG; ++g) z = (kc + x) / T::CPG == g ? kz[g] : z;
                 kv_key_zero(z, lo, hi, bits);
             }
-            st.k[kh][kc + x][lane] = kv_key_frag(k[x], lo, hi, bits);
+            st.k[part][kh][kc + x][lane] = kv_key_frag(k[x], lo, hi, bits);
         }
 #pragma unroll
         for (int x = 0; x < VW; ++x) {
             const int t = T::kHalf ? vt + 2 * x : x;
             if (T::kHalf && UT % 2 != 0 && t >= UT) continue;
-            uint32_t f[4];
+            uint32_t f[VK][4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 uint32_t w0 = vw[0][2 * p], w1 = vw[0][2 * p + 1];
@@ -751,107 +780,120 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
                     w0 = T::group_of(t) == g ? vw[g][2 * p] : w0;
                     w1 = T::group_of(t) == g ? vw[g][2 * p + 1] : w1;
                 }
-                const uint32_t z = ((__builtin_amdgcn_perm(w1, w0, 0x05040100u) << vshift) & vmask) | bits.z;
-                f[p] = kv_code_pair(T::kHalf ? v[x][p] >> (i & 8) : v[x][p] >> (vk & 2 ? 8 : 0), vmask, z, bits);
+                const uint32_t w = v[x][p] >> (T::kHalf ? i & 8 : vk & 2 ? 8 : 0);
+                if constexpr (KR == 2) {
+                    uint32_t lo, hi;
+                    kv_value_zero(w0, w1, lo, hi, bits);
+                    f[0][p] = kv_code_pair(w, bits.low, lo, bits);
+                    f[1][p] = kv_code_pair(w, bits.high, hi, bits);
+                } else {
+                    const uint32_t z = ((__builtin_amdgcn_perm(w1, w0, 0x05040100u) << vshift) & vmask) | bits.z;
+                    f[0][p] = kv_code_pair(w, vmask, z, bits);
+                }
             }
-            st.v[t][vk][lane] = kv_frag(f[0], f[1], f[2], f[3]);
+#pragma unroll
+            for (int y = 0; y < VK; ++y) st.v[part][t][vk + y][lane] = kv_frag(f[y][0], f[y][1], f[y][2], f[y][3]);
         }
 #pragma unroll
-        for (int x = 0; x < (NG + 3) / 4; ++x) {
-            const int g = wave + 4 * x;
-            if (g >= NG) continue;
-            float s = kv_scale(word[x]);
+        for (int x = 0; x < SW; ++x) {
+            const bool key = KR == 2 ? kh == 0 : lane < 32;
+            const int g = KR == 2 ? (lane >> 5) + 2 * x : q + 4 * x;
+            float sc = kv_scale(word[x]);
             // (words past the sequence's end are anything: no scale of theirs may meet a 0)
-            if (lane >= 32 && r * kKvTok + (lane - 32) >= u.len) s = 0.f;
-            (lane < 32 ? st.ks : st.vs)[g][lane & 31] = s;
+            if (!key && (r + part) * kKvTok + (lane & 31) >= u.len) sc = 0.f;
+            if (g < NG) (key ? st.ks : st.vs)[part][g][lane & 31] = sc;
         }
+        // (past the last record, or on a page that is not there: past every sequence's end)
+        if (q == 0 && lane == 0) st.at[part] = here && r + part < r1 ? (r + part) * kKvTok : 0x7fffff00;
     };
 
-    bool ok = false;
-    if (r0 < r1) {
-        start(r0);
-        convert(stage[0], r0);
-        ok = have;
-    }
     KvRows<NC, NT, PARTS> rows;
     rows.load(a, u, min(row0, u.rows - 1));
-    const bool idle = row0 >= u.rows;
     KvSums<UT, CL, NT> sums;
     sums.clear();
-    auto tile = [&](const Stage& st, int t0) {
-        const bool masked = rows.masked(t0);
-        float s[NT][8];
+    if (r0 < r1) {
+        start();
+        convert(stage[0], r0);
+        start();
+    }
+    __syncthreads();
+    for (int r = r0, b = 0; r < r1; r += KR, b ^= 1) {
+        convert(stage[b ^ 1], r + KR);
+        const Stage& st = stage[b];
+        float s[KR][NT][8];
+        int t0[KR];
+        bool masked = false;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            f32x4 acc[NT][2];
+        for (int y = 0; y < KR; ++y) {
+            t0[y] = __builtin_amdgcn_readfirstlane(st.at[y]);
+            masked = masked || rows.masked(t0[y]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int g = 0; g < NG; ++g) {
+                f32x4 acc[NT][2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int k = g * T::CPG; k < (g + 1) * T::CPG && k < NC; ++k)
+                    for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const f16x8 f = st.k[h][k][lane];
+                for (int c = g * T::CPG; c < (g + 1) * T::CPG && c < NC; ++c)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                    for (int h = 0; h < 2; ++h) {
+                        const f16x8 f = st.k[y][h][c][lane];
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][k], acc[n][h]);
-                }
-            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[g][8 * j + 4]);
+                        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+                            for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][c], acc[n][h]);
+                    }
+                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[y][g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[y][g][8 * j + 4]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
-                    s[n][e] = g == 0 ? sc * x : fmaf(sc, x, s[n][e]);
-                }
-        }
-        float sv[NG][8], big = 0.f;
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.vs[g][8 * j + 4]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sv[g][e] = e < 4 ? s0[e] : s1[e - 4];
-            big = fmaxf(big, kv_max8(sv[g]));
-        }
-        sums.weigh(s, rows, a.slopes != nullptr, t0, masked, big);
-        const bool unseen = masked && sums.has_nan(sv);
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            f16x8 pr[PARTS][NT];
-            if (unseen) sums.template weights<PARTS>(s, sv[g], true, pr);
-            else sums.template weights<PARTS>(s, sv[g], false, pr);
-#pragma unroll
-            for (int t = 0; t < UT; ++t) {
-                if (T::group_of(t) != g) continue;
-#pragma unroll
-                for (int k = 0; k < CL; ++k) {
-                    const f16x8 f = st.v[t][k][lane];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p) sums.o[t][k][n] = kv_mfma(f, pr[p][n], sums.o[t][k][n]);
-                }
+                    for (int e = 0; e < 8; ++e) {
+                        const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
+                        s[y][n][e] = g == 0 ? sc * x : fmaf(sc, x, s[y][n][e]);
+                    }
             }
         }
-    };
-    if (r0 + 1 < r1) start(r0 + 1);
-    __syncthreads();
-    for (int r = r0; r < r1; ++r) {
-        bool ok2 = false;
-        if (r + 1 < r1) {
-            convert(stage[r + 1 - r0 & 1], r + 1);
-            ok2 = have;
-            if (r + 2 < r1) start(r + 2);
-        }
-        const int t0 = r * kKvTok;
-        if (ok && !idle && t0 < rows.any_hi && t0 + kKvTok > rows.any_lo) tile(stage[r - r0 & 1], t0);
+        start();
+        float big = 0.f, sv[KR][NG][8];
+#pragma unroll
+        for (int y = 0; y < KR; ++y)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.vs[y][g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.vs[y][g][8 * j + 4]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sv[y][g][e] = e < 4 ? s0[e] : s1[e - 4];
+                big = fmaxf(big, kv_max8(sv[y][g]));
+            }
+        sums.weigh(s, rows, a.slopes != nullptr, t0, masked, big);
+        bool unseen = false;
+        if (masked)
+#pragma unroll
+            for (int y = 0; y < KR; ++y) unseen = unseen || sums.has_nan(sv[y]);
+#pragma unroll
+        for (int y = 0; y < KR; ++y)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                f16x8 pr[PARTS][NT];
+                if (unseen) sums.template weights<PARTS>(s[y], sv[y][g], true, pr);
+                else sums.template weights<PARTS>(s[y], sv[y][g], false, pr);
+#pragma unroll
+                for (int t = 0; t < UT; ++t) {
+                    if (T::group_of(t) != g) continue;
+#pragma unroll
+                    for (int c = 0; c < CL; ++c) {
+                        const f16x8 f = st.v[y][t][c][lane];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int p = 0; p < PARTS; ++p) sums.o[t][c][n] = kv_mfma(f, pr[p][n], sums.o[t][c][n]);
+                    }
+                }
+            }
         sums.pin();
-        ok = ok2;
         __syncthreads();
     }
-    if (idle) return;
+    if (row0 >= u.rows) return;
     sums.finish();
     const float back = __builtin_amdgcn_exp2f(-sums.shift);
 #pragma unroll
