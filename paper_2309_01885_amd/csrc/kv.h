@@ -98,7 +98,7 @@ struct KvAttn {
     int32_t causal, window;
     const float* slopes;           // or null
     int32_t dtype, group;
-    bool vec_q;                    // 16-byte loads of Q
+    bool vec_q, vec_o;             // 16-byte accesses of q and out
     int* status;
 };
 

@@ -46,6 +46,9 @@ struct KvUnit {
 // more than the join costs (a record takes a wave about 1.3 us, the join with its launch 6 us).
 constexpr int kKvMinRecords = 4, kKvSplitFrom = 24;
 
+// A value that is the same for the whole workgroup and not written by the kernel: a scalar load.
+__device__ inline int kv_scalar(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)p; }
+
 __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit, bool report)
 {
     KvUnit u;
@@ -58,14 +61,14 @@ __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit,
     u.first = u.b * a.max_q;
     int64_t nq = a.max_q;
     if (a.q_start) {
-        u.first = a.q_start[u.b];
-        nq = (int64_t)a.q_start[u.b + 1] - u.first;
+        u.first = kv_scalar(a.q_start + u.b);
+        nq = (int64_t)kv_scalar(a.q_start + u.b + 1) - u.first;
         bad = u.first < 0 || nq < 0 || nq > a.max_q || u.first + nq > a.total;
         u.first = u.first < 0 ? 0 : u.first;
         nq = max((int64_t)0, min(min(nq, a.max_q), a.total - u.first));
     }
     const int64_t room = a.width * (int64_t)a.c.per * kKvTok;
-    int64_t len = a.lengths[u.b];
+    int64_t len = kv_scalar(a.lengths + u.b);
     bad = bad || len < 0 || len > room;
     len = len < 0 ? 0 : min(len, room);
     if (bad && report && tile == 0 && u.kvh == 0) set_status(a.status, QE_ERR_ARG);
@@ -87,11 +90,12 @@ __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit,
     return u;
 }
 
-__device__ inline void kv_q8(const KvAttn& a, int64_t at, float* x)
+// Eight channels of out.  (Fp32 calls are the kernels with PARTS == 2.)
+template <int PARTS> __device__ inline void kv_out8(const KvAttn& a, int64_t at, const float* x)
 {
-    if (a.dtype == QE_F32) kv_load8(static_cast<const float*>(a.q) + at, a.vec_q, x);
-    else if (a.dtype == QE_F16) kv_load8(static_cast<const _Float16*>(a.q) + at, a.vec_q, x);
-    else kv_load8(static_cast<const __bf16*>(a.q) + at, a.vec_q, x);
+    if constexpr (PARTS == 2) kv_store8(static_cast<float*>(a.out) + at, a.vec_o, x);
+    else if (a.dtype == QE_F16) kv_store8(static_cast<_Float16*>(a.out) + at, a.vec_o, x);
+    else kv_store8(static_cast<__bf16*>(a.out) + at, a.vec_o, x);
 }
 __device__ inline void kv_out(const KvAttn& a, int64_t at, float x)
 {
@@ -99,7 +103,6 @@ __device__ inline void kv_out(const KvAttn& a, int64_t at, float x)
     else if (a.dtype == QE_F16) static_cast<_Float16*>(a.out)[at] = (_Float16)x;
     else static_cast<__bf16*>(a.out)[at] = (__bf16)x;
 }
-
 // Constants in registers: an instruction takes no two literals, and "and, or" is one instruction
 // with both of them in registers.
 struct KvBits {
@@ -184,8 +187,9 @@ template <int DP, int GROUP> struct KvTiles {
         return DP % 64 == 0 || kHalf ? u : min(u, DP / 4 - 1);   // (rows past the last unit give channels past DP)
     }
     static constexpr int group_of(int t) { return (kHalf ? 32 * t : 64 * t) / GROUP; }
-    __device__ static int channel(int t, int k, int row) { return kHalf ? 32 * t + 4 * (row & 7) + k + 2 * (row >> 3) : 64 * t + 4 * row + k; }
-    static constexpr bool kWhole = DP % 64 == 0 || kHalf;        // every channel() is below DP
+    // row r of unit tile t, class k is channel 64 t + 4 r + k; with groups of 32, 32 t + 4 (r & 7) + k + 2 (r >> 3)
+    static constexpr int kWidth = DP;
+    static constexpr bool kWhole = DP % 64 == 0 || kHalf;        // every one of them is below DP
 };
 
 // The zero points of a key row as the pairs kv_code_pair takes, and of two tokens' value words.
@@ -224,27 +228,65 @@ template <int NC, int NT, int PARTS> struct KvRows {
     __device__ void load(const KvAttn& a, const KvUnit& u, int row0)
     {
         const int i = threadIdx.x & 15, j = (threadIdx.x & 63) >> 4;
+        // all loads first (each with its conversion would wait for the one before)
+        constexpr int E = PARTS == 2 ? 4 : 2;                // bytes of a channel
+        u32x4 raw[NT][NC][E / 2];
+        int qi[NT], head[NT];
+        const char* at[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int row = row0 + 16 * n + i;
-            const bool have = row < u.rows;
-            const int qi = have ? row / u.per : 0, head = u.kvh * u.per + (have ? row - qi * u.per : 0);
+            const int row = min(row0 + 16 * n + i, u.rows - 1);
+            qi[n] = row / u.per;
+            head[n] = u.kvh * u.per + row - qi[n] * u.per;
+            at[n] = static_cast<const char*>(a.q) + ((u.first + qi[n]) * a.qt + head[n] * a.qh) * E;
+        }
+        if (a.vec_q) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int k = 0; k < NC; ++k)
+#pragma unroll
+                    for (int y = 0; y < E / 2; ++y)
+                        raw[n][k][y] = reinterpret_cast<const u32x4*>(at[n] + min(8 * (4 * k + j), a.c.dim - 8) * E)[y];
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int k = 0; k < NC; ++k)
+#pragma unroll
+                    for (int y = 0; y < E / 2; ++y)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const char* from = at[n] + min(8 * (4 * k + j), a.c.dim - 8) * E + 16 * y + 4 * w;
+                            if constexpr (PARTS == 2) raw[n][k][y][w] = *reinterpret_cast<const uint32_t*>(from);
+                            else raw[n][k][y][w] = *reinterpret_cast<const uint16_t*>(from) | (uint32_t)*reinterpret_cast<const uint16_t*>(from + 2) << 16;
+                        }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const bool have = row0 + 16 * n + i < u.rows;
             float x[NC][8], top = 0.f;
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
+                const bool in = have && 8 * (4 * k + j) < a.c.dim;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[k][e] = 0.f;
-                const int d = 8 * (4 * k + j);
-                if (have && d < a.c.dim) kv_q8(a, (u.first + qi) * a.qt + head * a.qh + d, x[k]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[k][e]));
+                for (int e = 0; e < 8; ++e) {
+                    float y;
+                    if constexpr (PARTS == 2) y = __uint_as_float(raw[n][k][e / 4][e % 4]);
+                    else {
+                        const uint32_t w = raw[n][k][0][e / 2];
+                        y = a.dtype == QE_BF16 ? __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) : (float)__builtin_bit_cast(f16x2, w)[e & 1];
+                    }
+                    x[k][e] = in ? y : 0.f;
+                    top = fmaxf(top, fabsf(x[k][e]));
+                }
             }
             top = kv_max4(top);
             // (a row of zeros, NaN or infinities keeps its values)
             const int e2 = top > 0.f && top <= 3.402823466e38f ? max(-100, min(100, 141 - (int)(__float_as_uint(top) >> 23))) : 0;
             const float mul = __uint_as_float((uint32_t)(127 + e2) << 23) * (a.scale < 0.f ? -1.f : 1.f);
             c[n] = fmaxf(fabsf(a.scale) * kLog2e * __uint_as_float((uint32_t)(127 - e2) << 23), 1e-37f);   // (0 times -inf)
-            slope[n] = a.slopes && have ? a.slopes[head] * kLog2e : 0.f;
+            slope[n] = a.slopes && have ? a.slopes[head[n]] * kLog2e : 0.f;
 #pragma unroll
             for (int k = 0; k < NC; ++k) {
                 uint32_t h[4], m[4];
@@ -259,7 +301,7 @@ template <int NC, int NT, int PARTS> struct KvRows {
                 q[0][n][k] = kv_frag(h[0], h[1], h[2], h[3]);
                 if constexpr (PARTS == 2) q[1][n][k] = kv_frag(m[0], m[1], m[2], m[3]);
             }
-            const int64_t pos = u.pos0 + qi;
+            const int64_t pos = u.pos0 + qi[n];
             hi[n] = have && a.causal ? (int)max((int64_t)0, pos + 1) : u.len;
             lo[n] = have && a.window ? (int)max((int64_t)0, pos - a.window + 1) : 0;
         }
@@ -279,7 +321,7 @@ template <int NC, int NT, int PARTS> struct KvRows {
     __device__ bool masked(int t0) const { return t0 > all_hi - kKvTok || t0 < all_lo; }
 };
 
-// The running softmax and the weighted sums of a wave's rows, o[t][k][n][e]: channel(t, k, 4 j + e).
+// The running softmax and the weighted sums of a wave's rows, o[t][k][n][e]: class k, row 4 j + e of tile t.
 // Probabilities are kept as p 2^shift, shift one number for all rows that brings the product with
 // the largest value scale so far to [2^10, 2^11): 2^15 at most, since p reaches 2^4 before the
 // maximum moves.  It drops out of o / mass.
@@ -418,6 +460,39 @@ template <int UT, int CL, int NT> struct KvSums {
             for (int k = 0; k < CL; ++k)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) asm("" : "+v"(o[t][k][n]));
+    }
+    // Calls f with the channel and the values of each octet of channels of tile n that ends up in this lane.
+    template <class T, class F> __device__ void octets(int n, F f)
+    {
+        const int j = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int t = 0; t < UT; ++t) {
+            float x[8];
+            if constexpr (T::kHalf) {
+                // rows 0 .. 7 (lanes j < 2) hold classes 0 and 1 of a unit, rows 8 .. 15 classes 2 and 3
+                const bool up = j >= 2;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float own = up ? o[t][k][n][2 + e] : o[t][k][n][e], give = up ? o[t][k][n][e] : o[t][k][n][2 + e];
+                        const float got = __shfl_xor(give, 32);
+                        x[4 * e + k] = up ? got : own;
+                        x[4 * e + 2 + k] = up ? own : got;
+                    }
+                f(32 * t + 16 * (j & 1) + (up ? 8 : 0), x);
+            } else {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[4 * e + k] = o[t][k][n][2 * y + e];
+                    const int d = 64 * t + 16 * j + 8 * y;
+                    if (T::kWhole || d < T::kWidth) f(d, x);
+                }
+            }
+        }
     }
     // after the last record: plain sums (odd classes were 16 times as large), the rows' masses.  What is
     // left of shift is a factor of both.
@@ -606,8 +681,9 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     sums.finish();
 
     // every wave to the common maximum (and shift), then sums over the waves
-    __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT];
-    __shared__ float acc[kKvWaves][16 * NT][DP + 1];
+    constexpr int kRow = DP + 4;                                 // floats of a row (16-byte aligned, spread over the banks)
+    __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT], rtop[16 * NT], rmass[16 * NT];
+    __shared__ __align__(16) float acc[kKvWaves][16 * NT][kRow];
     const float back = __builtin_amdgcn_exp2f(-sums.shift);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -618,42 +694,52 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        float m = wtop[0][16 * n + i];
+        float m = -kKvInf, l = 0.f;
 #pragma unroll
-        for (int w = 1; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][16 * n + i]);
-        const float f = m == sums.top[n] ? back : __builtin_amdgcn_exp2f(sums.top[n] - m) * back;
-#pragma unroll
-        for (int t = 0; t < UT; ++t)
-#pragma unroll
-            for (int k = 0; k < CL; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int d = T::channel(t, k, 4 * j + e);
-                    if (T::kWhole || d < DP) acc[wave][16 * n + i][d] = sums.o[t][k][n][e] * f;
-                }
-    }
-    __syncthreads();
-    for (int x = tid; x < 16 * NT * DP; x += 256) {
-        const int rr = x / DP, d = x - rr * DP, row = u.tile_row + rr;
-        if (row >= u.rows) break;
-        float m = -kKvInf, l = 0.f, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][rr]);
+        for (int w = 0; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][16 * n + i]);
 #pragma unroll
         for (int w = 0; w < kKvWaves; ++w) {
-            l += wtop[w][rr] == m ? wmass[w][rr] : wmass[w][rr] * __builtin_amdgcn_exp2f(wtop[w][rr] - m);
-            sum += acc[w][rr][d];
+            const float t = wtop[w][16 * n + i];
+            l = fmaf(t == m ? 1.f : __builtin_amdgcn_exp2f(t - m), wmass[w][16 * n + i], l);
         }
+        if (wave == 0 && j == 0) {
+            rtop[16 * n + i] = m;
+            rmass[16 * n + i] = l;
+        }
+        const float f = m == sums.top[n] ? back : __builtin_amdgcn_exp2f(sums.top[n] - m) * back;
+        sums.template octets<T>(n, [&](int d, const float* x) {
+#pragma unroll
+            for (int y = 0; y < 8; y += 4)
+                *reinterpret_cast<f32x4*>(&acc[wave][16 * n + i][d + y]) = f32x4{x[y] * f, x[y + 1] * f, x[y + 2] * f, x[y + 3] * f};
+        });
+    }
+    __syncthreads();
+    for (int x = tid; x < 16 * NT * (DP / 8); x += 256) {
+        const int rr = x / (DP / 8), d = 8 * (x - rr * (DP / 8)), row = u.tile_row + rr;
+        if (row >= u.rows) break;
+        f32x4 sum[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&acc[0][rr][d + 4 * y]), s1 = *reinterpret_cast<const f32x4*>(&acc[1][rr][d + 4 * y]);
+            const f32x4 s2 = *reinterpret_cast<const f32x4*>(&acc[2][rr][d + 4 * y]), s3 = *reinterpret_cast<const f32x4*>(&acc[3][rr][d + 4 * y]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[y][e] = (s0[e] + s1[e]) + (s2[e] + s3[e]);
+        }
+        const float m = rtop[rr], l = rmass[rr];
         if (u.splits > 1) {
             const int64_t slot = (unit * plan.nsplit + split) * plan.rows + rr;
-            plan.part[slot * DP + d] = sum;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) *reinterpret_cast<f32x4*>(plan.part + slot * DP + d + 4 * y) = sum[y];
             if (d == 0) {
                 plan.stat[2 * slot] = m;
                 plan.stat[2 * slot + 1] = l;
             }
         } else {
             const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
-            if (d < a.c.dim) kv_out(a, (u.first + qi) * a.ot + head * a.oh + d, l == 0.f ? 0.f : sum / l);
+            float out[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[e] = l == 0.f ? 0.f : sum[e >> 2][e & 3] / l;
+            if (d < a.c.dim) kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, out);
             if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
         }
     }
@@ -898,23 +984,21 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     const float back = __builtin_amdgcn_exp2f(-sums.shift);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int row = row0 + 16 * n + i;
-        if (row >= u.rows) continue;
-        const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
+        const int row = row0 + 16 * n + i, qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
         const int64_t slot = (unit * plan.nsplit + split) * plan.rows + (row - u.tile_row);
         const float f = u.splits > 1 ? back : sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n];
+        sums.template octets<T>(n, [&](int d, const float* x) {
+            float out[8];
 #pragma unroll
-        for (int t = 0; t < UT; ++t)
+            for (int e = 0; e < 8; ++e) out[e] = f == 0.f ? 0.f : x[e] * f;
+            if (row >= u.rows) return;
+            if (u.splits > 1) {
 #pragma unroll
-            for (int k = 0; k < CL; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int d = T::channel(t, k, 4 * j + e);
-                    if (u.splits > 1) {
-                        if (T::kWhole || d < DP) plan.part[slot * DP + d] = sums.o[t][k][n][e] * f;
-                    } else if (d < a.c.dim)
-                        kv_out(a, (u.first + qi) * a.ot + head * a.oh + d, sums.mass[n] == 0.f ? 0.f : sums.o[t][k][n][e] * f);
-                }
+                for (int y = 0; y < 8; y += 4) *reinterpret_cast<f32x4*>(plan.part + slot * DP + d + y) = f32x4{out[y], out[y + 1], out[y + 2], out[y + 3]};
+            } else if (d < a.c.dim)
+                kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, out);
+        });
+        if (row >= u.rows) continue;
         if (j == 0) {
             if (u.splits > 1) {
                 plan.stat[2 * slot] = sums.top[n];

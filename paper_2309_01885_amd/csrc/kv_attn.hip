@@ -69,6 +69,7 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     const int dp = kv_dp(a.c.dim);
     const size_t size = a.dtype == QE_F32 ? 4 : 2;
     a.vec_q = ((uintptr_t)a.q | (uint64_t)a.qt * size | (uint64_t)a.qh * size) % 16 == 0;
+    a.vec_o = ((uintptr_t)a.out | (uint64_t)a.ot * size | (uint64_t)a.oh * size) % 16 == 0;
     const Sizes z = sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.dtype == QE_F32);
     KvPlan plan{};
     plan.row_tiles = z.row_tiles;
