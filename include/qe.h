@@ -417,7 +417,8 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  * fp16 parts each), probabilities times value scales are rounded to fp16 (to 2^-11 of
  * themselves, or 2^-35 of the largest such product where that is more); statistics and
  * sums are fp32.
- * max_q: at least every nq.  Lengths past width * page, queries past `total` or max_q and
+ * max_q: at least every nq.  batch * kv_heads * (max_q * heads / kv_heads / 16 + 1) above 2^23 is
+ * QE_ERR_UNSUPPORTED.  Lengths past width * page, queries past `total` or max_q and
  * page numbers outside of the cache set QE_ERR_ARG in the workspace's status word (which
  * this call never clears; qe_sync_status does) and count as absent. */
 size_t qe_kv_attn_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads,

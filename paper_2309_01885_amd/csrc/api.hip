@@ -100,7 +100,7 @@ int dtype_bytes(int dtype) { return dtype == QE_F32 ? 4 : 2; }
 
 KvCache kv_cache(const void* pages, int64_t num_pages, int page, int kv_heads, int dim)
 {
-    return {static_cast<uint8_t*>(const_cast<void*>(pages)), num_pages * page, (uint32_t)(page / kKvTok), kv_heads, dim};
+    return {static_cast<uint8_t*>(const_cast<void*>(pages)), num_pages, num_pages * page, (uint32_t)(page / kKvTok), kv_heads, dim};
 }
 
 __global__ void status_copy_kernel(const int* from, int* to)
@@ -408,7 +408,9 @@ qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim
     if (total < 0 || total > 0x7fffffff || batch < 0 || batch > 0x7fffffff || max_q < 0 || width < 0) return QE_ERR_ARG;
     if (!std::isfinite(scale) || window < 0 || (!causal && (window || slopes))) return QE_ERR_ARG;
     if (!q_start && total != batch * max_q) return QE_ERR_ARG;
-    if (std::min(max_q, total) * (heads / kv_heads) > 0x7fffffff - 1024) return QE_ERR_ARG;   // query rows of a sequence and key head
+    // (tiles of 16 query rows are counted in 32 bits, and a launch takes 2^24 workgroups of 256 threads)
+    const int64_t rows = std::min(max_q, total) * (heads / kv_heads);
+    if (rows > (int64_t(1) << 30) || batch * kv_heads > (int64_t(1) << 23) / (rows / 16 + 1)) return QE_ERR_UNSUPPORTED;
     if (total == 0 || batch == 0 || max_q == 0) return QE_OK;
     if (!Q || !pages || !lengths || !out || (width > 0 && !table) || misaligned(pages, 16)) return QE_ERR_ARG;
     if (misaligned(Q, dtype_bytes(dtype)) || misaligned(out, dtype_bytes(dtype))) return QE_ERR_ARG;

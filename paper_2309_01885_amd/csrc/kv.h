@@ -34,7 +34,7 @@ inline int64_t kv_record_bytes(int dp, int group) { return kKvTok * (int64_t)(dp
 
 struct KvCache {
     uint8_t* pages;
-    int64_t slots;        // num_pages * page
+    int64_t pages_count, slots;          // slots: pages_count * page
     uint32_t per;         // records of a page
     int heads, dim;
 };

@@ -30,33 +30,41 @@ constexpr float kLog2e = 1.44269504088896341f;
 // nsplit workgroups along the tokens, whose results kv_join_kernel joins.
 struct KvPlan {
     int64_t row_tiles, units;               // units of a sequence and key head; of the call
-    int nsplit, rows;
+    int nsplit, rows, rows_log2, per;       // per: heads of a key head
     float* part;                            // nsplit > 1: (unit, split, row, DP) sums relative to the maximum
     float* stat;                            // (unit, split, row, 2): maximum (log2) and mass
 };
 
 // What a workgroup works on; the join recomputes it.
 struct KvUnit {
-    int64_t unit, first, pos0;              // first row of Q, position of query 0
+    int64_t first, pos0;                    // first row of Q, position of query 0
     int b, kvh, per, tile_row, rows;        // per: heads of a key head; the unit's first row; rows of the sequence
-    int len, nq, rec0, rec1, splits;        // cached tokens, queries; records that some row sees; splits in use
+    int len, rec0, rec1, splits;            // cached tokens; records that some row sees; splits in use
+
+    // records [from(s), from(s + 1)) are split s's
+    __device__ int from(int split) const
+    {
+        const uint32_t n = rec1 - rec0, q = n / (uint32_t)splits;
+        return rec0 + (int)(q * split + min((uint32_t)split, n - q * splits));
+    }
 };
 
 // Records a split has at least (a workgroup's waves take them in turn), and from which splitting gains
 // more than the join costs (a record takes a wave about 1.3 us, the join with its launch 6 us).
-constexpr int kKvMinRecords = 4, kKvSplitFrom = 24;
+constexpr int kKvMinRecords = 4, kKvSplitFrom = 20;
 
 // A value that is the same for the whole workgroup and not written by the kernel: a scalar load.
 __device__ inline int kv_scalar(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)p; }
 
-__device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit, bool report)
+// (Divisions are of 32 bits: units and the rows of a sequence are fewer than 2^31, checked on the
+// host, and one of 64 bits takes 130 instructions.)
+__device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, uint32_t unit, bool report)
 {
     KvUnit u;
-    const int64_t bh = unit / p.row_tiles, tile = unit - bh * p.row_tiles;
-    u.unit = unit;
-    u.b = (int)(bh / a.c.heads);
-    u.kvh = (int)(bh - (int64_t)u.b * a.c.heads);
-    u.per = a.heads / a.c.heads;
+    const uint32_t bh = unit / (uint32_t)p.row_tiles, tile = unit - bh * (uint32_t)p.row_tiles;
+    u.b = (int)(bh / (uint32_t)a.c.heads);
+    u.kvh = (int)(bh - (uint32_t)u.b * a.c.heads);
+    u.per = p.per;
     bool bad = false;
     u.first = u.b * a.max_q;
     int64_t nq = a.max_q;
@@ -73,16 +81,16 @@ __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, int64_t unit,
     len = len < 0 ? 0 : min(len, room);
     if (bad && report && tile == 0 && u.kvh == 0) set_status(a.status, QE_ERR_ARG);
     u.len = (int)len;
-    u.nq = (int)nq;
     u.pos0 = len - nq;
-    const int64_t r0 = tile * p.rows, rows = nq * u.per;
-    u.tile_row = (int)min(r0, rows);        // (rows of a sequence: below 2^31, checked on the host)
-    u.rows = (int)rows;
+    u.rows = (int)(nq * u.per);
+    const int64_t r0 = (int64_t)tile * p.rows;
+    u.tile_row = (int)min(r0, (int64_t)u.rows);
     // the unit's queries i0 .. i1
-    const int64_t i0 = r0 / u.per, i1 = min(nq, (r0 + p.rows + u.per - 1) / u.per) - 1;
+    const uint32_t i0 = (uint32_t)u.tile_row / (uint32_t)u.per;
+    const int64_t i1 = min(nq, (int64_t)(((uint32_t)u.tile_row + p.rows + u.per - 1) / (uint32_t)u.per)) - 1;
     int64_t end = a.causal ? min(len, u.pos0 + i1 + 1) : len;
     const int64_t begin = a.window ? max((int64_t)0, u.pos0 + i0 - a.window + 1) : 0;
-    if (r0 >= rows || end < begin) end = begin;
+    if (r0 >= u.rows || end < begin) end = begin;
     u.rec0 = (int)(begin / kKvTok);
     u.rec1 = end > begin ? (int)((end + kKvTok - 1) / kKvTok) : u.rec0;
     const int records = u.rec1 - u.rec0;
@@ -266,21 +274,20 @@ template <int NC, int NT, int PARTS> struct KvRows {
         for (int n = 0; n < NT; ++n) {
             const bool have = row0 + 16 * n + i < u.rows;
             float x[NC][8], top = 0.f;
+            auto take = [&](auto channel) {
 #pragma unroll
-            for (int k = 0; k < NC; ++k) {
-                const bool in = have && 8 * (4 * k + j) < a.c.dim;
+                for (int k = 0; k < NC; ++k) {
+                    const bool in = have && 8 * (4 * k + j) < a.c.dim;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float y;
-                    if constexpr (PARTS == 2) y = __uint_as_float(raw[n][k][e / 4][e % 4]);
-                    else {
-                        const uint32_t w = raw[n][k][0][e / 2];
-                        y = a.dtype == QE_BF16 ? __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) : (float)__builtin_bit_cast(f16x2, w)[e & 1];
+                    for (int e = 0; e < 8; ++e) {
+                        x[k][e] = in ? channel(k, e) : 0.f;
+                        top = fmaxf(top, fabsf(x[k][e]));
                     }
-                    x[k][e] = in ? y : 0.f;
-                    top = fmaxf(top, fabsf(x[k][e]));
                 }
-            }
+            };
+            if constexpr (PARTS == 2) take([&](int k, int e) { return __uint_as_float(raw[n][k][e / 4][e % 4]); });
+            else if (a.dtype == QE_BF16) take([&](int k, int e) { return __uint_as_float(e & 1 ? raw[n][k][0][e / 2] & 0xffff0000u : raw[n][k][0][e / 2] << 16); });
+            else take([&](int k, int e) { return (float)__builtin_bit_cast(f16x2, (uint32_t)raw[n][k][0][e / 2])[e & 1]; });
             top = kv_max4(top);
             // (a row of zeros, NaN or infinities keeps its values)
             const int e2 = top > 0.f && top <= 3.402823466e38f ? max(-100, min(100, 141 - (int)(__float_as_uint(top) >> 23))) : 0;
@@ -527,26 +534,23 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     using R = KvRec<DP, GROUP>;
     using T = KvTiles<DP, GROUP>;
     constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
-    const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t unit = wg / plan.nsplit;
-    const int split = (int)(wg - unit * plan.nsplit);
-    if (unit >= plan.units) return;
+    const uint32_t unit = blockIdx.x / (uint32_t)plan.nsplit;
+    const int split = (int)(blockIdx.x - unit * plan.nsplit);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i = tid & 15, j = (tid & 63) >> 4;
     const KvUnit u = kv_unit(a, plan, unit, tid == 0 && split == 0);
     if (split >= u.splits || u.tile_row >= u.rows) return;
-    const int count = u.rec1 - u.rec0;
-    const int r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
-    int r = u.rec0 + (int)((int64_t)count * split / u.splits) + wave;
+    const int r1 = u.from(split + 1);
+    int r = u.from(split) + wave;
 
     // A record's words.  The keys' registers are free once the scores are there and take the next
     // record's keys; the values' likewise after the weighted sum.
     const KvBits bits;
     uint32_t k[2][NC], kw[NG][8], kz[2][NG], v[UT][4], vw[NG][8];
-    const int64_t pages = a.c.slots / ((int64_t)a.c.per * kKvTok);
+    const int64_t pages = a.c.pages_count;
     const int32_t* table = a.table + u.b * a.width;
     const int per = (int)a.c.per;
-    int pg = r / per, rem = r - pg * per;
+    int pg = (uint32_t)r / (uint32_t)per, rem = r - pg * per;
     int id = r < r1 ? table[pg] : 0;
     const uint8_t* rec = a.c.pages;
     bool here = false;                                           // whether the record is there (else any other is read, and not used)
@@ -727,7 +731,7 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
         }
         const float m = rtop[rr], l = rmass[rr];
         if (u.splits > 1) {
-            const int64_t slot = (unit * plan.nsplit + split) * plan.rows + rr;
+            const int64_t slot = ((int64_t)unit * plan.nsplit + split) * plan.rows + rr;
 #pragma unroll
             for (int y = 0; y < 2; ++y) *reinterpret_cast<f32x4*>(plan.part + slot * DP + d + 4 * y) = sum[y];
             if (d == 0) {
@@ -772,18 +776,15 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     __shared__ Stage stage[2];
     // workgroups of an XCD (every eighth) get a contiguous stretch of units: rows of the same keys
     // share its L2
-    const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t total = plan.units * plan.nsplit, q8 = total / 8, r8 = total % 8, x8 = wg & 7;
-    if (wg >= total) return;
-    const int64_t mine = x8 * q8 + (x8 < r8 ? x8 : r8) + (wg >> 3);
-    const int64_t unit = mine / plan.nsplit;
+    const uint32_t wg = blockIdx.x, q8 = gridDim.x / 8, r8 = gridDim.x % 8, x8 = wg & 7;
+    const uint32_t mine = x8 * q8 + min(x8, r8) + (wg >> 3);
+    const uint32_t unit = mine / (uint32_t)plan.nsplit;
     const int split = (int)(mine - unit * plan.nsplit);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int i = tid & 15, j = lane >> 4;
     const KvUnit u = kv_unit(a, plan, unit, tid == 0 && split == 0);
     if (split >= u.splits || u.tile_row >= u.rows) return;
-    const int count = u.rec1 - u.rec0;
-    const int r0 = u.rec0 + (int)((int64_t)count * split / u.splits), r1 = u.rec0 + (int)((int64_t)count * (split + 1) / u.splits);
+    const int r0 = u.from(split), r1 = u.from(split + 1);
     const int row0 = u.tile_row + wave * (16 * NT);
 
     // what the wave converts: of record `part` of a stage, key half kh from channel block kc on, value
@@ -797,11 +798,11 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     const int token = T::key_token(i, kh);
     uint32_t k[CW], kz[NG], v[VW][4], vw[NG][8], word[SW];
 
-    const int64_t pages = a.c.slots / ((int64_t)a.c.per * kKvTok);
+    const int64_t pages = a.c.pages_count;
     const int32_t* table = a.table + u.b * a.width;
     const int per = (int)a.c.per;
     // the wave's record of the next stage to be loaded, its page's place in the table and its place in the page
-    int next = min(r0 + part, r1 - 1), pg = next / per, rem = next - pg * per;
+    int next = max(0, min(r0 + part, r1 - 1)), pg = (uint32_t)next / (uint32_t)per, rem = next - pg * per;
     int id = r0 < r1 ? table[pg] : 0;
     bool here = false;                                           // whether the record is there (else any other is read, and not used)
     // Starts the loads of the wave's share of the next stage, whose page number was read before, and reads
@@ -985,7 +986,7 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = row0 + 16 * n + i, qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
-        const int64_t slot = (unit * plan.nsplit + split) * plan.rows + (row - u.tile_row);
+        const int64_t slot = ((int64_t)unit * plan.nsplit + split) * plan.rows + (row - u.tile_row);
         const float f = u.splits > 1 ? back : sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n];
         sums.template octets<T>(n, [&](int d, const float* x) {
             float out[8];
@@ -1017,13 +1018,14 @@ template <int DP, bool ONE> __global__ __launch_bounds__(256) void kv_join_kerne
     __shared__ float sum[kKvWaves][DP], mass[kKvWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (ONE ? 1 : kKvWaves) + (ONE ? 0 : wave);
-    const int64_t unit = at / plan.rows;
-    const int rr = (int)(at - unit * plan.rows);
-    if (unit >= plan.units) return;
+    if (at >= plan.units * plan.rows) return;
+    // (plan.rows is a power of two)
+    const uint32_t unit = (uint32_t)(at >> plan.rows_log2);
+    const int rr = (int)(at & (plan.rows - 1));
     const KvUnit u = kv_unit(a, plan, unit, false);
     const int row = u.tile_row + rr;
     if (u.splits <= 1 || row >= u.rows) return;
-    const int64_t slot = unit * plan.nsplit * plan.rows + rr;
+    const int64_t slot = (int64_t)unit * plan.nsplit * plan.rows + rr;
     float m = -kKvInf;
     for (int s = lane; s < u.splits; s += 64) m = fmaxf(m, plan.stat[2 * (slot + (int64_t)s * plan.rows)]);
 #pragma unroll

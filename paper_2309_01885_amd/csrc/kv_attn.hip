@@ -74,13 +74,15 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     KvPlan plan{};
     plan.row_tiles = z.row_tiles;
     plan.units = z.units;
+    plan.per = a.heads / a.c.heads;
+    plan.rows_log2 = __builtin_ctz((unsigned)z.rows);
     plan.rows = z.rows;
     int64_t records = a.width * a.c.per;
     if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
     plan.nsplit = splits_of(z.form.many, z.units, records);
     plan.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes);
     plan.stat = reinterpret_cast<float*>(reinterpret_cast<char*>(plan.part) + align256(part_floats(z, dp, plan.nsplit) * 4));
-    const dim3 grid = grid_xy(z.units * plan.nsplit, 256);
+    const dim3 grid((unsigned)(z.units * plan.nsplit));
     switch (dp) {
         case 64: kv_attn_width<64>(a, plan, z.form, grid, s); break;
         case 96: kv_attn_width<96>(a, plan, z.form, grid, s); break;
