@@ -378,12 +378,52 @@ template <int UT, int CL, int NT> struct KvSums {
                     for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
         }
     }
-    // s: the products times their key scales, of KR records that start at tokens t0; on return p 2^shift
-    // (0 where the row sees nothing).  masked: some row does not see all of them.  big: the lane's
-    // largest value scale.
-    template <int KR, int NC, int PARTS>
-    __device__ void weigh(float (&s)[KR][NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, const int (&t0)[KR], bool masked, float big)
+    // Where some row does not see a token (its score s is -inf), a NaN scale of that token would meet a
+    // probability of 0.  NaN scales become 0, and the sums of the rows and groups that see one NaN.
+    template <class T, int KR, int NG> __device__ void clear_nans(const float (&s)[KR][NT][8], float (&sv)[KR][NG][8])
     {
+        float x = 0.f;
+#pragma unroll
+        for (int y = 0; y < KR; ++y)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x += sv[y][g][e];
+        if (!__any(x != x)) return;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float met = 0.f;
+#pragma unroll
+                for (int y = 0; y < KR; ++y)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) met = s[y][n][e] != -kKvInf && sv[y][g][e] != sv[y][g][e] ? 1.f : met;
+                const float add = kv_max4(met) == 0.f ? 0.f : __builtin_nanf("");
+#pragma unroll
+                for (int t = 0; t < UT; ++t)
+                    if (T::group_of(t) == g)
+#pragma unroll
+                        for (int k = 0; k < CL; ++k)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[t][k][n][e] += add;
+            }
+#pragma unroll
+            for (int y = 0; y < KR; ++y)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sv[y][g][e] = sv[y][g][e] != sv[y][g][e] ? 0.f : sv[y][g][e];
+        }
+    }
+    // s: the products times their key scales, of KR records that start at tokens t0; on return p 2^shift
+    // (0 where the row sees nothing).  masked: some row does not see all of them.  sv: the value scales.
+    template <class T, int KR, int NG, int NC, int PARTS>
+    __device__ void weigh(float (&s)[KR][NT][8], float (&sv)[KR][NG][8], const KvRows<NC, NT, PARTS>& r, bool slopes, const int (&t0)[KR], bool masked)
+    {
+        float big = 0.f;
+#pragma unroll
+        for (int y = 0; y < KR; ++y)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) big = fmaxf(big, kv_max8(sv[y][g]));
         float at[NT], c[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -410,6 +450,7 @@ template <int UT, int CL, int NT> struct KvSums {
                 }
                 c[n] = 1.f;
             }
+            clear_nans<T>(s, sv);
         }
         move(at, big);
 #pragma unroll
@@ -424,20 +465,15 @@ template <int UT, int CL, int NT> struct KvSums {
             }
         }
     }
-    // The products' fp16 weights p s' of a group.  unseen: a token that some row does not see may have
-    // a NaN scale, and 0 is to stay 0.
-    template <int PARTS> __device__ static void weights(const float (&s)[NT][8], const float (&sv)[8], bool unseen, f16x8 (&pr)[PARTS][NT])
+    // The products' fp16 weights p s' of a group.
+    template <int PARTS> __device__ static void weights(const float (&s)[NT][8], const float (&sv)[8], f16x8 (&pr)[PARTS][NT])
     {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             uint32_t h[4], m[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
-                if (unseen) {
-                    x0 = s[n][2 * p] == 0.f ? 0.f : x0;
-                    x1 = s[n][2 * p + 1] == 0.f ? 0.f : x1;
-                }
+                const float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
                 h[p] = kv_pack(x0, x1);
                 if constexpr (PARTS == 2) {
                     const f16x2 hv = __builtin_bit_cast(f16x2, h[p]);
@@ -447,16 +483,6 @@ template <int UT, int CL, int NT> struct KvSums {
             pr[0][n] = kv_frag(h[0], h[1], h[2], h[3]);
             if constexpr (PARTS == 2) pr[1][n] = kv_frag(m[0], m[1], m[2], m[3]);
         }
-    }
-    // Whether a scale of the lane's tokens is a NaN.
-    template <int NG> __device__ static bool has_nan(const float (&sv)[NG][8])
-    {
-        float x = 0.f;
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x += sv[g][e];
-        return __any(x != x);
     }
     // Keeps every sum in one place from record to record (the compiler copied half of them otherwise).
     __device__ void pin()
@@ -642,21 +668,17 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
 #pragma unroll
                 for (int g = 0; g < NG; ++g) vw[g][e] = t0 + 8 * j + e < u.len ? vw[g][e] : 0u;
         }
-        float sv[NG][8], big = 0.f;
+        float sv[1][NG][8];
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sv[g][e] = kv_scale(vw[g][e]);
-            big = fmaxf(big, kv_max8(sv[g]));
-        }
+            for (int e = 0; e < 8; ++e) sv[0][g][e] = kv_scale(vw[g][e]);
         const int at[1] = {t0};
-        sums.weigh(s, rows, a.slopes != nullptr, at, masked, big);
-        const bool unseen = masked && sums.has_nan(sv);
+        sums.template weigh<T>(s, sv, rows, a.slopes != nullptr, at, masked);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             f16x8 pr[PARTS][NT];
-            if (unseen) sums.template weights<PARTS>(s[0], sv[g], true, pr);
-            else sums.template weights<PARTS>(s[0], sv[g], false, pr);
+            sums.template weights<PARTS>(s[0], sv[0][g], pr);
             uint32_t lo[4], hi[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) kv_value_zero(vw[g][2 * p], vw[g][2 * p + 1], lo[p], hi[p], bits);
@@ -768,9 +790,10 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     constexpr int CW = KR == 2 ? NC : (NC + 1) / 2;              // key products a wave converts
     constexpr int VW = T::kHalf ? (UT + 1) / 2 : UT, VK = KR;    // unit tiles and classes
     constexpr int SW = KR == 2 ? (NG + 1) / 2 : (NG + 3) / 4;    // scales a lane converts
+    constexpr int SG = SW * (KR == 2 ? 2 : 4);
     struct Stage {
         f16x8 k[KR][2][NC][64], v[KR][UT][CL][64];
-        float ks[KR][NG][kKvTok], vs[KR][NG][kKvTok];
+        float ks[KR][SG][kKvTok], vs[KR][SG][kKvTok];            // (groups past NG: what lanes without a group write)
         int at[KR];                                              // the records' first tokens
     };
     __shared__ Stage stage[2];
@@ -887,11 +910,11 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             const int g = KR == 2 ? (lane >> 5) + 2 * x : q + 4 * x;
             float sc = kv_scale(word[x]);
             // (words past the sequence's end are anything: no scale of theirs may meet a 0)
-            if (!key && (r + part) * kKvTok + (lane & 31) >= u.len) sc = 0.f;
-            if (g < NG) (key ? st.ks : st.vs)[part][g][lane & 31] = sc;
+            sc = !key && (r + part) * kKvTok + (lane & 31) >= u.len ? 0.f : sc;
+            (key ? st.ks : st.vs)[part][g][lane & 31] = sc;
         }
         // (past the last record, or on a page that is not there: past every sequence's end)
-        if (q == 0 && lane == 0) st.at[part] = here && r + part < r1 ? (r + part) * kKvTok : 0x7fffff00;
+        st.at[part] = here && r + part < r1 ? (r + part) * kKvTok : 0x7fffff00;
     };
 
     KvRows<NC, NT, PARTS> rows;
@@ -942,7 +965,7 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             }
         }
         start();
-        float big = 0.f, sv[KR][NG][8];
+        float sv[KR][NG][8];
 #pragma unroll
         for (int y = 0; y < KR; ++y)
 #pragma unroll
@@ -950,20 +973,14 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
                 const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.vs[y][g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.vs[y][g][8 * j + 4]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sv[y][g][e] = e < 4 ? s0[e] : s1[e - 4];
-                big = fmaxf(big, kv_max8(sv[y][g]));
             }
-        sums.weigh(s, rows, a.slopes != nullptr, t0, masked, big);
-        bool unseen = false;
-        if (masked)
-#pragma unroll
-            for (int y = 0; y < KR; ++y) unseen = unseen || sums.has_nan(sv[y]);
+        sums.template weigh<T>(s, sv, rows, a.slopes != nullptr, t0, masked);
 #pragma unroll
         for (int y = 0; y < KR; ++y)
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 f16x8 pr[PARTS][NT];
-                if (unseen) sums.template weights<PARTS>(s[y], sv[y][g], true, pr);
-                else sums.template weights<PARTS>(s[y], sv[y][g], false, pr);
+                sums.template weights<PARTS>(s[y], sv[y][g], pr);
 #pragma unroll
                 for (int t = 0; t < UT; ++t) {
                     if (T::group_of(t) != g) continue;
