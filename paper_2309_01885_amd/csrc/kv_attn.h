@@ -569,10 +569,24 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     const int r1 = u.from(split + 1);
     int r = u.from(split) + wave;
 
-    // A record's words.  The keys' registers are free once the scores are there and take the next
-    // record's keys; the values' likewise after the weighted sum.
+    // A record's codes, and a word of each group: a key's (lanes 0 .. 31) or a value's.  The keys' registers
+    // are free once the scores are there and take the next record's keys; the values' likewise after
+    // the weighted sum.  The words' scales and zero points reach the lanes that need them through the
+    // wave's part of LDS.  (Read from memory by each of those lanes they took 18 registers a group and
+    // 32 more instructions.)
+    struct Words {
+        float s[NG][64];                                         // scales
+        uint16_t lo[NG][64], hi[NG][64];                         // -(1024 + z), -(1024 + 16 z) in fp16
+    };
+    constexpr int kRow = DP + 4;                                 // floats of a row (16-byte aligned, spread over the banks)
+    __shared__ __align__(16) union {
+        Words words[kKvWaves];
+        float acc[kKvWaves][16 * NT][kRow];
+    } shared;
+    Words& held = shared.words[wave];
+    const int lane = tid & 63;
     const KvBits bits;
-    uint32_t k[2][NC], kw[NG][8], kz[2][NG], v[UT][4], vw[NG][8];
+    uint32_t k[2][NC], v[UT][4], word[NG];
     const int64_t pages = a.c.pages_count;
     const int32_t* table = a.table + u.b * a.width;
     const int per = (int)a.c.per;
@@ -598,21 +612,28 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     };
     auto keys = [&] {
 #pragma unroll
+        for (int g = 0; g < NG; ++g)
+            word[g] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)((lane < 32 ? R::kKeyWords : R::kValWords) + g * (4 * kKvTok) + 4 * (lane & 31)));
+#pragma unroll
         for (int h = 0; h < 2; ++h) kv_words<NC>(rec + (uint32_t)(T::key_token(i, h) * R::kKeyRow + j * (4 * NC)), k[h]);
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            const uint32_t kp = R::kKeyWords + g * (4 * kKvTok);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) kz[h][g] = *reinterpret_cast<const uint32_t*>(rec + (kp + 4 * T::key_token(i, h)));
-            kv_words<8>(rec + (kp + 32 * j), kw[g]);
-        }
     };
     auto values = [&] {
 #pragma unroll
-        for (int g = 0; g < NG; ++g) kv_words<8>(rec + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), vw[g]);
-#pragma unroll
         for (int t = 0; t < UT; ++t) kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(t, i) * (2 * kKvTok) + 16 * j), v[t]);
     };
+    // (LDS serves a wave in order: what was read before is not overwritten.)
+    auto hold = [&](int t0) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            // words past the sequence's end are anything: no value scale of theirs may meet a 0
+            held.s[g][lane] = lane >= 32 && t0 > u.len - 1 - (lane & 31) ? 0.f : kv_scale(word[g]);
+            held.lo[g][lane] = (uint16_t)(0xE400u | (word[g] & 15u));
+            held.hi[g][lane] = (uint16_t)(0xE400u | (word[g] & 15u) << 4);
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+    auto first_token = [&](int r) { return here ? r * kKvTok : 0x7fffff00; };    // (of no record: past every sequence's end)
     if (r < r1) {
         find(r);
         keys();
@@ -623,9 +644,11 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     KvSums<UT, CL, NT> sums;
     sums.clear();
 
+    int t0 = first_token(r);
+    if (r < r1) hold(t0);
     for (; r < r1; r += kKvWaves) {
-        const int t0 = here ? r * kKvTok : 0x7fffff00;           // (past every sequence's end)
         const bool masked = rows.masked(t0), more = r + kKvWaves < r1;
+        const int at[1] = {t0};
         float s[1][NT][8];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -636,8 +659,7 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
                 for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                uint32_t lo, hi;
-                kv_key_zero(kz[h][g], lo, hi, bits);
+                const uint32_t l = held.lo[g][T::key_token(i, h)], x = held.hi[g][T::key_token(i, h)], lo = l << 16 | l, hi = x << 16 | x;
 #pragma unroll
                 for (int c = g * T::CPG; c < (g + 1) * T::CPG && c < NC; ++c) {
                     const f16x8 f = kv_key_frag(k[h][c], lo, hi, bits);
@@ -647,9 +669,10 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
                         for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][c], acc[n][h]);
                 }
             }
+            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&held.s[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&held.s[g][8 * j + 4]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float sc = kv_scale(kw[g][e]);
+                const float sc = e < 4 ? s0[e] : s1[e - 4];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float x = acc[n][e >> 2][e & 3];
@@ -661,27 +684,19 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
             find(r + kKvWaves);
             keys();
         }
-        if (t0 > u.len - kKvTok) {
-            // words past the sequence's end are anything: no scale of theirs may meet a 0
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int g = 0; g < NG; ++g) vw[g][e] = t0 + 8 * j + e < u.len ? vw[g][e] : 0u;
-        }
         float sv[1][NG][8];
 #pragma unroll
-        for (int g = 0; g < NG; ++g)
+        for (int g = 0; g < NG; ++g) {
+            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&held.s[g][32 + 8 * j]), s1 = *reinterpret_cast<const f32x4*>(&held.s[g][36 + 8 * j]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sv[0][g][e] = kv_scale(vw[g][e]);
-        const int at[1] = {t0};
+            for (int e = 0; e < 8; ++e) sv[0][g][e] = e < 4 ? s0[e] : s1[e - 4];
+        }
         sums.template weigh<T>(s, sv, rows, a.slopes != nullptr, at, masked);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             f16x8 pr[PARTS][NT];
             sums.template weights<PARTS>(s[0], sv[0][g], pr);
-            uint32_t lo[4], hi[4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) kv_value_zero(vw[g][2 * p], vw[g][2 * p + 1], lo[p], hi[p], bits);
+            const u32x4 lo = *reinterpret_cast<const u32x4*>(&held.lo[g][32 + 8 * j]), hi = *reinterpret_cast<const u32x4*>(&held.hi[g][32 + 8 * j]);
 #pragma unroll
             for (int t = 0; t < UT; ++t) {
                 if (T::group_of(t) != g) continue;
@@ -701,15 +716,18 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
                 }
             }
         }
-        if (more) values();
+        if (more) {
+            values();
+            t0 = first_token(r + kKvWaves);
+            hold(t0);
+        }
         sums.pin();
     }
     sums.finish();
 
     // every wave to the common maximum (and shift), then sums over the waves
-    constexpr int kRow = DP + 4;                                 // floats of a row (16-byte aligned, spread over the banks)
     __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT], rtop[16 * NT], rmass[16 * NT];
-    __shared__ __align__(16) float acc[kKvWaves][16 * NT][kRow];
+    auto& acc = shared.acc;                                      // (written after a barrier that ends the use of the words)
     const float back = __builtin_amdgcn_exp2f(-sums.shift);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
