@@ -350,7 +350,8 @@ qe_status qe_outliers_csr(const float* H, int64_t q, int64_t p, const int64_t* s
  * Grid.  The dim channels of a token's key (or value) in one head are cut into
  * groups of `group` consecutive channels.  A group x gets, in fp32,
  *   lo = min(0, min x), hi = max(0, max x),
- *   s = max((hi - lo) / 15, 2^-126), its bit pattern rounded to a multiple of 16,
+ *   s = max((hi - lo) * r, 2^-126), r = 1 / 15 rounded, its bit pattern rounded to a
+ *   multiple of 16,
  *   z = rint(-lo * (1 / s)),  n = clamp(rint(x * (1 / s)) + z, 0, 15),
  * and is held as the codes n and one word, the bit pattern of s with z in its low
  * four bits; it stands for s (n - z), each element within s / 2 of x (up to rounding).  A

@@ -24,7 +24,7 @@ def quantize_group(x):
         span = F(hi - lo)
         if not np.all(np.isfinite(x)) or not np.isfinite(span):
             return np.zeros(x.size, np.uint8), np.uint32(0x7fc00000), 0
-        s = np.maximum(F(span / F(15)), F(2.0 ** -126))
+        s = np.maximum(F(span * F(1 / 15)), F(2.0 ** -126))
         bits = np.uint32((int(s.view(np.uint32)) + 8) // 16 * 16)
         inv = F(F(1) / bits.view(F))
         z = np.clip(np.rint(F(-lo * inv)), 0, 15)

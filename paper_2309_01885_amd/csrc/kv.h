@@ -8,6 +8,7 @@ namespace qe {
 
 constexpr int kKvTok = 32;            // tokens of a record
 constexpr float kKvMinScale = 1.17549435e-38f;   // 2^-126
+constexpr float kKvFifteenth = 1.f / 15.f;       // (rounded)
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

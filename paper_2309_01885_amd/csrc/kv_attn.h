@@ -473,7 +473,10 @@ template <int UT, int CL, int NT> struct KvSums {
             uint32_t h[4], m[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                const float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
+                float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
+                // (one rounded product for both parts: fused into the first part's conversion only, it made
+                // the parts miss each other by a step of fp16 once in some thousand)
+                if (PARTS == 2) asm("" : "+v"(x0), "+v"(x1));
                 h[p] = kv_pack(x0, x1);
                 if constexpr (PARTS == 2) {
                     const f16x2 hv = __builtin_bit_cast(f16x2, h[p]);
@@ -550,10 +553,11 @@ __device__ inline float kv_lse(float top, float mass) { return mass == 0.f ? -kK
 // Workgroups of a CU that the registers are to allow.
 constexpr int kv_few_occupancy(int dp, int group, int nt, int parts)
 {
-    return dp <= 128 && group > 32 && nt == 1 ? 3 : dp == 64 && group > 32 ? 3 : 2;
+    if (dp == 64) return nt == 1 ? 4 : 3;
+    if (dp <= 128 && nt == 1) return group == 128 && parts == 1 ? 4 : group >= 64 ? 3 : 2;
+    return 2;
 }
-// A workgroup's waves share the rows of a unit (16 NT) and take its records in turn, each on its
-// own; at the end they are joined through LDS.
+
 template <int DP, int GROUP, int NT, int PARTS>
 __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void kv_few_kernel(KvAttn a, KvPlan plan)
 {

@@ -12,9 +12,10 @@ extern template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, di
 namespace {
 
 constexpr int64_t kManyFrom = 128;  // query rows of a sequence and key head from which waves have rows of their own
-// Workgroups that fill the chip once: three of a CU with few rows (rounds more than one help only
-// where the sequences' lengths differ), two with many.
-constexpr int64_t kFillMany = 512, kFillFew = 768;
+// Workgroups that fill the chip: two of a CU with many rows, three with few.  Twice as many where there
+// are enough sequences for their lengths to differ: the long ones are not left to the end (64
+// sequences of 2048 to 8192 tokens 89 -> 86 us; two of the same length 111 -> 117).
+constexpr int64_t kFillMany = 512, kFillFew = 768, kUneven = 8;
 
 KvForm form_of(int64_t rows, int dp, bool f32)
 {
@@ -23,10 +24,11 @@ KvForm form_of(int64_t rows, int dp, bool f32)
 }
 
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
-int splits_of(bool many, int64_t units, int64_t records)
+int splits_of(bool many, int64_t units, int64_t batch, int64_t records)
 {
     if (records < kKvSplitFrom) return 1;
-    return (int)std::max<int64_t>(1, std::min((many ? kFillMany : kFillFew) / std::max<int64_t>(units, 1), records / kKvMinRecords));
+    const int64_t fill = many ? kFillMany : batch < kUneven ? kFillFew : 2 * kFillFew;
+    return (int)std::max<int64_t>(1, std::min(fill / std::max<int64_t>(units, 1), records / kKvMinRecords));
 }
 
 struct Sizes {
@@ -56,7 +58,7 @@ size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, i
     size_t need = 0;
     for (int f32 = 0; f32 < 2; ++f32) {
         const Sizes z = sizes_of(batch, max_q, heads, kv_heads, dim, f32 != 0);
-        const int nsplit = splits_of(z.form.many, z.units, INT32_MAX);
+        const int nsplit = splits_of(z.form.many, z.units, batch, INT32_MAX);
         if (nsplit > 1)
             need = std::max(need, align256(part_floats(z, kv_dp(dim), nsplit) * 4) + align256(stat_floats(z, nsplit) * 4));
     }
@@ -79,7 +81,7 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     plan.rows = z.rows;
     int64_t records = a.width * a.c.per;
     if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
-    plan.nsplit = splits_of(z.form.many, z.units, records);
+    plan.nsplit = splits_of(z.form.many, z.units, a.batch, records);
     plan.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes);
     plan.stat = reinterpret_cast<float*>(reinterpret_cast<char*>(plan.part) + align256(part_floats(z, dp, plan.nsplit) * 4));
     const dim3 grid((unsigned)(z.units * plan.nsplit));

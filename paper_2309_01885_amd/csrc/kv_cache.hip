@@ -3,7 +3,7 @@
 // A group of channels x gets an asymmetric min/max grid as the weights' rows do
 // (grid_minmax_kernel), in fp32:
 //   lo = min(0, min x), hi = max(0, max x),
-//   s = max((hi - lo) / 15, 2^-126), to 20 bits of mantissa (the zero point takes the
+//   s = max((hi - lo) * fp32(1 / 15), 2^-126), to 20 bits of mantissa (the zero point takes the
 //   other four), z = rint(-lo (1 / s)),  n = clamp(rint(x (1 / s)) + z, 0, 15).
 // Every step is one correctly rounded fp32 operation, so the codes depend on the group's
 // values alone.  Both kernels are bound by memory: each value is moved once.
@@ -71,7 +71,7 @@ template <int LANES> __device__ inline uint32_t quantize8(const float* x, uint32
     uint32_t n8 = 0;
     word = 0x7fc00000u;                                  // a NaN scale: the group reads back as NaN
     if (range <= 3.402823466e38f) {
-        word = (__float_as_uint(fmaxf(range / 15.f, kKvMinScale)) + 8u) & ~15u;
+        word = (__float_as_uint(fmaxf(range * kKvFifteenth, kKvMinScale)) + 8u) & ~15u;
         const float inv = 1.f / __uint_as_float(word);
         const float z = fminf(fmaxf(rintf(-lo * inv), 0.f), 15.f);
         word |= (uint32_t)z;

@@ -328,6 +328,20 @@ def test_attention_magnitudes(qe, dtype, kscale, vscale, qscale):
     attend(qe, [140], [20], 4, 2, 128, 32, 64, dtype, seed=2, kscale=kscale, vscale=vscale, qscale=qscale)
 
 
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("nq", [4, 96])
+def test_attention_fp32_as_a_whole(qe, nq, group):
+    """fp32 calls over many rows: the 2-norm of the error is within 2^-20 of the result's (fp16 parts
+    that miss each other by a step in one weight of some thousand are 10 times that, and within the
+    bound of a single element)."""
+    n, heads, dim = 500, 8, 80
+    pages, table, held = cache(qe, [n], heads, dim, group, 32, "f32", 5)
+    q = draw((nq, heads, dim), 12, "f32", 0.5).cuda()
+    out = qe.kv_attn(q, pages, dev(table), dev(np.array([n], np.int32)), group=group)
+    ref, _, _ = okv.attention(f64(q), *held[0], n - nq + np.arange(nq), dim ** -0.5)
+    assert np.linalg.norm(f64(out) - ref) <= 2.0 ** -20 * np.linalg.norm(ref)
+
+
 def test_attention_zero_queries_and_values(qe):
     pages, table, held = cache(qe, [50], 2, 64, 64, 64)
     for dtype in DT:
