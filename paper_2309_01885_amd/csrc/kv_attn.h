@@ -379,51 +379,61 @@ template <int UT, int CL, int NT> struct KvSums {
         }
     }
     // Where some row does not see a token (its score s is -inf), a NaN scale of that token would meet a
-    // probability of 0.  NaN scales become 0, and the sums of the rows and groups that see one NaN.
-    template <class T, int KR, int NG> __device__ void clear_nans(const float (&s)[KR][NT][8], float (&sv)[KR][NG][8])
+    // probability of 0.  Such scales are to be taken as 0 (the result), and the sums of the rows and
+    // groups that do see one become NaN here.
+    template <class T, int KR, int NG, class F> __device__ bool meet_nans(const float (&s)[KR][NT][8], F scales)
     {
-        float x = 0.f;
+        float sum = 0.f;
 #pragma unroll
         for (int y = 0; y < KR; ++y)
 #pragma unroll
-            for (int g = 0; g < NG; ++g)
+            for (int g = 0; g < NG; ++g) {
+                float sv[8];
+                scales(y, g, sv);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x += sv[y][g][e];
-        if (!__any(x != x)) return;
-#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += sv[e];
+            }
+        if (!__any(sum != sum)) return false;
+#pragma unroll 1
         for (int g = 0; g < NG; ++g) {
+            float met[NT] = {};
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float met = 0.f;
+            for (int y = 0; y < KR; ++y) {
+                float sv[8];
+                scales(y, g, sv);
 #pragma unroll
-                for (int y = 0; y < KR; ++y)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) met = s[y][n][e] != -kKvInf && sv[y][g][e] != sv[y][g][e] ? 1.f : met;
-                const float add = kv_max4(met) == 0.f ? 0.f : __builtin_nanf("");
-#pragma unroll
-                for (int t = 0; t < UT; ++t)
-                    if (T::group_of(t) == g)
-#pragma unroll
-                        for (int k = 0; k < CL; ++k)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[t][k][n][e] += add;
+                    for (int e = 0; e < 8; ++e) met[n] = s[y][n][e] != -kKvInf && sv[e] != sv[e] ? 1.f : met[n];
             }
 #pragma unroll
-            for (int y = 0; y < KR; ++y)
+            for (int n = 0; n < NT; ++n) {
+                const float add = kv_max4(met[n]) == 0.f ? 0.f : __builtin_nanf("");
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sv[y][g][e] = sv[y][g][e] != sv[y][g][e] ? 0.f : sv[y][g][e];
+                for (int t = 0; t < UT; ++t)
+#pragma unroll
+                    for (int k = 0; k < CL; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[t][k][n][e] += T::group_of(t) == g ? add : 0.f;
+            }
         }
+        return true;
     }
     // s: the products times their key scales, of KR records that start at tokens t0; on return p 2^shift
-    // (0 where the row sees nothing).  masked: some row does not see all of them.  sv: the value scales.
-    template <class T, int KR, int NG, int NC, int PARTS>
-    __device__ void weigh(float (&s)[KR][NT][8], float (&sv)[KR][NG][8], const KvRows<NC, NT, PARTS>& r, bool slopes, const int (&t0)[KR], bool masked)
+    // (0 where the row sees nothing).  masked: some row does not see all of them.  scales(y, g, x) gives
+    // the lane's value scales; clear() is called if NaNs among them are to be taken as 0.
+    template <class T, int KR, int NG, int NC, int PARTS, class F, class C>
+    __device__ void weigh(float (&s)[KR][NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, const int (&t0)[KR], bool masked, F scales, C clear)
     {
         float big = 0.f;
 #pragma unroll
         for (int y = 0; y < KR; ++y)
 #pragma unroll
-            for (int g = 0; g < NG; ++g) big = fmaxf(big, kv_max8(sv[y][g]));
+            for (int g = 0; g < NG; ++g) {
+                float sv[8];
+                scales(y, g, sv);
+                big = fmaxf(big, kv_max8(sv));
+            }
         float at[NT], c[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -450,7 +460,7 @@ template <int UT, int CL, int NT> struct KvSums {
                 }
                 c[n] = 1.f;
             }
-            clear_nans<T>(s, sv);
+            if (masked && meet_nans<T, KR, NG>(s, scales)) clear();
         }
         move(at, big);
 #pragma unroll
@@ -543,6 +553,62 @@ template <int UT, int CL, int NT> struct KvSums {
                 for (int k = 1; k < CL; k += 2)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[t][k][n][e] *= 0.0625f;
+        }
+    }
+};
+
+// A lane's value scales of KR records.  Up to two groups are kept in registers; more are read from LDS where they
+// are used (held, they were 64 registers with eight groups).
+template <int KR, int NG> struct KvScales {
+    static constexpr bool kKept = NG <= 2;
+    float s[kKept ? KR : 1][kKept ? NG : 1][8];
+    const float* at[kKept ? 1 : KR];                             // group 0's; the others' are `step` floats apart
+    int step;
+    bool nans;
+
+    __device__ static void read(const float* p, float (&x)[8])
+    {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e < 4 ? a[e] : b[e - 4];
+    }
+    template <class F> __device__ void load(F from)
+    {
+        nans = false;
+        if constexpr (kKept) {
+#pragma unroll
+            for (int y = 0; y < KR; ++y)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) read(from(y, g), s[y][g]);
+        } else {
+            step = (int)(from(0, 1) - from(0, 0));
+#pragma unroll
+            for (int y = 0; y < KR; ++y) at[y] = from(y, 0);
+        }
+    }
+    __device__ void get(int y, int g, float (&x)[8]) const
+    {
+        if constexpr (kKept) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = NG == 1 ? s[y][0][e] : g == 0 ? s[y][0][e] : s[y][NG - 1][e];
+        } else {
+            read(at[y] + g * step, x);
+            if (nans) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = x[e] != x[e] ? 0.f : x[e];
+            }
+        }
+    }
+    __device__ void clear()
+    {
+        nans = true;
+        if constexpr (kKept) {
+#pragma unroll
+            for (int y = 0; y < KR; ++y)
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[y][g][e] = s[y][g][e] != s[y][g][e] ? 0.f : s[y][g][e];
         }
     }
 };
@@ -688,18 +754,15 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
             find(r + kKvWaves);
             keys();
         }
-        float sv[1][NG][8];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&held.s[g][32 + 8 * j]), s1 = *reinterpret_cast<const f32x4*>(&held.s[g][36 + 8 * j]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sv[0][g][e] = e < 4 ? s0[e] : s1[e - 4];
-        }
-        sums.template weigh<T>(s, sv, rows, a.slopes != nullptr, at, masked);
+        KvScales<1, NG> sv;
+        sv.load([&](int, int g) { return &held.s[g][32 + 8 * j]; });
+        sums.template weigh<T, 1, NG>(s, rows, a.slopes != nullptr, at, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             f16x8 pr[PARTS][NT];
-            sums.template weights<PARTS>(s[0], sv[0][g], pr);
+            float x[8];
+            sv.get(0, g, x);
+            sums.template weights<PARTS>(s[0], x, pr);
             const u32x4 lo = *reinterpret_cast<const u32x4*>(&held.lo[g][32 + 8 * j]), hi = *reinterpret_cast<const u32x4*>(&held.hi[g][32 + 8 * j]);
 #pragma unroll
             for (int t = 0; t < UT; ++t) {
@@ -709,10 +772,10 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
                 for (int p = 0; p < 4; ++p) w[p] = T::kHalf ? v[t][p] >> (i & 8) : v[t][p];
 #pragma unroll
                 for (int c = 0; c < CL; ++c) {
-                    uint32_t x[4];
+                    uint32_t pair[4];
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) x[p] = kv_code_pair(w[p] >> (c >= 2 ? 8 : 0), c & 1 ? bits.high : bits.low, c & 1 ? hi[p] : lo[p], bits);
-                    const f16x8 f = kv_frag(x[0], x[1], x[2], x[3]);
+                    for (int p = 0; p < 4; ++p) pair[p] = kv_code_pair(w[p] >> (c >= 2 ? 8 : 0), c & 1 ? bits.high : bits.low, c & 1 ? hi[p] : lo[p], bits);
+                    const f16x8 f = kv_frag(pair[0], pair[1], pair[2], pair[3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -841,7 +904,8 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     const KvBits bits;
     const uint32_t vmask = vk & 1 ? bits.high : bits.low, vshift = vk & 1 ? 4 : 0;   // (KR == 1)
     const int token = T::key_token(i, kh);
-    uint32_t k[CW], kz[NG], v[VW][4], vw[NG][8], word[SW];
+    constexpr int VG = T::kHalf ? VW : NG;                       // value groups whose zero points the wave needs
+    uint32_t k[CW], kz[CW], v[VW][4], vw[VG][8], word[SW];
 
     const int64_t pages = a.c.pages_count;
     const int32_t* table = a.table + u.b * a.width;
@@ -862,10 +926,11 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
         const uint8_t* rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
         kv_words<CW>(rec + (uint32_t)(token * R::kKeyRow + j * (4 * NC)) + 4 * kc, k);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            kz[g] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(R::kKeyWords + g * (4 * kKvTok) + 4 * token));
-            kv_words<8>(rec + (uint32_t)(R::kValWords + g * (4 * kKvTok) + 32 * j), vw[g]);
-        }
+        for (int x = 0; x < CW; ++x)
+            kz[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(R::kKeyWords + min((kc + x) / T::CPG, NG - 1) * (4 * kKvTok) + 4 * token));
+#pragma unroll
+        for (int x = 0; x < VG; ++x)
+            kv_words<8>(rec + (uint32_t)(R::kValWords + (T::kHalf ? min(vt + 2 * x, NG - 1) : x) * (4 * kKvTok) + 32 * j), vw[x]);
 #pragma unroll
         for (int x = 0; x < VW; ++x)
             kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(T::kHalf ? min(vt + 2 * x, UT - 1) : x, i) * (2 * kKvTok) + 16 * j), v[x]);
@@ -890,13 +955,7 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
         for (int x = 0; x < CW; ++x) {
             if (KR == 1 && NC % 2 != 0 && kc + x >= NC) continue;
             uint32_t lo, hi;
-            if constexpr (KR == 2) kv_key_zero(kz[x / T::CPG], lo, hi, bits);
-            else {
-                uint32_t z = kz[0];
-#pragma unroll
-                for (int g = 1; g < NG; ++g) z = (kc + x) / T::CPG == g ? kz[g] : z;
-                kv_key_zero(z, lo, hi, bits);
-            }
+            kv_key_zero(kz[x], lo, hi, bits);
             st.k[part][kh][kc + x][lane] = kv_key_frag(k[x], lo, hi, bits);
         }
 #pragma unroll
@@ -906,12 +965,7 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             uint32_t f[VK][4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                uint32_t w0 = vw[0][2 * p], w1 = vw[0][2 * p + 1];
-#pragma unroll
-                for (int g = 1; g < NG; ++g) {
-                    w0 = T::group_of(t) == g ? vw[g][2 * p] : w0;
-                    w1 = T::group_of(t) == g ? vw[g][2 * p + 1] : w1;
-                }
+                const uint32_t w0 = vw[T::kHalf ? x : T::group_of(x)][2 * p], w1 = vw[T::kHalf ? x : T::group_of(x)][2 * p + 1];
                 const uint32_t w = v[x][p] >> (T::kHalf ? i & 8 : vk & 2 ? 8 : 0);
                 if constexpr (KR == 2) {
                     uint32_t lo, hi;
@@ -987,22 +1041,17 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             }
         }
         start();
-        float sv[KR][NG][8];
-#pragma unroll
-        for (int y = 0; y < KR; ++y)
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.vs[y][g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.vs[y][g][8 * j + 4]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sv[y][g][e] = e < 4 ? s0[e] : s1[e - 4];
-            }
-        sums.template weigh<T>(s, sv, rows, a.slopes != nullptr, t0, masked);
+        KvScales<KR, NG> sv;
+        sv.load([&](int y, int g) { return &st.vs[y][g][8 * j]; });
+        sums.template weigh<T, KR, NG>(s, rows, a.slopes != nullptr, t0, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
 #pragma unroll
         for (int y = 0; y < KR; ++y)
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 f16x8 pr[PARTS][NT];
-                sums.template weights<PARTS>(s[y], sv[y][g], pr);
+                float x[8];
+                sv.get(y, g, x);
+                sums.template weights<PARTS>(s[y], x, pr);
 #pragma unroll
                 for (int t = 0; t < UT; ++t) {
                     if (T::group_of(t) != g) continue;
