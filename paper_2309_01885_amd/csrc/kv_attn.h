@@ -274,16 +274,22 @@ template <int NC, int NT, int PARTS> struct KvRows {
         for (int n = 0; n < NT; ++n) {
             const bool have = row0 + 16 * n + i < u.rows;
             float x[NC][8], top = 0.f;
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                const uint32_t in = have && 8 * (4 * k + j) < a.c.dim ? ~0u : 0u;
+#pragma unroll
+                for (int y = 0; y < E / 2; ++y)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) raw[n][k][y][w] &= in;
+            }
             auto take = [&](auto channel) {
 #pragma unroll
-                for (int k = 0; k < NC; ++k) {
-                    const bool in = have && 8 * (4 * k + j) < a.c.dim;
+                for (int k = 0; k < NC; ++k)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        x[k][e] = in ? channel(k, e) : 0.f;
+                        x[k][e] = channel(k, e);
                         top = fmaxf(top, fabsf(x[k][e]));
                     }
-                }
             };
             if constexpr (PARTS == 2) take([&](int k, int e) { return __uint_as_float(raw[n][k][e / 4][e % 4]); });
             else if (a.dtype == QE_BF16) take([&](int k, int e) { return __uint_as_float(e & 1 ? raw[n][k][0][e / 2] & 0xffff0000u : raw[n][k][0][e / 2] << 16); });
@@ -885,14 +891,12 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     // workgroups of an XCD (every eighth) get a contiguous stretch of units: rows of the same keys
     // share its L2
     const uint32_t wg = blockIdx.x, q8 = gridDim.x / 8, r8 = gridDim.x % 8, x8 = wg & 7;
-    const uint32_t mine = x8 * q8 + min(x8, r8) + (wg >> 3);
-    const uint32_t unit = mine / (uint32_t)plan.nsplit;
-    const int split = (int)(mine - unit * plan.nsplit);
+    const uint32_t unit = x8 * q8 + min(x8, r8) + (wg >> 3);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int i = tid & 15, j = lane >> 4;
-    const KvUnit u = kv_unit(a, plan, unit, tid == 0 && split == 0);
-    if (split >= u.splits || u.tile_row >= u.rows) return;
-    const int r0 = u.from(split), r1 = u.from(split + 1);
+    const KvUnit u = kv_unit(a, plan, unit, tid == 0);
+    if (u.tile_row >= u.rows) return;
+    const int r0 = u.rec0, r1 = u.rec1;
     const int row0 = u.tile_row + wave * (16 * NT);
 
     // what the wave converts: of record `part` of a stage, key half kh from channel block kc on, value
@@ -993,12 +997,12 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
         st.at[part] = here && r + part < r1 ? (r + part) * kKvTok : 0x7fffff00;
     };
 
+    if (r0 < r1) start();
     KvRows<NC, NT, PARTS> rows;
     rows.load(a, u, min(row0, u.rows - 1));
     KvSums<UT, CL, NT> sums;
     sums.clear();
     if (r0 < r1) {
-        start();
         convert(stage[0], r0);
         start();
     }
@@ -1070,31 +1074,17 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     }
     if (row0 >= u.rows) return;
     sums.finish();
-    const float back = __builtin_amdgcn_exp2f(-sums.shift);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = row0 + 16 * n + i, qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
-        const int64_t slot = ((int64_t)unit * plan.nsplit + split) * plan.rows + (row - u.tile_row);
-        const float f = u.splits > 1 ? back : sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n];
+        const float f = sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n];
         sums.template octets<T>(n, [&](int d, const float* x) {
             float out[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) out[e] = f == 0.f ? 0.f : x[e] * f;
-            if (row >= u.rows) return;
-            if (u.splits > 1) {
-#pragma unroll
-                for (int y = 0; y < 8; y += 4) *reinterpret_cast<f32x4*>(plan.part + slot * DP + d + y) = f32x4{out[y], out[y + 1], out[y + 2], out[y + 3]};
-            } else if (d < a.c.dim)
-                kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, out);
+            if (row < u.rows && d < a.c.dim) kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, out);
         });
-        if (row >= u.rows) continue;
-        if (j == 0) {
-            if (u.splits > 1) {
-                plan.stat[2 * slot] = sums.top[n];
-                plan.stat[2 * slot + 1] = sums.mass[n] * back;
-            } else if (a.lse)
-                a.lse[(u.first + qi) * a.heads + head] = kv_lse(sums.top[n] - sums.shift, sums.mass[n]);
-        }
+        if (row < u.rows && j == 0 && a.lse) a.lse[(u.first + qi) * a.heads + head] = kv_lse(sums.top[n] - sums.shift, sums.mass[n]);
     }
 }
 
@@ -1150,17 +1140,17 @@ template <int DP, bool ONE> __global__ __launch_bounds__(256) void kv_join_kerne
 struct KvForm { bool many; int nt; };
 
 // Tiles of a wave with many rows: what the registers hold.
-constexpr int kv_many_nt(int dp, bool f32) { return dp <= 128 && !f32 ? 2 : 1; }
+constexpr int kv_many_nt(int dp, int group, bool f32) { return dp <= 128 && !f32 && (group > 32 || dp == 64) ? 2 : 1; }
 
 template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm form, dim3 grid, hipStream_t s)
 {
     kv_dispatch_group<DP>(a.group, [&](auto shape) {
         constexpr int G = decltype(shape)::GROUP;
         if (a.dtype == QE_F32) {
-            if (form.many) hipLaunchKernelGGL((kv_many_kernel<DP, G, kv_many_nt(DP, true), 2>), grid, dim3(256), 0, s, a, plan);
+            if (form.many) hipLaunchKernelGGL((kv_many_kernel<DP, G, kv_many_nt(DP, G, true), 2>), grid, dim3(256), 0, s, a, plan);
             else hipLaunchKernelGGL((kv_few_kernel<DP, G, 1, 2>), grid, dim3(256), 0, s, a, plan);
         } else if (form.many) {
-            hipLaunchKernelGGL((kv_many_kernel<DP, G, kv_many_nt(DP, false), 1>), grid, dim3(256), 0, s, a, plan);
+            hipLaunchKernelGGL((kv_many_kernel<DP, G, kv_many_nt(DP, G, false), 1>), grid, dim3(256), 0, s, a, plan);
         } else if (DP > 128 || form.nt == 1) {
             hipLaunchKernelGGL((kv_few_kernel<DP, G, 1, 1>), grid, dim3(256), 0, s, a, plan);
         } else {

@@ -11,23 +11,30 @@ extern template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, di
 
 namespace {
 
-constexpr int64_t kManyFrom = 128;  // query rows of a sequence and key head from which waves have rows of their own
-// Workgroups that fill the chip: two of a CU with many rows, three with few.  Twice as many where there
+// Workgroups of the many-row form from which it is taken: two of a CU.  Below that the few-row form is
+// faster, since its workgroups are smaller and share a row's tokens.  2048 tokens, bf16, many against
+// few, in us: 128 channels in groups of 128, 128 workgroups 67 / 39, 256 69 / 68, 384 84 / 90; 192
+// channels, 256 workgroups 110 / 80, 512 135 / 133; 256 channels, 512 workgroups 137 / 151; fp32,
+// 400 workgroups of uneven lengths 56 / 32; 2048 queries of 32 heads over 16384 tokens 681 / 802.
+// 256 channels in groups of 32 do not fit the few-row form's registers: 256 workgroups 293 / 378.
+constexpr int64_t kManyRows = 128, kManyFill = 512, kManyFillWide = 128;
+// Workgroups of the few-row form that fill the chip, three of a CU.  Twice as many where there
 // are enough sequences for their lengths to differ: the long ones are not left to the end (64
 // sequences of 2048 to 8192 tokens 89 -> 86 us; two of the same length 111 -> 117).
-constexpr int64_t kFillMany = 512, kFillFew = 768, kUneven = 8;
+constexpr int64_t kFill = 768, kUneven = 8;
 
-KvForm form_of(int64_t rows, int dp, bool f32)
+KvForm form_of(int64_t heads, int64_t rows, int dp, int group, bool f32)
 {
-    if (rows >= kManyFrom) return {true, kv_many_nt(dp, f32)};
+    const int nt = kv_many_nt(dp, group, f32);
+    if (rows >= kManyRows && heads * cdiv(rows, 16 * nt * kKvWaves) >= (dp == 8 * group ? kManyFillWide : kManyFill)) return {true, nt};
     return {false, rows <= 16 || f32 || dp > 128 ? 1 : 2};
 }
 
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
-int splits_of(bool many, int64_t units, int64_t batch, int64_t records)
+int splits_of(KvForm form, int64_t units, int64_t batch, int64_t records)
 {
-    if (records < kKvSplitFrom) return 1;
-    const int64_t fill = many ? kFillMany : batch < kUneven ? kFillFew : 2 * kFillFew;
+    if (form.many || records < kKvSplitFrom) return 1;
+    const int64_t fill = batch < kUneven ? kFill : 2 * kFill;
     return (int)std::max<int64_t>(1, std::min(fill / std::max<int64_t>(units, 1), records / kKvMinRecords));
 }
 
@@ -37,11 +44,11 @@ struct Sizes {
     int64_t row_tiles, units;
 };
 
-Sizes sizes_of(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, bool f32)
+Sizes sizes_of(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int group, bool f32)
 {
     Sizes z;
     const int64_t rows = max_q * (heads / kv_heads);
-    z.form = form_of(rows, kv_dp(dim), f32);
+    z.form = form_of(batch * kv_heads, rows, kv_dp(dim), group, f32);
     z.rows = 16 * z.form.nt * (z.form.many ? kKvWaves : 1);
     z.row_tiles = cdiv(rows, z.rows);
     z.units = batch * kv_heads * z.row_tiles;
@@ -56,9 +63,10 @@ size_t stat_floats(const Sizes& z, int nsplit) { return (size_t)z.units * nsplit
 size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim)
 {
     size_t need = 0;
+    // (The many-row form has no splits, and a group of 32 only takes it earlier: a group of 128 needs the most.)
     for (int f32 = 0; f32 < 2; ++f32) {
-        const Sizes z = sizes_of(batch, max_q, heads, kv_heads, dim, f32 != 0);
-        const int nsplit = splits_of(z.form.many, z.units, batch, INT32_MAX);
+        const Sizes z = sizes_of(batch, max_q, heads, kv_heads, dim, 128, f32 != 0);
+        const int nsplit = splits_of(z.form, z.units, batch, INT32_MAX);
         if (nsplit > 1)
             need = std::max(need, align256(part_floats(z, kv_dp(dim), nsplit) * 4) + align256(stat_floats(z, nsplit) * 4));
     }
@@ -72,7 +80,7 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     const size_t size = a.dtype == QE_F32 ? 4 : 2;
     a.vec_q = ((uintptr_t)a.q | (uint64_t)a.qt * size | (uint64_t)a.qh * size) % 16 == 0;
     a.vec_o = ((uintptr_t)a.out | (uint64_t)a.ot * size | (uint64_t)a.oh * size) % 16 == 0;
-    const Sizes z = sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.dtype == QE_F32);
+    const Sizes z = sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, a.dtype == QE_F32);
     KvPlan plan{};
     plan.row_tiles = z.row_tiles;
     plan.units = z.units;
@@ -81,7 +89,7 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     plan.rows = z.rows;
     int64_t records = a.width * a.c.per;
     if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
-    plan.nsplit = splits_of(z.form.many, z.units, a.batch, records);
+    plan.nsplit = splits_of(z.form, z.units, a.batch, records);
     plan.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes);
     plan.stat = reinterpret_cast<float*>(reinterpret_cast<char*>(plan.part) + align256(part_floats(z, dp, plan.nsplit) * 4));
     const dim3 grid((unsigned)(z.units * plan.nsplit));

@@ -433,6 +433,91 @@ def test_attention_reports_bad_pages_lengths_and_ranges(qe):
     check(out, None, q, held, [1], dim ** -0.5, "f32")
 
 
+def many_rows(kv, lens, nqs, group, dim):
+    """The sequences and as many short ones beside them as let the call take the form for many rows
+    (its rule: 512 workgroups of at most 128 query rows of a key head, at least 128 rows a head)."""
+    fill = -(-512 // kv)
+    return list(lens) + [7] * fill, list(nqs) + [1] * fill
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dim", [8, 40, 64, 80, 96, 128, 152, 192, 256])
+def test_attention_many_rows_widths(qe, dim, group):
+    """Every width and group; rows that see nothing, a head's rows in several tiles, empty sequences."""
+    for dtype in DT:
+        print(f"[kv] many dim={dim} group={group} {dtype}", flush=True)
+        lens, nqs = many_rows(16, [131, 33, 0, 200], [131, 60, 2, 35], group, dim)
+        attend(qe, lens, nqs, 16, 16, dim, group, 32 if dim % 16 else 64, dtype, seed=dim + group)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("heads,kv", [(12, 4), (29, 1), (40, 8)])
+def test_attention_many_rows_shared_heads(qe, heads, kv, dtype):
+    lens, nqs = many_rows(kv, [260, 97], [128, 97], 64, 64)
+    attend(qe, lens, nqs, heads, kv, 64, 64, 64, dtype, seed=heads)
+    attend(qe, lens, nqs, heads, kv, 128, 32, 32, dtype, seed=heads + 1, window=50, slopes=True)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("window", [0, 1, 33, 100, 5000])
+def test_attention_many_rows_masks(qe, window, dtype):
+    lens, nqs = many_rows(24, [300, 129, 3], [140, 129, 40], 64, 96)
+    attend(qe, lens, nqs, 24, 24, 96, 64, 32, dtype, seed=window, window=window, slopes=True)
+    attend(qe, lens, nqs, 24, 24, 96, 128, 64, dtype, seed=window + 1, window=window, causal=window != 0)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_attention_many_rows_all_visible(qe, dtype):
+    lens, nqs = many_rows(24, [300, 129, 3], [140, 129, 40], 64, 128)
+    attend(qe, lens, nqs, 24, 24, 128, 64, 32, dtype, seed=2, causal=False)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("kscale,vscale,qscale", [(1e-6, 1e4, 1e4), (30.0, 1e-6, 1.0), (1e-3, 1e-3, 1e-3)])
+def test_attention_many_rows_magnitudes(qe, dtype, kscale, vscale, qscale):
+    if dtype == "f16" and qscale == 1e4:
+        pytest.skip("fp16 holds no such queries and values")
+    lens, nqs = many_rows(16, [140], [140], 64, 64)
+    attend(qe, lens, nqs, 16, 16, 64, 64, 64, dtype, seed=1, kscale=kscale, vscale=vscale, qscale=qscale)
+
+
+def test_attention_many_rows_fp32_as_a_whole(qe):
+    n, heads, dim = 500, 64, 80
+    pages, table, held = cache(qe, [n], heads, dim, 64, 32, "f32", 5)
+    q = draw((n, heads, dim), 12, "f32", 0.5).cuda()
+    out = qe.kv_attn(q, pages, dev(table), dev(np.array([n], np.int32)))
+    ref, _, _ = okv.attention(f64(q), *held[0], np.arange(n), dim ** -0.5)
+    assert np.linalg.norm(f64(out) - ref) <= 2.0 ** -20 * np.linalg.norm(ref)
+
+
+def test_attention_many_rows_bad_values_and_pages(qe):
+    """NaN and infinite groups spoil the rows that see them, also beside a page that is missing; the
+    bytes past a sequence's end spoil none."""
+    dim, heads, n = 64, 200, 140
+    pages = qe.kv_pages(6, heads, dim, 32, 32)
+    pages.fill_(0xFF)
+    k, v = draw((n, heads, dim), 1).cuda(), draw((n, heads, dim), 2).cuda()
+    v[20, :, 40] = float("nan")
+    k[10, :, 3] = float("inf")
+    qe.kv_write(k, v, torch.arange(n, device="cuda"), pages, group=32)
+    table, L = np.array([[0, 1, 2, 3, 4]], np.int32), dev(np.array([n], np.int32))
+    q = draw((n, heads, dim), 3).cuda()
+    ws = qe.workspace(qe.kv_attn_workspace_size(n, 1, n, heads, heads, dim), "cuda")
+    out = qe.kv_attn(q, pages, dev(table), L, group=32, window=5, ws=ws)
+    assert qe.sync_status(ws) == 0
+    assert bool(torch.isnan(out[10:15]).all()) and bool(torch.isfinite(out[:10]).all())
+    assert bool(torch.isfinite(out[15:20]).all()) and bool(torch.isfinite(out[25:]).all())
+    assert bool(torch.isnan(out[20:25, :, 32:]).all()) and bool(torch.isfinite(out[20:25, :, :32]).all())
+    for absent in (-1, 10 ** 6):
+        table[0, 0] = absent
+        out = qe.kv_attn(q, pages, dev(table), L, group=32, ws=ws)
+        assert qe.sync_status(ws) == qe.QE_ERR_ARG
+        assert not bool(out[:32].any())
+        seen = f64(qe.kv_read(pages, torch.arange(n, device="cuda"), dim, group=32)[0]), f64(
+            qe.kv_read(pages, torch.arange(n, device="cuda"), dim, group=32)[1])
+        check(out[32:], None, q[32:], [tuple(x[32:] for x in seen)], [n - 32], dim ** -0.5, "f32")
+
+
 def test_attention_is_deterministic_and_replays(qe):
     """The same bits from call to call, on another stream, and from a graph between other work."""
     lens = [3000, 77]
