@@ -52,6 +52,7 @@ struct KvUnit {
 // Records a split has at least (a workgroup's waves take them in turn), and from which splitting gains
 // more than the join costs (a record takes a wave about 1.3 us, the join with its launch 6 us).
 constexpr int kKvMinRecords = 4, kKvSplitFrom = 20;
+constexpr int kKvFewSplits = 8;
 
 // A value that is the same for the whole workgroup and not written by the kernel: a scalar load.
 __device__ inline int kv_scalar(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)p; }
@@ -1088,14 +1089,13 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     }
 }
 
-// Joins the splits of a row.  ONE: one workgroup per row, whose waves take the splits in turn; else a
-// wave per row (few splits of many rows: a quarter of the workgroups).
-template <int DP, bool ONE> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a, KvPlan plan)
+// Joins the splits of a row: one workgroup a row, whose waves take the splits in turn.
+template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a, KvPlan plan)
 {
     constexpr int C = (DP + 63) / 64;
     __shared__ float sum[kKvWaves][DP], mass[kKvWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t at = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (ONE ? 1 : kKvWaves) + (ONE ? 0 : wave);
+    const int64_t at = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (at >= plan.units * plan.rows) return;
     // (plan.rows is a power of two)
     const uint32_t unit = (uint32_t)(at >> plan.rows_log2);
@@ -1110,7 +1110,7 @@ template <int DP, bool ONE> __global__ __launch_bounds__(256) void kv_join_kerne
     for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
     float l = 0.f, x[C] = {};
 #pragma unroll 4
-    for (int s = ONE ? wave : 0; s < u.splits; s += ONE ? kKvWaves : 1) {
+    for (int s = wave; s < u.splits; s += kKvWaves) {
         const int64_t k = slot + (int64_t)s * plan.rows;
         const float t = plan.stat[2 * k], f = t == m ? 1.f : __builtin_amdgcn_exp2f(t - m);
         l = fmaf(plan.stat[2 * k + 1], f, l);
@@ -1119,21 +1119,66 @@ template <int DP, bool ONE> __global__ __launch_bounds__(256) void kv_join_kerne
             if (DP % 64 == 0 || 64 * c + lane < DP) x[c] = fmaf(plan.part[k * DP + 64 * c + lane], f, x[c]);
     }
     const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
-    const int64_t to = (u.first + qi) * a.ot + head * a.oh;
-    if constexpr (ONE) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (DP % 64 == 0 || 64 * c + lane < DP) sum[wave][64 * c + lane] = x[c];
-        if (lane == 0) mass[wave] = l;
-        __syncthreads();
-        l = (mass[0] + mass[1]) + (mass[2] + mass[3]);
-        if (tid < a.c.dim) kv_out(a, to + tid, l == 0.f ? 0.f : ((sum[0][tid] + sum[1][tid]) + (sum[2][tid] + sum[3][tid])) / l);
-    } else {
+    for (int c = 0; c < C; ++c)
+        if (DP % 64 == 0 || 64 * c + lane < DP) sum[wave][64 * c + lane] = x[c];
+    if (lane == 0) mass[wave] = l;
+    __syncthreads();
+    l = (mass[0] + mass[1]) + (mass[2] + mass[3]);
+    if (tid < a.c.dim)
+        kv_out(a, (u.first + qi) * a.ot + head * a.oh + tid,
+               l == 0.f ? 0.f : ((sum[0][tid] + sum[1][tid]) + (sum[2][tid] + sum[3][tid])) / l);
+    if (a.lse && tid == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
+}
+
+// The same for few splits (kKvFewSplits at most) of many rows: one workgroup a unit, a thread 8 channels of a row,
+// four splits on the way at a time.
+template <int DP> __global__ __launch_bounds__(256) void kv_join_unit_kernel(KvAttn a, KvPlan plan)
+{
+    const uint32_t unit = blockIdx.x;
+    const KvUnit u = kv_unit(a, plan, unit, false);
+    if (u.splits <= 1) return;
+    const float2* const stat = reinterpret_cast<const float2*>(plan.stat);
+    for (int x = threadIdx.x; x < plan.rows * (DP / 8); x += 256) {
+        const int rr = x / (DP / 8), d = 8 * (x - rr * (DP / 8)), row = u.tile_row + rr;
+        if (row >= u.rows) break;
+        const int64_t slot = (int64_t)unit * plan.nsplit * plan.rows + rr;
+        auto place = [&](int s) { return slot + (int64_t)min(s, u.splits - 1) * plan.rows; };
+        float2 st[kKvFewSplits];
+        float m = -kKvInf, l = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (64 * c + lane < a.c.dim) kv_out(a, to + 64 * c + lane, l == 0.f ? 0.f : x[c] / l);
+        for (int s = 0; s < kKvFewSplits; ++s) st[s] = stat[place(s)];
+#pragma unroll
+        for (int s = 0; s < kKvFewSplits; ++s) m = fmaxf(m, st[s].x);
+        f32x4 sum[2] = {};
+#pragma unroll
+        for (int s0 = 0; s0 < kKvFewSplits; s0 += 4) {
+            if (s0 >= u.splits) break;
+            f32x4 part[4][2];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) part[s][y] = *reinterpret_cast<const f32x4*>(plan.part + place(s0 + s) * DP + d + 4 * y);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if (s0 + s >= u.splits) break;
+                const float f = st[s0 + s].x == m ? 1.f : __builtin_amdgcn_exp2f(st[s0 + s].x - m);
+                l = fmaf(st[s0 + s].y, f, l);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e >> 2][e & 3] = fmaf(part[s][e >> 2][e & 3], f, sum[e >> 2][e & 3]);
+            }
+        }
+        const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
+        const int64_t to = (u.first + qi) * a.ot + head * a.oh + d;
+        float out[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = l == 0.f ? 0.f : sum[e >> 2][e & 3] / l;
+        if (d < a.c.dim) {
+            if (a.dtype == QE_F32) kv_out8<2>(a, to, out);
+            else kv_out8<1>(a, to, out);
+        }
+        if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
     }
-    if (a.lse && (ONE ? tid : lane) == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
 }
 
 // The form of a call: many rows or few, and a wave's tiles of 16 rows.
@@ -1157,10 +1202,10 @@ template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm
             hipLaunchKernelGGL((kv_few_kernel<DP, G, DP <= 128 ? 2 : 1, 1>), grid, dim3(256), 0, s, a, plan);
         }
     });
-    if (plan.nsplit > 8)
-        hipLaunchKernelGGL((kv_join_kernel<DP, true>), grid_xy(plan.units * plan.rows, 256), dim3(256), 0, s, a, plan);
+    if (plan.nsplit > kKvFewSplits)
+        hipLaunchKernelGGL((kv_join_kernel<DP>), grid_xy(plan.units * plan.rows, 256), dim3(256), 0, s, a, plan);
     else if (plan.nsplit > 1)
-        hipLaunchKernelGGL((kv_join_kernel<DP, false>), grid_xy(cdiv(plan.units * plan.rows, kKvWaves), 256), dim3(256), 0, s, a, plan);
+        hipLaunchKernelGGL((kv_join_unit_kernel<DP>), dim3((unsigned)plan.units), dim3(256), 0, s, a, plan);
 }
 
 }  // namespace qe
