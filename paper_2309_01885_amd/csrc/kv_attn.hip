@@ -20,14 +20,19 @@ namespace {
 constexpr int64_t kManyRows = 128, kManyFill = 512, kManyFillWide = 128;
 // Workgroups of the few-row form that fill the chip, three of a CU.  Twice as many where there
 // are enough sequences for their lengths to differ: the long ones are not left to the end (64
-// sequences of 2048 to 8192 tokens 89 -> 86 us; two of the same length 111 -> 117).
+// sequences of 2048 to 8192 tokens 89 -> 80 us; two of the same length 111 -> 118).
 constexpr int64_t kFill = 768, kUneven = 8;
+// Records (32 tokens of one head for one unit) from which the few-row form takes 32 rows a unit
+// instead of 16: a record's codes are then converted for twice the rows, but by half as many workgroups.
+// 128 channels, 32 against 16 rows, in us: 256 units of 64 records 38 / 33, 1024 of 32 42 / 44, 256
+// of 256 88 / 104; 64 channels: 21 of 63 15 / 14, 512 of 256 81 / 96.
+constexpr int64_t kWideFrom = 32768;
 
-KvForm form_of(int64_t heads, int64_t rows, int dp, int group, bool f32)
+KvForm form_of(int64_t heads, int64_t rows, int64_t records, int dp, int group, bool f32)
 {
     const int nt = kv_many_nt(dp, group, f32);
     if (rows >= kManyRows && heads * cdiv(rows, 16 * nt * kKvWaves) >= (dp == 8 * group ? kManyFillWide : kManyFill)) return {true, nt};
-    return {false, rows <= 16 || f32 || dp > 128 ? 1 : 2};
+    return {false, rows <= 16 || f32 || dp > 128 || heads * cdiv(rows, 32) < cdiv(kWideFrom, std::max<int64_t>(records, 1)) ? 1 : 2};
 }
 
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
@@ -44,11 +49,11 @@ struct Sizes {
     int64_t row_tiles, units;
 };
 
-Sizes sizes_of(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int group, bool f32)
+Sizes sizes_of(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int group, int64_t records, bool f32)
 {
     Sizes z;
     const int64_t rows = max_q * (heads / kv_heads);
-    z.form = form_of(batch * kv_heads, rows, kv_dp(dim), group, f32);
+    z.form = form_of(batch * kv_heads, rows, records, kv_dp(dim), group, f32);
     z.rows = 16 * z.form.nt * (z.form.many ? kKvWaves : 1);
     z.row_tiles = cdiv(rows, z.rows);
     z.units = batch * kv_heads * z.row_tiles;
@@ -63,12 +68,15 @@ size_t stat_floats(const Sizes& z, int nsplit) { return (size_t)z.units * nsplit
 size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim)
 {
     size_t need = 0;
-    // (The many-row form has no splits, and a group of 32 only takes it earlier: a group of 128 needs the most.)
-    for (int f32 = 0; f32 < 2; ++f32) {
-        const Sizes z = sizes_of(batch, max_q, heads, kv_heads, dim, 128, f32 != 0);
-        const int nsplit = splits_of(z.form, z.units, batch, INT32_MAX);
-        if (nsplit > 1)
-            need = std::max(need, align256(part_floats(z, kv_dp(dim), nsplit) * 4) + align256(stat_floats(z, nsplit) * 4));
+    // (The many-row form has no splits, and a group of 32 only takes it earlier: a group of 128 needs the
+    // most.  With few records units have 16 rows, with many 32; fp32 calls have 16.)
+    for (int64_t records : {(int64_t)1, (int64_t)INT32_MAX}) {
+        for (int f32 = 0; f32 < 2; ++f32) {
+            const Sizes z = sizes_of(batch, max_q, heads, kv_heads, dim, 128, records, f32 != 0);
+            const int nsplit = splits_of(z.form, z.units, batch, INT32_MAX);
+            if (nsplit > 1)
+                need = std::max(need, align256(part_floats(z, kv_dp(dim), nsplit) * 4) + align256(stat_floats(z, nsplit) * 4));
+        }
     }
     return kStatusBytes + need;
 }
@@ -80,15 +88,15 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     const size_t size = a.dtype == QE_F32 ? 4 : 2;
     a.vec_q = ((uintptr_t)a.q | (uint64_t)a.qt * size | (uint64_t)a.qh * size) % 16 == 0;
     a.vec_o = ((uintptr_t)a.out | (uint64_t)a.ot * size | (uint64_t)a.oh * size) % 16 == 0;
-    const Sizes z = sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, a.dtype == QE_F32);
+    int64_t records = a.width * a.c.per;
+    if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
+    const Sizes z = sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, records, a.dtype == QE_F32);
     KvPlan plan{};
     plan.row_tiles = z.row_tiles;
     plan.units = z.units;
     plan.per = a.heads / a.c.heads;
     plan.rows_log2 = __builtin_ctz((unsigned)z.rows);
     plan.rows = z.rows;
-    int64_t records = a.width * a.c.per;
-    if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
     plan.nsplit = splits_of(z.form, z.units, a.batch, records);
     plan.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes);
     plan.stat = reinterpret_cast<float*>(reinterpret_cast<char*>(plan.part) + align256(part_floats(z, dp, plan.nsplit) * 4));

@@ -250,8 +250,9 @@ def check(out, lse, q, held, nqs, scale, dtype, lens=None, **kw):
 
 
 def attend(qe, lens, nqs, heads, kv, dim, group, page, dtype, seed=0, scale=None, kscale=1.0, vscale=1.0,
-           qscale=1.0, slopes=False, give_lse=True, **kw):
+           qscale=1.0, slopes=False, give_lse=True, spare=0, **kw):
     pages, table, held = cache(qe, lens, kv, dim, group, page, dtype, seed, kscale, vscale)
+    table = np.pad(table, ((0, 0), (0, spare)), constant_values=-1)     # pages for sequences that grow
     total = sum(nqs)
     q = draw((total, heads, dim), seed + 7, dtype, qscale).cuda()
     scale = 1.0 / dim ** 0.5 if scale is None else scale
@@ -431,6 +432,61 @@ def test_attention_reports_bad_pages_lengths_and_ranges(qe):
                      q_start=dev(np.array([0, 400], np.int32)))
     assert qe.sync_status(ws) == qe.QE_ERR_ARG
     check(out, None, q, held, [1], dim ** -0.5, "f32")
+
+
+# Room in the page table from which rows of few units share tiles of 32 (32768 records of 32
+# tokens over all units).
+SPARE = 32768
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dim", [8, 40, 64, 80, 96, 128, 152, 256])
+def test_attention_wide_tiles(qe, dim, group, dtype):
+    """Tables with room for long sequences: rows that end inside of the first, the second and the third tile."""
+    attend(qe, [70, 33, 0, 41], [9, 3, 1, 30], 6, 2, dim, group, 64, dtype, seed=dim, spare=SPARE)
+    attend(qe, [800, 5000, 9], [1, 1, 1], 29, 1, dim, group, 32, dtype, seed=dim + 1, spare=SPARE)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_wide_tiles_masks(qe, dtype):
+    attend(qe, [300, 17], [33, 12], 20, 20, 80, 64, 32, dtype, seed=4, slopes=True, spare=SPARE)
+    attend(qe, [300, 17], [33, 40], 8, 2, 128, 64, 64, dtype, seed=5, causal=False, spare=SPARE)
+    for window in (1, 33, 3000):
+        # (a window bounds what a unit can read, so the units are many here)
+        attend(qe, [90, 141], [90, 70], 64 if window < 3000 else 72, 64 if window < 3000 else 72, 64, 32, 32, dtype,
+               seed=window, window=window, spare=SPARE)
+    attend(qe, [140], [1], 32, 1, 64, 64, 64, dtype, seed=1, kscale=30.0, vscale=1e-6, spare=SPARE)
+    attend(qe, [140], [20], 4, 2, 128, 32, 64, dtype, seed=2, kscale=1e-3, vscale=1e-3, qscale=1e-3, spare=SPARE)
+
+
+def test_attention_wide_tiles_windows(qe):
+    """Windows that mask (they bound the records of a unit, so it takes 4096 units of 8)."""
+    attend(qe, [150, 4, 5, 6], [120, 1, 2, 1], 256, 256, 64, 32, 32, "bf16", seed=9, window=100, spare=64)
+
+
+def test_attention_wide_tiles_bad_values_and_pages(qe):
+    dim, n = 64, 50
+    pages = qe.kv_pages(4, 1, dim, 32, 32)
+    pages.fill_(0xFF)
+    k, v = draw((n, 1, dim), 1).cuda(), draw((n, 1, dim), 2).cuda()
+    v[40, 0, 40] = float("nan")
+    qe.kv_write(k, v, torch.arange(n, device="cuda"), pages, group=32)
+    table = np.full((1, SPARE), -1, np.int32)
+    table[0, :2] = 0, 1
+    L = dev(np.array([n], np.int32))
+    q = draw((n, 2, dim), 3, "bf16").cuda()
+    ws = qe.workspace(qe.kv_attn_workspace_size(n, 1, n, 2, 1, dim), "cuda")
+    out = qe.kv_attn(q, pages, dev(table), L, group=32, ws=ws)
+    assert qe.sync_status(ws) == 0
+    assert bool(torch.isfinite(out[:40]).all()) and bool(torch.isfinite(out[40:, :, :32]).all())
+    assert bool(torch.isnan(out[40:, :, 32:]).all())
+    table[0, 0] = -1
+    out = qe.kv_attn(q, pages, dev(table), L, group=32, ws=ws)
+    assert qe.sync_status(ws) == qe.QE_ERR_ARG
+    seen = [f64(x)[32:40] for x in qe.kv_read(pages, torch.arange(n, device="cuda"), dim, group=32)]
+    assert not bool(out[:32].any())
+    check(out[32:40], None, q[32:40], [seen], [8], dim ** -0.5, "bf16")
 
 
 def many_rows(kv, lens, nqs, group, dim):
