@@ -416,8 +416,10 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  * scaled by a power of two and rounded to fp16 (exact for fp16 and bf16 inputs up to
  * 2^-25 of the row's largest value; fp32 rows and their probabilities are split into two
  * fp16 parts each), probabilities times value scales are rounded to fp16 (to 2^-11 of
- * themselves, or 2^-35 of the largest such product where that is more); statistics and
- * sums are fp32.
+ * themselves, or 2^-35 of the largest such product of the row and channel group where that
+ * is more, or 2^-145); statistics and sums are fp32.  Scores whose sum over d of |q_d| times the key
+ * scales passes fp32's largest number with the largest |q_d| taken as 2^15 are infinite (keys from about
+ * 1e31 on).
  * max_q: at least every nq.  batch * kv_heads * (max_q * heads / kv_heads / 16 + 1) above 2^23 is
  * QE_ERR_UNSUPPORTED.  Lengths past width * page, queries past `total` or max_q and
  * page numbers outside of the cache set QE_ERR_ARG in the workspace's status word (which

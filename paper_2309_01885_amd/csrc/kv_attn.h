@@ -31,6 +31,7 @@ typedef uint32_t u32x3a4 __attribute__((ext_vector_type(3), aligned(4)));
 constexpr int kKvWaves = 4;                 // waves of a workgroup
 constexpr float kKvInf = __builtin_inff();
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kKvUnit = 120.f, kKvLag = 60.f;   // of KvSums: the largest exponent of unit; what a maximum may lag behind
 
 // How a call is cut into workgroups.  A unit is a tile of `rows` query rows (row = query *
 // heads per key head + head in the group) of one sequence and key head; each unit has
@@ -38,8 +39,8 @@ constexpr float kLog2e = 1.44269504088896341f;
 struct KvPlan {
     int64_t row_tiles, units;               // units of a sequence and key head; of the call
     int nsplit, rows, rows_log2, per;       // per: heads of a key head
-    float* part;                            // nsplit > 1: (unit, split, row, DP) sums relative to the maximum
-    float* stat;                            // (unit, split, row, 2): maximum (log2) and mass
+    float* part;                            // nsplit > 1: (unit, split, row, DP) sums divided by the split's mass
+    float* stat;                            // (unit, split, row, 2): a mass f 2^(e + kKvJoinLog2) as e and f
 };
 
 // What a workgroup works on; the join recomputes it.
@@ -60,6 +61,9 @@ struct KvUnit {
 // more than the join costs (a record takes a wave about 1.3 us, the join with its launch 6 us).
 constexpr int kKvMinRecords = 4, kKvSplitFrom = 20;
 constexpr int kKvFewSplits = 8;
+// Masses reach the join as f 2^(e + kKvJoinLog2), f in [2^-12, 2^-11): neither the sum of as many of them as there
+// are splits (kFill doubled at most) nor that of the parts that they weigh overflows.
+constexpr int kKvJoinLog2 = 12;
 
 // A value that is the same for the whole workgroup and not written by the kernel: a scalar load.
 __device__ inline int kv_scalar(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)p; }
@@ -174,15 +178,31 @@ __device__ inline uint32_t kv_pack(float a, float b)
 }
 __device__ inline f32x4 kv_mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-__device__ inline float kv_max4(float x)    // over the four lanes of a query
+// Over the four lanes of a query, 16 apart.  The swap instructions exchange rows of 16 (or halves of 32) lanes of two
+// copies of x, after which the two hold a lane's own value and its partner's.  (With exchanges through
+// LDS one token over 500 of 8 key heads took 9.4 us, with these 9.1.)
+__device__ inline float kv_swap(float x, int by, float& other)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    const uint32_t u = __float_as_uint(x);
+    const auto r = by == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    other = __uint_as_float(r[1]);
+    return __uint_as_float(r[0]);
+}
+__device__ inline float kv_max4(float x)
+{
+    float y;
+    x = kv_swap(x, 16, y);
+    x = fmaxf(x, y);
+    x = kv_swap(x, 32, y);
+    return fmaxf(x, y);
 }
 __device__ inline float kv_sum4(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    float y;
+    x = kv_swap(x, 16, y);
+    x += y;
+    x = kv_swap(x, 32, y);
+    return x + y;
 }
 
 // Channels a lane's words are made of.  A key word is an octet: row `token`, octet 4 c + j.  A
@@ -343,13 +363,20 @@ template <int NC, int NT, int PARTS> struct KvRows {
 };
 
 // The running softmax and the weighted sums of a wave's rows, o[t][k][n][e]: class k, row 4 j + e of tile t.
-// Probabilities are kept as p 2^shift, shift one number for all rows that brings the product with
-// the largest value scale so far to [2^10, 2^11): 2^15 at most, since p reaches 2^4 before the
-// maximum moves.  It drops out of o / mass.
-template <int UT, int CL, int NT> struct KvSums {
+// A probability is p = 2^(score - top), top an integer that the row's scores pass by kKvLag at most.  The fp16
+// weights of a row and channel group are p s' 2^e (unit: 2^e).  e is the row's and the group's own, so that
+// what other rows see and other channels hold takes no bits from them: when it is set, the largest product so
+// far lies in [2^10, 2^12); it is lowered where a product could pass fp16's range.  When top moves by d, e follows by d
+// and the sums stay as they are, up to e = kKvUnit (value scales below 2^-109 lose bits); what p times unit can be is
+// finite, so that it is 0 for a token that the row does not see, whatever its scale.  Factors are powers of two.
+// (One exponent for a wave, from the value scales of all tokens read, was faster: 648 against 682 us, 2048
+// queries over 16384 tokens of 32 heads of 128, 32 against 37 with five fp32 chunks and slopes.  But a row lost
+// its bits to a large value that it does not see: 3e-5 of an fp32 result to one 2^20 times the others, all
+// of it from 2^37 times on.)
+template <class T, int NT> struct KvSums {
+    static constexpr int UT = T::UT, CL = T::CL, NG = T::NG;
     f32x4 o[UT][CL][NT];
-    float top[NT], mass[NT];
-    float shift, limit;                     // limit: the largest value scale that fits shift
+    float top[NT], mass[NT], unit[NT][NG];
 
     __device__ void clear()
     {
@@ -361,41 +388,69 @@ template <int UT, int CL, int NT> struct KvSums {
                 for (int k = 0; k < CL; ++k) o[t][k][n] = f32x4{0.f, 0.f, 0.f, 0.f};
             top[n] = -kKvInf;
             mass[n] = 0.f;
-        }
-        shift = 0.f;
-        limit = 0.f;
-    }
-    // Moves the maxima and the shift, and the sums with them, where a row's maximum (at: a lane's) or a
-    // value scale (big: a lane's largest) is out of range.
-    __device__ void move(const float (&at)[NT], float big)
-    {
-        bool out = big > limit;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) out = out || at[n] > top[n] + 4.f;
-        if (!__any(out)) return;
-        big = fmaxf(kv_max4(big), limit);
-        const int e = __builtin_amdgcn_readfirstlane(__float_as_int(big)) >> 23, ex = e < 77 ? 77 : e;   // (shift at most 60)
-        const float to = (float)(137 - ex), g = limit == 0.f ? 1.f : __builtin_amdgcn_exp2f(to - shift);
-        limit = __int_as_float(ex << 23 | 0x7fffff);
-        shift = to;
+            for (int g = 0; g < NG; ++g) unit[n][g] = 1.f;
+        }
+    }
+    __device__ static float exponent(float x) { return (float)((int)(__float_as_uint(x) >> 23) - 127); }
+    // Moves the maxima and the units where a row's maximum (at: a lane's, in powers of two) or a weight (big: a lane's
+    // largest value scales, seen or not: the products themselves are compared only then) is out of range.
+    // s c: the scores.
+    template <int KR, class F> __device__ void move(const float (&at)[NT], const float (&c)[NT], const float (&big)[NG], const float (&s)[KR][NT][8], F scales)
+    {
+        bool out = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float m = kv_max4(fmaxf(top[n], at[n]));
-            const float f = m == top[n] ? g : g * __builtin_amdgcn_exp2f(top[n] - m);
+            const float p = __builtin_amdgcn_exp2f(at[n] - top[n]);          // (NaN: nothing seen so far, nor here)
+            out = out || at[n] > top[n] + kKvLag;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) out = out || p * unit[n][g] * big[g] > 65000.f;
+        }
+        if (!__any(out)) return;
+        float y[NT][NG];                                                     // the largest products of the records, 127 more than their logarithms
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) y[n][g] = -kKvInf;
+#pragma unroll
+            for (int r = 0; r < KR; ++r) {
+                float sv[8];
+                scales(r, g, sv);
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)                             // (a number's bits are its logarithm, to 0.09, plus 127)
+                        y[n][g] = fmaxf(y[n][g], fmaf(s[r][n][x], c[n], (float)(int)__float_as_uint(sv[x]) * 0x1p-23f));
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float m = __builtin_ceilf(kv_max4(fmaxf(top[n], at[n])));
+            const bool first = top[n] == -kKvInf;
+            const float d = m == top[n] ? 0.f : m - top[n];
+            mass[n] *= __builtin_amdgcn_exp2f(-d);
             top[n] = m;
-            mass[n] *= f;
 #pragma unroll
-            for (int t = 0; t < UT; ++t)
+            for (int g = 0; g < NG; ++g) {
+                const float keep = first ? kKvUnit : exponent(unit[n][g]) + d;
+                const float e = fminf(fminf(keep, kKvUnit), __builtin_ceilf(137.f - (kv_max4(y[n][g]) - m)));
+                const float f = first ? 1.f : __builtin_amdgcn_exp2f(e - keep);
+                unit[n][g] = __uint_as_float((uint32_t)((int)fmaxf(e, -kKvUnit) + 127) << 23);
 #pragma unroll
-                for (int k = 0; k < CL; ++k)
+                for (int t = 0; t < UT; ++t) {
+                    if (T::group_of(t) != g) continue;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[t][k][n][e] *= f;
+                    for (int k = 0; k < CL; ++k)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) o[t][k][n][x] *= f;
+                }
+            }
         }
     }
     // Where some row does not see a token (its score s is -inf), a NaN scale of that token would meet a
     // probability of 0.  Such scales are to be taken as 0 (the result), and the sums of the rows and
     // groups that do see one become NaN here.
-    template <class T, int KR, int NG, class F> __device__ bool meet_nans(const float (&s)[KR][NT][8], F scales)
+    template <int KR, class F> __device__ bool meet_nans(const float (&s)[KR][NT][8], F scales)
     {
         float sum = 0.f;
 #pragma unroll
@@ -433,20 +488,20 @@ template <int UT, int CL, int NT> struct KvSums {
         }
         return true;
     }
-    // s: the products times their key scales, of KR records that start at tokens t0; on return p 2^shift
-    // (0 where the row sees nothing).  masked: some row does not see all of them.  scales(y, g, x) gives
+    // s: the products times their key scales, of KR records that start at tokens t0; on return the probabilities
+    // (0 where the row does not see the token).  masked: some row does not see all of them.  scales(y, g, x) gives
     // the lane's value scales; clear() is called if NaNs among them are to be taken as 0.
-    template <class T, int KR, int NG, int NC, int PARTS, class F, class C>
+    template <int KR, int NC, int PARTS, class F, class C>
     __device__ void weigh(float (&s)[KR][NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, const int (&t0)[KR], bool masked, F scales, C clear)
     {
-        float big = 0.f;
+        float big[NG];
 #pragma unroll
         for (int y = 0; y < KR; ++y)
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 float sv[8];
                 scales(y, g, sv);
-                big = fmaxf(big, kv_max8(sv));
+                big[g] = y == 0 ? kv_max8(sv) : fmaxf(big[g], kv_max8(sv));
             }
         float at[NT], c[NT];
 #pragma unroll
@@ -474,12 +529,12 @@ template <int UT, int CL, int NT> struct KvSums {
                 }
                 c[n] = 1.f;
             }
-            if (masked && meet_nans<T, KR, NG>(s, scales)) clear();
+            if (masked && meet_nans<KR>(s, scales)) clear();
         }
-        move(at, big);
+        move<KR>(at, c, big, s, scales);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float off = top[n] == -kKvInf ? 0.f : shift - top[n];     // (nothing seen so far: every s is -inf)
+            const float off = top[n] == -kKvInf ? 0.f : -top[n];            // (nothing seen so far: every s is -inf)
 #pragma unroll
             for (int y = 0; y < KR; ++y) {
                 float (&x)[8] = s[y][n];
@@ -490,14 +545,14 @@ template <int UT, int CL, int NT> struct KvSums {
         }
     }
     // The products' fp16 weights p s' of a group.
-    template <int PARTS> __device__ static void weights(const float (&s)[NT][8], const float (&sv)[8], f16x8 (&pr)[PARTS][NT])
+    template <int PARTS> __device__ void weights(const float (&s)[NT][8], int g, const float (&sv)[8], f16x8 (&pr)[PARTS][NT]) const
     {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             uint32_t h[4], m[4];
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                float x0 = s[n][2 * p] * sv[2 * p], x1 = s[n][2 * p + 1] * sv[2 * p + 1];
+                float x0 = s[n][2 * p] * unit[n][g] * sv[2 * p], x1 = s[n][2 * p + 1] * unit[n][g] * sv[2 * p + 1];
                 // (one rounded product for both parts: fused into the first part's conversion only, it made
                 // the parts miss each other by a step of fp16 once in some thousand)
                 if (PARTS == 2) asm("" : "+v"(x0), "+v"(x1));
@@ -521,12 +576,17 @@ template <int UT, int CL, int NT> struct KvSums {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) asm("" : "+v"(o[t][k][n]));
     }
-    // Calls f with the channel and the values of each octet of channels of tile n that ends up in this lane.
-    template <class T, class F> __device__ void octets(int n, F f)
+    // Calls f with the channel and the values, times `by` (relative to top), of each octet of channels of tile n that ends
+    // up in this lane.
+    template <class F> __device__ void octets(int n, float moved, float by, F f)
     {
         const int j = (threadIdx.x & 63) >> 4;
+        float to[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) to[g] = __builtin_amdgcn_exp2f(moved - exponent(unit[n][g])) * by;
 #pragma unroll
         for (int t = 0; t < UT; ++t) {
+            const float of = to[T::group_of(t)];
             float x[8];
             if constexpr (T::kHalf) {
                 // rows 0 .. 7 (lanes j < 2) hold classes 0 and 1 of a unit, rows 8 .. 15 classes 2 and 3
@@ -537,8 +597,8 @@ template <int UT, int CL, int NT> struct KvSums {
                     for (int k = 0; k < 2; ++k) {
                         const float own = up ? o[t][k][n][2 + e] : o[t][k][n][e], give = up ? o[t][k][n][e] : o[t][k][n][2 + e];
                         const float got = __shfl_xor(give, 32);
-                        x[4 * e + k] = up ? got : own;
-                        x[4 * e + 2 + k] = up ? own : got;
+                        x[4 * e + k] = (up ? got : own) * of;
+                        x[4 * e + 2 + k] = (up ? own : got) * of;
                     }
                 f(32 * t + 16 * (j & 1) + (up ? 8 : 0), x);
             } else {
@@ -547,15 +607,14 @@ template <int UT, int CL, int NT> struct KvSums {
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[4 * e + k] = o[t][k][n][2 * y + e];
+                        for (int k = 0; k < 4; ++k) x[4 * e + k] = o[t][k][n][2 * y + e] * of;
                     const int d = 64 * t + 16 * j + 8 * y;
                     if (T::kWhole || d < T::kWidth) f(d, x);
                 }
             }
         }
     }
-    // after the last record: plain sums (odd classes were 16 times as large), the rows' masses.  What is
-    // left of shift is a factor of both.
+    // after the last record: plain sums (odd classes were 16 times as large), the rows' masses
     __device__ void finish()
     {
 #pragma unroll
@@ -571,10 +630,10 @@ template <int UT, int CL, int NT> struct KvSums {
     }
 };
 
-// A lane's value scales of KR records.  Up to two groups are kept in registers; more are read from LDS where they
-// are used (held, they were 64 registers with eight groups).
+// A lane's value scales of KR records.  Up to two of a lane's sets of eight are kept in registers; more are read from LDS
+// where they are used (held, they were 64 registers with eight groups).
 template <int KR, int NG> struct KvScales {
-    static constexpr bool kKept = NG <= 2;
+    static constexpr bool kKept = KR * NG <= 2;
     float s[kKept ? KR : 1][kKept ? NG : 1][8];
     const float* at[kKept ? 1 : KR];                             // group 0's; the others' are `step` floats apart
     int step;
@@ -734,7 +793,7 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     }
     KvRows<NC, NT, PARTS> rows;
     rows.load(a, u, u.tile_row);
-    KvSums<UT, CL, NT> sums;
+    KvSums<T, NT> sums;
     sums.clear();
 
     int t0 = first_token(r);
@@ -779,13 +838,13 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
         }
         KvScales<1, NG> sv;
         sv.load([&](int, int g) { return &held.s[g][32 + 8 * j]; });
-        sums.template weigh<T, 1, NG>(s, rows, a.slopes != nullptr, at, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
+        sums.template weigh<1>(s, rows, a.slopes != nullptr, at, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             f16x8 pr[PARTS][NT];
             float x[8];
             sv.get(0, g, x);
-            sums.template weights<PARTS>(s[0], x, pr);
+            sums.template weights<PARTS>(s[0], g, x, pr);
             const u32x4 lo = *reinterpret_cast<const u32x4*>(&held.lo[g][32 + 8 * j]), hi = *reinterpret_cast<const u32x4*>(&held.hi[g][32 + 8 * j]);
 #pragma unroll
             for (int t = 0; t < UT; ++t) {
@@ -815,15 +874,15 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
     }
     sums.finish();
 
-    // every wave to the common maximum (and shift), then sums over the waves
+    // every wave to the common maximum, divided by the common mass (sums of large values would pass the
+    // largest number before it), then sums over the waves
     __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT], rtop[16 * NT], rmass[16 * NT];
     auto& acc = shared.acc;                                      // (written after a barrier that ends the use of the words)
-    const float back = __builtin_amdgcn_exp2f(-sums.shift);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
         if (j == 0) {
             wtop[wave][16 * n + i] = sums.top[n];
-            wmass[wave][16 * n + i] = sums.mass[n] * back;
+            wmass[wave][16 * n + i] = sums.mass[n];
         }
     __syncthreads();
 #pragma unroll
@@ -840,11 +899,9 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
             rtop[16 * n + i] = m;
             rmass[16 * n + i] = l;
         }
-        const float f = m == sums.top[n] ? back : __builtin_amdgcn_exp2f(sums.top[n] - m) * back;
-        sums.template octets<T>(n, [&](int d, const float* x) {
+        sums.octets(n, m == sums.top[n] ? 0.f : sums.top[n] - m, l == 0.f ? 0.f : 1.f / l, [&](int d, const float* x) {
 #pragma unroll
-            for (int y = 0; y < 8; y += 4)
-                *reinterpret_cast<f32x4*>(&acc[wave][16 * n + i][d + y]) = f32x4{x[y] * f, x[y + 1] * f, x[y + 2] * f, x[y + 3] * f};
+            for (int y = 0; y < 8; y += 4) *reinterpret_cast<f32x4*>(&acc[wave][16 * n + i][d + y]) = f32x4{x[y], x[y + 1], x[y + 2], x[y + 3]};
         });
     }
     __syncthreads();
@@ -865,14 +922,15 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
 #pragma unroll
             for (int y = 0; y < 2; ++y) *reinterpret_cast<f32x4*>(plan.part + slot * DP + d + 4 * y) = sum[y];
             if (d == 0) {
-                plan.stat[2 * slot] = m;
-                plan.stat[2 * slot + 1] = l;
+                const int e = (int)(__float_as_uint(l) >> 23) - 127;      // (of no mass: m is -inf)
+                plan.stat[2 * slot] = m + (float)e;
+                plan.stat[2 * slot + 1] = l * __uint_as_float((uint32_t)(127 - kKvJoinLog2 - e) << 23);
             }
         } else {
             const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
             float out[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = l == 0.f ? 0.f : sum[e >> 2][e & 3] / l;
+            for (int e = 0; e < 8; ++e) out[e] = sum[e >> 2][e & 3];
             if (d < a.c.dim) kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, out);
             if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
         }
@@ -897,6 +955,10 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     using T = KvTiles<DP, GROUP>;
     constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
     constexpr int KR = kv_stage_records(DP), W = kKvWaves / KR;  // records of a stage, waves that convert one
+    // Records whose exponentials are taken together: all of a stage, where the registers hold them.  Two tiles
+    // of two groups spill (2048 queries of 32 heads of 128 in groups of 64 over 8192 tokens: 560 us
+    // together, 433 one by one; groups of 128 694 / 735, 64 channels in groups of 64 269 / 282).
+    constexpr int KW = NG == 2 && NT == 2 && DP > 64 ? 1 : KR;
     constexpr int CW = KR == 2 ? NC : (NC + 1) / 2;              // key products a wave converts
     constexpr int VW = T::kHalf ? (UT + 1) / 2 : UT, VK = KR;    // unit tiles and classes
     constexpr int SW = KR == 2 ? (NG + 1) / 2 : (NG + 3) / 4;    // scales a lane converts
@@ -1008,8 +1070,8 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
             const bool key = KR == 2 ? kh == 0 : lane < 32;
             const int g = KR == 2 ? (lane >> 5) + 2 * x : q + 4 * x;
             float sc = kv_scale(word[x]);
-            // (words past the sequence's end are anything: no scale of theirs may meet a 0)
-            sc = !key && (r + part) * kKvTok + (lane & 31) >= u.len ? 0.f : sc;
+            // (words past the sequence's end, or of a record that is not there, are anything: no scale of theirs may meet a 0)
+            sc = !key && (!here || (r + part) * kKvTok + (lane & 31) >= u.len) ? 0.f : sc;
             (key ? st.ks : st.vs)[part][g][lane & 31] = sc;
         }
         // (past the last record, or on a page that is not there: past every sequence's end)
@@ -1019,7 +1081,7 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     if (r0 < r1) start();
     KvRows<NC, NT, PARTS> rows;
     rows.load(a, u, min(row0, u.rows - 1));
-    KvSums<UT, CL, NT> sums;
+    KvSums<T, NT> sums;
     sums.clear();
     if (r0 < r1) {
         convert(stage[0], r0);
@@ -1029,65 +1091,68 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     for (int r = r0, b = 0; r < r1; r += KR, b ^= 1) {
         convert(stage[b ^ 1], r + KR);
         const Stage& st = stage[b];
-        float s[KR][NT][8];
-        int t0[KR];
-        bool masked = false;
 #pragma unroll
-        for (int y = 0; y < KR; ++y) {
-            t0[y] = __builtin_amdgcn_readfirstlane(st.at[y]);
-            masked = masked || rows.masked(t0[y]);
+        for (int y0 = 0; y0 < KR; y0 += KW) {
+            float s[KW][NT][8];
+            int t0[KW];
+            bool masked = false;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                f32x4 acc[NT][2];
+            for (int y = 0; y < KW; ++y) {
+                t0[y] = __builtin_amdgcn_readfirstlane(st.at[y0 + y]);
+                masked = masked || rows.masked(t0[y]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int g = 0; g < NG; ++g) {
+                    f32x4 acc[NT][2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int c = g * T::CPG; c < (g + 1) * T::CPG && c < NC; ++c)
+                        for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const f16x8 f = st.k[y][h][c][lane];
+                    for (int c = g * T::CPG; c < (g + 1) * T::CPG && c < NC; ++c)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int h = 0; h < 2; ++h) {
+                            const f16x8 f = st.k[y0 + y][h][c][lane];
 #pragma unroll
-                            for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][c], acc[n][h]);
-                    }
-                const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[y][g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[y][g][8 * j + 4]);
+                            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                                for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][c], acc[n][h]);
+                        }
+                    const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[y0 + y][g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[y0 + y][g][8 * j + 4]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
-                        s[y][n][e] = g == 0 ? sc * x : fmaf(sc, x, s[y][n][e]);
-                    }
-            }
-        }
-        start();
-        KvScales<KR, NG> sv;
-        sv.load([&](int y, int g) { return &st.vs[y][g][8 * j]; });
-        sums.template weigh<T, KR, NG>(s, rows, a.slopes != nullptr, t0, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int y = 0; y < KR; ++y)
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                f16x8 pr[PARTS][NT];
-                float x[8];
-                sv.get(y, g, x);
-                sums.template weights<PARTS>(s[y], x, pr);
-#pragma unroll
-                for (int t = 0; t < UT; ++t) {
-                    if (T::group_of(t) != g) continue;
-#pragma unroll
-                    for (int c = 0; c < CL; ++c) {
-                        const f16x8 f = st.v[y][t][c][lane];
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int p = 0; p < PARTS; ++p) sums.o[t][c][n] = kv_mfma(f, pr[p][n], sums.o[t][c][n]);
-                    }
+                        for (int e = 0; e < 8; ++e) {
+                            const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
+                            s[y][n][e] = g == 0 ? sc * x : fmaf(sc, x, s[y][n][e]);
+                        }
                 }
             }
+            if (y0 == 0) start();
+            KvScales<KW, NG> sv;
+            sv.load([&](int y, int g) { return &st.vs[y0 + y][g][8 * j]; });
+            sums.template weigh<KW>(s, rows, a.slopes != nullptr, t0, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
+#pragma unroll
+            for (int y = 0; y < KW; ++y)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    f16x8 pr[PARTS][NT];
+                    float x[8];
+                    sv.get(y, g, x);
+                    sums.template weights<PARTS>(s[y], g, x, pr);
+#pragma unroll
+                    for (int t = 0; t < UT; ++t) {
+                        if (T::group_of(t) != g) continue;
+#pragma unroll
+                        for (int c = 0; c < CL; ++c) {
+                            const f16x8 f = st.v[y0 + y][t][c][lane];
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int p = 0; p < PARTS; ++p) sums.o[t][c][n] = kv_mfma(f, pr[p][n], sums.o[t][c][n]);
+                        }
+                    }
+                }
+        }
         sums.pin();
         __syncthreads();
     }
@@ -1096,14 +1161,10 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = row0 + 16 * n + i, qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
-        const float f = sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n];
-        sums.template octets<T>(n, [&](int d, const float* x) {
-            float out[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = f == 0.f ? 0.f : x[e] * f;
-            if (row < u.rows && d < a.c.dim) kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, out);
+        sums.octets(n, 0.f, sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n], [&](int d, const float* x) {
+            if (row < u.rows && d < a.c.dim) kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, x);
         });
-        if (row < u.rows && j == 0 && a.lse) a.lse[(u.first + qi) * a.heads + head] = kv_lse(sums.top[n] - sums.shift, sums.mass[n]);
+        if (row < u.rows && j == 0 && a.lse) a.lse[(u.first + qi) * a.heads + head] = kv_lse(sums.top[n], sums.mass[n]);
     }
 }
 
@@ -1130,8 +1191,8 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a
 #pragma unroll 4
     for (int s = wave; s < u.splits; s += kKvWaves) {
         const int64_t k = slot + (int64_t)s * plan.rows;
-        const float t = plan.stat[2 * k], f = t == m ? 1.f : __builtin_amdgcn_exp2f(t - m);
-        l = fmaf(plan.stat[2 * k + 1], f, l);
+        const float t = plan.stat[2 * k], f = plan.stat[2 * k + 1] * (t == m ? 1.f : __builtin_amdgcn_exp2f(t - m));
+        l += f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (DP % 64 == 0 || 64 * c + lane < DP) x[c] = fmaf(plan.part[k * DP + 64 * c + lane], f, x[c]);
@@ -1146,7 +1207,7 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a
     if (tid < a.c.dim)
         kv_out(a, (u.first + qi) * a.ot + head * a.oh + tid,
                l == 0.f ? 0.f : ((sum[0][tid] + sum[1][tid]) + (sum[2][tid] + sum[3][tid])) / l);
-    if (a.lse && tid == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
+    if (a.lse && tid == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m + kKvJoinLog2, l);
 }
 
 // The same for few splits (kKvFewSplits at most) of many rows: one workgroup a unit, a thread 8 channels of a row,
@@ -1180,8 +1241,8 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_unit_kernel(KvA
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 if (s0 + s >= u.splits) break;
-                const float f = st[s0 + s].x == m ? 1.f : __builtin_amdgcn_exp2f(st[s0 + s].x - m);
-                l = fmaf(st[s0 + s].y, f, l);
+                const float f = st[s0 + s].y * (st[s0 + s].x == m ? 1.f : __builtin_amdgcn_exp2f(st[s0 + s].x - m));
+                l += f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e >> 2][e & 3] = fmaf(part[s][e >> 2][e & 3], f, sum[e >> 2][e & 3]);
             }
@@ -1195,7 +1256,7 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_unit_kernel(KvA
             if (a.dtype == QE_F32) kv_out8<2>(a, to, out);
             else kv_out8<1>(a, to, out);
         }
-        if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
+        if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m + kKvJoinLog2, l);
     }
 }
 
