@@ -155,6 +155,15 @@ def workspace(nbytes: int, device) -> torch.Tensor:
     return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+def _on(stream, make):
+    """make() with `stream` as torch's current stream (None: as it is).  A call's own buffers are made there, so that
+    their filling comes before the call's work and their memory is reused after it."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
 def sync_status(ws: torch.Tensor, stream=None) -> int:
     """Waits for the stream; returns (and clears) the workspace's device status word."""
     return load().qe_sync_status(_vp(ws.data_ptr()), _stream(stream))
@@ -472,7 +481,8 @@ def kv_read(pages: torch.Tensor, slots: torch.Tensor, dim: int, group: int = 64,
             K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None,
             status: Optional[torch.Tensor] = None, stream=None):
     """The keys and values (tokens x kv_heads x dim) that the cache holds at the slots
-    (qe_kv_read); into K and V where given."""
+    (qe_kv_read); into K and V where given (otherwise they are tensors of `stream`: record_stream
+    them before they are used on another)."""
     num, page, heads, dev = _pages(pages, dim, group)
     n = slots.numel()
     shape = (n, heads, dim)
@@ -481,9 +491,9 @@ def kv_read(pages: torch.Tensor, slots: torch.Tensor, dim: int, group: int = 64,
     if dtype not in _DTYPES:
         raise ValueError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
     if K is None:
-        K = torch.empty(shape, dtype=dtype, device=pages.device)
+        K = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
     if V is None:
-        V = torch.empty(shape, dtype=dtype, device=pages.device)
+        V = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
     kt, kh = _heads(K, "K", shape, dtype, dev)
     vt, vh = _heads(V, "V", shape, dtype, dev)
     code = load().qe_kv_read(pages.data_ptr(), num, page, _flat(slots, "slots", torch.int64, dev), n, heads, dim, group,
@@ -510,7 +520,8 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
     sequences + 1) and max_q their queries, without them total / sequences queries each.
     scale: 1 / sqrt(dim) unless given.  lse: None or float32, total x heads, written.  The call does
     not wait for the device; check=True does, and raises if it met a bad page number, length or
-    query range (sync_status(ws) tells later otherwise)."""
+    query range (sync_status(ws) tells later otherwise).  An output or a workspace that the call makes is
+    a tensor of `stream`."""
     shape, dtype = Q.shape, Q.dtype
     if len(shape) != 3 or dtype not in _DTYPES:
         _bad("Q", Q, "total x heads x dim in float32, float16 or bfloat16")
@@ -528,11 +539,12 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
         raise ValueError("q_start needs max_q, the largest number of queries of a sequence")
     shape = (total, heads, dim)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=pages.device)
+        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
     qt, qh = _heads(Q, "Q", shape, dtype, dev)
     ot, oh = _heads(out, "out", shape, dtype, dev)
     if ws is None:
-        ws = workspace(kv_attn_workspace_size(total, batch, max_q, heads, kv, dim), pages.device)
+        need = kv_attn_workspace_size(total, batch, max_q, heads, kv, dim)
+        ws = _on(stream, lambda: workspace(need, pages.device))
     code = load().qe_kv_attn(Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
                              _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
                              num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
