@@ -191,10 +191,10 @@ def gram(X: torch.Tensor, layout: int = QE_LAYOUT_PN, Sigma: Optional[torch.Tens
     if bf16x3:
         layout |= QE_GRAM_BF16X3
     if Sigma is None:
-        Sigma = torch.empty((p, p), dtype=torch.float32, device=X.device)
+        Sigma = _on(stream, lambda: torch.empty((p, p), dtype=torch.float32, device=X.device))
     need = lib.qe_gram_workspace_size(p, n)
     if ws is None:
-        ws = workspace(need, X.device)
+        ws = _on(stream, lambda: workspace(need, X.device))
     _check(lib.qe_gram(_ptr(X, torch.float32, "X"), p, n, layout,
                        _ptr(Sigma, torch.float32, "Sigma", p * p), 1 if accumulate else 0,
                        float(damp), _vp(ws.data_ptr()), ws.numel(), _stream(stream)), "qe_gram")
@@ -207,8 +207,8 @@ def grid_minmax(W: torch.Tensor, bits: int, H: Optional[torch.Tensor] = None,
                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     lib = load()
     q, p = W.shape
-    scale = torch.empty(q, dtype=torch.float32, device=W.device)
-    zero = torch.empty(q, dtype=torch.float32, device=W.device)
+    scale = _on(stream, lambda: torch.empty(q, dtype=torch.float32, device=W.device))
+    zero = _on(stream, lambda: torch.empty(q, dtype=torch.float32, device=W.device))
     _check(lib.qe_grid_minmax(_ptr(W, torch.float32, "W"), _ptr(H, torch.float32, "H", q * p)
                               if H is not None else _vp(None), q, p, bits,
                               _ptr(scale, torch.float32, "scale"), _ptr(zero, torch.float32, "zero"),
@@ -228,7 +228,7 @@ def cd_sweep(W, Sigma, bits, scale, zero, W_hat, codes, R, sweeps, block: int = 
     lib = load()
     q, p = W.shape
     if ws is None:
-        ws = workspace(cd_workspace_size(q, p, block), W.device)
+        ws = _on(stream, lambda: workspace(cd_workspace_size(q, p, block), W.device))
     if obj is not None and (obj.dtype != torch.float64 or obj.numel() < sweeps):
         raise ValueError("obj must be a float64 device tensor with >= sweeps entries")
     _check(lib.qe_cd_sweep(_ptr(W, torch.float32, "W"), _ptr(Sigma, torch.float32, "Sigma", p * p),
@@ -278,7 +278,7 @@ def cd_outlier_sweep(W, Sigma, bits, scale, zero, W_hat, codes, H, E, s, lambda_
     lib = load()
     q, p = W.shape
     if ws is None:
-        ws = workspace(outlier_workspace_size(q, p, block, s), W.device)
+        ws = _on(stream, lambda: workspace(outlier_workspace_size(q, p, block, s), W.device))
     if obj is not None and (obj.dtype != torch.float64 or obj.numel() < 2 * sweeps):
         raise ValueError("obj must be a float64 device tensor with >= 2*sweeps entries")
     _check(lib.qe_cd_outlier_sweep(
@@ -300,11 +300,11 @@ def topk_abs(V: torch.Tensor, s: int, ws: Optional[torch.Tensor] = None, check: 
     """P_s(V) over all entries of V: returns (dense P_s(V), support int64[s], nnz int64[1])."""
     lib = load()
     count = V.numel()
-    out = torch.empty_like(V)
-    support = torch.zeros(max(int(s), 1), dtype=torch.int64, device=V.device)
-    nnz = torch.zeros(1, dtype=torch.int64, device=V.device)
+    out = _on(stream, lambda: torch.empty_like(V))
+    support = _on(stream, lambda: torch.zeros(max(int(s), 1), dtype=torch.int64, device=V.device))
+    nnz = _on(stream, lambda: torch.zeros(1, dtype=torch.int64, device=V.device))
     if ws is None:
-        ws = workspace(lib.qe_topk_workspace_size(count, s), V.device)
+        ws = _on(stream, lambda: workspace(lib.qe_topk_workspace_size(count, s), V.device))
     _check(lib.qe_topk_abs(_ptr(V, torch.float32, "V"), count, int(s),
                            _ptr(out, torch.float32, "out"), _vp(support.data_ptr()),
                            _ptr(nnz, torch.int64, "nnz"), _vp(ws.data_ptr()), ws.numel(),
@@ -320,12 +320,12 @@ def topk_columns(V: torch.Tensor, c: int, ws: Optional[torch.Tensor] = None,
     nnz int64[1])."""
     lib = load()
     q, p = V.shape
-    out = torch.empty_like(V)
-    cols = torch.full((max(int(c), 1),), -1, dtype=torch.int64, device=V.device)
-    support = torch.zeros(max(int(q * c), 1), dtype=torch.int64, device=V.device)
-    nnz = torch.zeros(1, dtype=torch.int64, device=V.device)
+    out = _on(stream, lambda: torch.empty_like(V))
+    cols = _on(stream, lambda: torch.full((max(int(c), 1),), -1, dtype=torch.int64, device=V.device))
+    support = _on(stream, lambda: torch.zeros(max(int(q * c), 1), dtype=torch.int64, device=V.device))
+    nnz = _on(stream, lambda: torch.zeros(1, dtype=torch.int64, device=V.device))
     if ws is None:
-        ws = workspace(lib.qe_topk_columns_workspace_size(q, p), V.device)
+        ws = _on(stream, lambda: workspace(lib.qe_topk_columns_workspace_size(q, p), V.device))
     _check(lib.qe_topk_columns(_ptr(V, torch.float32, "V"), q, p, int(c),
                                _ptr(out, torch.float32, "out"), _vp(cols.data_ptr()),
                                _vp(support.data_ptr()), _ptr(nnz, torch.int64, "nnz"),
@@ -340,8 +340,8 @@ def pack_codes(codes: torch.Tensor, bits: int, stream=None) -> torch.Tensor:
     """q x p uint8 codes -> q x qe_packed_row_bytes(p, bits) uint8 bit streams."""
     lib = load()
     q, p = codes.shape
-    out = torch.empty((q, int(lib.qe_packed_row_bytes(p, bits))), dtype=torch.uint8,
-                      device=codes.device)
+    out = _on(stream, lambda: torch.empty((q, int(lib.qe_packed_row_bytes(p, bits))), dtype=torch.uint8,
+                                          device=codes.device))
     _check(lib.qe_pack_codes(_ptr(codes, torch.uint8, "codes"), q, p, int(bits),
                              _vp(out.data_ptr()), _stream(stream)), "qe_pack_codes")
     return out
@@ -353,9 +353,9 @@ def outliers_csr(H: torch.Tensor, support: torch.Tensor, nnz: torch.Tensor, stre
     lib = load()
     q, p = H.shape
     cap = support.numel()
-    rowptr = torch.empty(q + 1, dtype=torch.int64, device=H.device)
-    cols = torch.empty(max(cap, 1), dtype=torch.int32, device=H.device)
-    vals = torch.empty(max(cap, 1), dtype=torch.float32, device=H.device)
+    rowptr = _on(stream, lambda: torch.empty(q + 1, dtype=torch.int64, device=H.device))
+    cols = _on(stream, lambda: torch.empty(max(cap, 1), dtype=torch.int32, device=H.device))
+    vals = _on(stream, lambda: torch.empty(max(cap, 1), dtype=torch.float32, device=H.device))
     _check(lib.qe_outliers_csr(_ptr(H, torch.float32, "H"), q, p,
                                _ptr(support, torch.int64, "support"), _ptr(nnz, torch.int64, "nnz"),
                                cap, _vp(rowptr.data_ptr()), _vp(cols.data_ptr()),
@@ -369,9 +369,9 @@ def objective(W, W_hat, Sigma, H: Optional[torch.Tensor] = None,
     """Device float64[2]: (||(W_hat + H - W) X||^2, ||W X||^2) through Sigma."""
     lib = load()
     q, p = W.shape
-    out = torch.zeros(2, dtype=torch.float64, device=W.device)
+    out = _on(stream, lambda: torch.zeros(2, dtype=torch.float64, device=W.device))
     if ws is None:
-        ws = workspace(lib.qe_objective_workspace_size(q, p), W.device)
+        ws = _on(stream, lambda: workspace(lib.qe_objective_workspace_size(q, p), W.device))
     _check(lib.qe_objective(_ptr(W, torch.float32, "W"), _ptr(W_hat, torch.float32, "W_hat", q * p),
                             _ptr(H, torch.float32, "H", q * p) if H is not None else _vp(None),
                             _ptr(Sigma, torch.float32, "Sigma", p * p), q, p,
@@ -387,7 +387,7 @@ def lambda_max(Sigma: torch.Tensor, max_iters: int = 500, tol: float = 1e-7,
     lib = load()
     p = Sigma.shape[0]
     if ws is None:
-        ws = workspace(lib.qe_lambda_workspace_size(p), Sigma.device)
+        ws = _on(stream, lambda: workspace(lib.qe_lambda_workspace_size(p), Sigma.device))
     out = _f32(0.0)
     _check(lib.qe_lambda_max(_ptr(Sigma, torch.float32, "Sigma", p * p), p, int(max_iters),
                              float(tol), ctypes.byref(out), _vp(ws.data_ptr()), ws.numel(),

@@ -35,3 +35,28 @@ def test_kv_attn_and_read_on_another_stream(qe):
         assert torch.equal(k, want_k) and torch.equal(v, want_v)
         out = qe.kv_attn(q, pages, T, L, stream=side, check=True)
         assert torch.equal(out, want)
+
+
+def test_quantizer_calls_on_another_stream(qe):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    W = torch.randn(96, 160, device="cuda", generator=g)
+    X = torch.randn(160, 1024, device="cuda", generator=g)
+
+    def calls(stream):
+        S = qe.gram(X, damp=0.01, stream=stream)
+        scale, zero = qe.grid_minmax(W, 4, stream=stream)
+        top = qe.topk_abs(W, 50, stream=stream)
+        cols = qe.topk_columns(W, 3, stream=stream)
+        csr = qe.outliers_csr(top[0], top[1], top[2], stream=stream)
+        obj = qe.objective(W, top[0], S, stream=stream)
+        lam = torch.tensor(qe.lambda_max(S, stream=stream))
+        return [S, scale, zero, *top, *cols, *csr, obj, lam]
+
+    want = [t.clone() for t in calls(None)]
+    side = torch.cuda.Stream()
+    for _ in range(2):
+        torch.cuda.synchronize()
+        torch.cuda._sleep(2000000)
+        got = calls(side)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

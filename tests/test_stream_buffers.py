@@ -56,3 +56,24 @@ def test_kv_calls(calls):
     assert calls["made"] == [s, s] and calls["stream"] == [77]
     Q.kv_read(pages, torch.ones(5, dtype=torch.int64), 64, stream=s)
     assert calls["made"] == [s] * 4 and calls["stream"] == [77] * 2
+
+
+def test_other_calls(calls, monkeypatch):
+    """The quantizer's calls: every buffer of theirs, too."""
+    s = Stream()
+    monkeypatch.setattr(Q, "_ptr", lambda t, *args, **kw: Q._vp(None))
+    W, S, codes = torch.ones((8, 16)), torch.ones((16, 16)), torch.ones((8, 16), dtype=torch.uint8)
+    idx, nnz, row = torch.ones(3, dtype=torch.int64), torch.ones(1, dtype=torch.int64), torch.ones(8)
+    Q.gram(W, stream=s, check=False)
+    Q.grid_minmax(W, 4, stream=s)
+    Q.cd_sweep(W, S, 4, row, row, W, codes, W, 1, stream=s, check=False)
+    Q.cd_outlier_sweep(W, S, 4, row, row, W, codes, W, W, 3, 1.0, idx, nnz, 1, stream=s, check=False)
+    Q.topk_abs(W, 3, stream=s, check=False)
+    Q.topk_columns(W, 3, stream=s, check=False)
+    Q.pack_codes(codes, 4, stream=s)
+    Q.outliers_csr(W, idx, nnz, stream=s)
+    Q.objective(W, W, S, stream=s, check=False)
+    Q.lambda_max(S, stream=s)
+    assert len(calls["made"]) == 2 + 2 + 1 + 1 + 4 + 5 + 1 + 3 + 2 + 1
+    assert all(m is s for m in calls["made"]), calls["made"]
+    assert calls["stream"] == [77] * 10
