@@ -373,7 +373,8 @@ qe_status qe_outliers_csr(const float* H, int64_t q, int64_t p, const int64_t* s
  *
  * dtype of K, V, Q, out: QE_F32, QE_F16 or QE_BF16; a head's dim channels are
  * contiguous, tokens and heads lie at the given strides (in elements; an output's
- * elements must not overlap).
+ * elements must not overlap).  Pointers are multiples of their elements' size, pages and the
+ * workspace of 16 (QE_ERR_ARG otherwise).
  * ------------------------------------------------------------------------ */
 #define QE_F32  0
 #define QE_F16  1

@@ -371,6 +371,7 @@ qe_status qe_kv_write(const void* K, const void* V, int dtype, int64_t tokens, i
     if (tokens == 0) return QE_OK;
     if (!K || !V || !slots || !pages || misaligned(pages, 16)) return QE_ERR_ARG;
     if (misaligned(K, dtype_bytes(dtype)) || misaligned(V, dtype_bytes(dtype))) return QE_ERR_ARG;
+    if (misaligned(slots, 8) || misaligned(status, 4)) return QE_ERR_ARG;
     const int64_t strides[4] = {k_stride, k_head_stride, v_stride, v_head_stride};
     return launch_kv_write(K, V, dtype, strides, slots, tokens, kv_cache(pages, num_pages, page, kv_heads, dim), group,
                            status, as_stream(stream));
@@ -384,6 +385,7 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
     if (tokens == 0) return QE_OK;
     if (!K || !V || !slots || !pages || misaligned(pages, 16)) return QE_ERR_ARG;
     if (misaligned(K, dtype_bytes(dtype)) || misaligned(V, dtype_bytes(dtype))) return QE_ERR_ARG;
+    if (misaligned(slots, 8) || misaligned(status, 4)) return QE_ERR_ARG;
     const int64_t strides[4] = {k_stride, k_head_stride, v_stride, v_head_stride};
     return launch_kv_read(kv_cache(pages, num_pages, page, kv_heads, dim), group, slots, tokens, K, V, dtype, strides,
                           status, as_stream(stream));
@@ -414,6 +416,9 @@ qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim
     if (total == 0 || batch == 0 || max_q == 0) return QE_OK;
     if (!Q || !pages || !lengths || !out || (width > 0 && !table) || misaligned(pages, 16)) return QE_ERR_ARG;
     if (misaligned(Q, dtype_bytes(dtype)) || misaligned(out, dtype_bytes(dtype))) return QE_ERR_ARG;
+    for (const void* p : {(const void*)q_start, (const void*)table, (const void*)lengths, (const void*)slopes, (const void*)lse})
+        if (misaligned(p, 4)) return QE_ERR_ARG;
+    if (misaligned(ws, 16)) return QE_ERR_ARG;            // (16-byte accesses, and an atomic on the status word)
     if (!ws || ws_bytes < qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim)) return QE_ERR_WORKSPACE;
     KvAttn a{};
     a.c = kv_cache(pages, num_pages, page, kv_heads, dim);
