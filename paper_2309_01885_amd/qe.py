@@ -518,7 +518,7 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
 
     table (int32, sequences x pages) and lengths (int32) describe the sequences; q_start (int32,
     sequences + 1) and max_q their queries, without them total / sequences queries each.
-    scale: 1 / sqrt(dim) unless given.  lse: None or float32, total x heads, written.  The call does
+    scale: 1 / sqrt(dim) unless given.  window: 0 for none; one wider than every sequence hides nothing.  lse: None or float32, total x heads, written.  The call does
     not wait for the device; check=True does, and raises if it met a bad page number, length or
     query range (sync_status(ws) tells later otherwise).  An output or a workspace that the call makes is
     a tensor of `stream`."""
@@ -538,6 +538,8 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
     elif max_q is None:
         raise ValueError("q_start needs max_q, the largest number of queries of a sequence")
     shape = (total, heads, dim)
+    if not -0x80000000 <= window <= 0x7fffffff:      # (a C int would take its low bits: 2^32 as no window)
+        window = 0x7fffffff if window > 0 else -1
     if out is None:
         out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
     qt, qh = _heads(Q, "Q", shape, dtype, dev)
