@@ -258,7 +258,7 @@ template <int NC, int NT, int PARTS> struct KvRows {
     f16x8 q[PARTS][NT][NC];
     float c[NT], slope[NT];                 // score of a product: c s + slope (t - pos), in powers of two
     int lo[NT], hi[NT];                     // the tokens that the lane's row sees
-    int all_lo, all_hi, any_lo, any_hi;     // that every row and that some row of the wave sees
+    int all_lo, all_hi;                     // that every row of the wave sees
 
     // A row is scaled by 2^e to a largest element in [2^14, 2^15) and rounded to fp16.
     __device__ void load(const KvAttn& a, const KvUnit& u, int row0)
@@ -346,17 +346,13 @@ template <int NC, int NT, int PARTS> struct KvRows {
             hi[n] = have && a.causal ? (int)max((int64_t)0, pos + 1) : u.len;
             lo[n] = have && a.window ? (int)max((int64_t)0, pos - a.window + 1) : 0;
         }
-        all_lo = any_lo = 0;
-        all_hi = any_hi = u.len;
+        all_lo = 0;
+        all_hi = u.len;
         if (a.causal) {
             // the first and the last row bound the others
             const int64_t p0 = u.pos0 + row0 / u.per, p1 = u.pos0 + (min(u.rows, row0 + 16 * NT) - 1) / u.per;
             all_hi = (int)max((int64_t)0, p0 + 1);
-            any_hi = (int)max((int64_t)0, p1 + 1);
-            if (a.window) {
-                any_lo = (int)max((int64_t)0, p0 - a.window + 1);
-                all_lo = (int)max((int64_t)0, p1 - a.window + 1);
-            }
+            if (a.window) all_lo = (int)max((int64_t)0, p1 - a.window + 1);
         }
     }
     __device__ bool masked(int t0) const { return t0 > all_hi - kKvTok || t0 < all_lo; }
