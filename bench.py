@@ -53,15 +53,22 @@ KERNEL_SOURCES = {
 
 
 def kernel_source_hash(kernel):
-    """sha256 over the HIP sources `kernel` is compiled from (and the ABI header)."""
+    """sha256 over the HIP sources `kernel` is compiled from and what they use of the ABI header: the
+    macros whose names they contain.  (Declarations and comments of other calls change no kernel.)"""
     import hashlib
     h = hashlib.sha256()
-    files = [os.path.join(ROOT, "paper_2309_01885_amd", "csrc", f) for f in KERNEL_SOURCES[kernel]]
-    files.append(os.path.join(ROOT, "include", "qe.h"))
-    for path in files:
-        h.update(os.path.basename(path).encode())
-        with open(path, "rb") as f:
-            h.update(f.read())
+    text = ""
+    for name in KERNEL_SOURCES[kernel]:
+        with open(os.path.join(ROOT, "paper_2309_01885_amd", "csrc", name), encoding="utf-8") as f:
+            body = f.read()
+        h.update((name + "\n" + body).encode())
+        text += body
+    with open(os.path.join(ROOT, "include", "qe.h"), encoding="utf-8") as f:
+        header = re.sub(r"/\*.*?\*/", " ", f.read(), flags=re.S).replace("\\\n", " ")
+    used = set(re.findall(r"\bQE_\w+", text))
+    for name, rest in re.findall(r"^[ \t]*#define[ \t]+(\w+)(.*)$", header, re.M):
+        if name in used:
+            h.update(f"{name} {' '.join(rest.split())}\n".encode())
     return h.hexdigest()
 
 
