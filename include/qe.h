@@ -412,7 +412,8 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  *   scale q . k_t + slopes[h] (t - pos)       (slopes NULL: without the last term;
  *                                              causal only).
  * A row that sees no token is 0, its lse -infinity.  lse: NULL or total x heads floats
- * (device): the natural logarithm of the softmax's denominator.
+ * (device): the natural logarithm of the softmax's denominator.  Rows of Q that are no
+ * sequence's (before q_start[0], from q_start[batch] on) are neither read nor written.
  * Products run on the fp16 matrix cores: codes are exact there, a query row is
  * scaled by a power of two and rounded to fp16 (exact for fp16 and bf16 inputs up to
  * 2^-25 of the row's largest value; fp32 rows and their probabilities are split into two
@@ -424,7 +425,11 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  * max_q: at least every nq.  batch * kv_heads * (max_q * heads / kv_heads / 16 + 1) above 2^23 is
  * QE_ERR_UNSUPPORTED.  Lengths past width * page, queries past `total` or max_q and
  * page numbers outside of the cache set QE_ERR_ARG in the workspace's status word (which
- * this call never clears; qe_sync_status does) and count as absent. */
+ * this call never clears; qe_sync_status does) and count as absent.
+ * The lengths are known to the device alone: the work is cut into splits along the tokens, and
+ * tiles are chosen, for sequences that fill the table (or the window).  A table much wider than its
+ * sequences costs a small call workgroups without work and the launch that joins splits.  Few
+ * rows take more splits, so a smaller call may need a larger workspace: ask for each. */
 size_t qe_kv_attn_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads,
                                  int dim);
 qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,

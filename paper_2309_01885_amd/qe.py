@@ -521,7 +521,9 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
     scale: 1 / sqrt(dim) unless given.  window: 0 for none; one wider than every sequence hides nothing.  lse: None or float32, total x heads, written.  The call does
     not wait for the device; check=True does, and raises if it met a bad page number, length or
     query range (sync_status(ws) tells later otherwise).  An output or a workspace that the call makes is
-    a tensor of `stream`."""
+    a tensor of `stream`; rows of it that are no sequence's are not written.  The kernels cut their work for
+    sequences that fill the table, so a table much wider than they are costs time.  No gradient:
+    the output has no graph."""
     shape, dtype = Q.shape, Q.dtype
     if len(shape) != 3 or dtype not in _DTYPES:
         _bad("Q", Q, "total x heads x dim in float32, float16 or bfloat16")
