@@ -18,10 +18,13 @@ namespace {
 // 400 workgroups of uneven lengths 56 / 32; 2048 queries of 32 heads over 16384 tokens 681 / 802.
 // 256 channels in groups of 32 do not fit the few-row form's registers: 256 workgroups 293 / 378.
 constexpr int64_t kManyRows = 128, kManyFill = 512, kManyFillWide = 128;
-// Workgroups of the few-row form that fill the chip, three of a CU.  Twice as many where there
-// are enough sequences for their lengths to differ: the long ones are not left to the end (64
-// sequences of 2048 to 8192 tokens 89 -> 80 us; two of the same length 111 -> 118).
-constexpr int64_t kFill = 768, kUneven = 8;
+// Workgroups of the few-row form that fill the chip, three of a CU.  Units that are more than half of that would not be
+// split; they are, in two or three, where each has kSplitLong records (8192 tokens) or more: the last ones, or the
+// long ones, are not left to the end.  29 query heads on one of 64 channels, us with 768 / 1536 workgroups:
+// 8192 tokens (2048 to 8192): 128 units 36 / 46 (32 / 41), 256 59 / 64 (50 / 51), 400 106 / 90 (91 / 73), 512 107 / 107
+// (93 / 88), 640 136 / 128 (106 / 102), 768 139 / 150 (116 / 119); 4096 tokens (1024 to 4096): 448 54 / 61 (49 / 47),
+// 512 58 / 64 (48 / 52); 16384 tokens (4096 to 16384): 400 196 / 156 (173 / 125), 640 263 / 233 (198 / 180).
+constexpr int64_t kFill = 768, kSplitLong = 256;
 // Records (32 tokens of one head for one unit) from which the few-row form takes 32 rows a unit
 // instead of 16: a record's codes are then converted for twice the rows, but by half as many workgroups.
 // 128 channels, 32 against 16 rows, in us: 256 units of 64 records 38 / 33, 1024 of 32 42 / 44, 256
@@ -36,10 +39,10 @@ KvForm form_of(int64_t heads, int64_t rows, int64_t records, int dp, int group, 
 }
 
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
-int splits_of(KvForm form, int64_t units, int64_t batch, int64_t records)
+int splits_of(KvForm form, int64_t units, int64_t records)
 {
     if (form.many || records < kKvSplitFrom) return 1;
-    const int64_t fill = batch < kUneven ? kFill : 2 * kFill;
+    const int64_t fill = units > kFill / 2 && units < kFill && records >= kSplitLong ? 2 * kFill : kFill;
     return (int)std::max<int64_t>(1, std::min(fill / std::max<int64_t>(units, 1), records / kKvMinRecords));
 }
 
@@ -73,7 +76,7 @@ size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, i
     for (int64_t records : {(int64_t)1, (int64_t)INT32_MAX}) {
         for (int f32 = 0; f32 < 2; ++f32) {
             const Sizes z = sizes_of(batch, max_q, heads, kv_heads, dim, 128, records, f32 != 0);
-            const int nsplit = splits_of(z.form, z.units, batch, INT32_MAX);
+            const int nsplit = splits_of(z.form, z.units, INT32_MAX);
             if (nsplit > 1)
                 need = std::max(need, align256(part_floats(z, kv_dp(dim), nsplit) * 4) + align256(stat_floats(z, nsplit) * 4));
         }
@@ -97,7 +100,7 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     plan.per = a.heads / a.c.heads;
     plan.rows_log2 = __builtin_ctz((unsigned)z.rows);
     plan.rows = z.rows;
-    plan.nsplit = splits_of(z.form, z.units, a.batch, records);
+    plan.nsplit = splits_of(z.form, z.units, records);
     plan.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes);
     plan.stat = reinterpret_cast<float*>(reinterpret_cast<char*>(plan.part) + align256(part_floats(z, dp, plan.nsplit) * 4));
     const dim3 grid((unsigned)(z.units * plan.nsplit));

@@ -14,14 +14,14 @@ DIMS = [(64, 64), (40, 32), (96, 32), (128, 64), (128, 128), (192, 64), (256, 12
 
 
 def splits(lens, nqs, heads, kv, page, rows_of_a_unit, spare=0, window=0):
-    """Splits of the call by the planner's rule (768 workgroups, 1536 from 8 sequences on; at least 4 records each,
-    none below 20 records).  2 to 8 are joined by units."""
+    """Splits of the call by the planner's rule (768 workgroups, 1536 for 385 to 767 units of 256 records and more; at least
+    4 records each, none below 20 records).  2 to 8 are joined by units."""
     tiles = -(-max(nqs) * (heads // kv) // rows_of_a_unit)
     records = (max(max(-(-n // page) for n in lens), 1) + 1 + spare) * (page // 32)
     if window:
         records = min(records, (window + max(nqs)) // 32 + 2)
     units = len(lens) * kv * tiles
-    return min((768 if len(lens) < 8 else 1536) // units, records // 4) if records >= 20 else 1
+    return min((1536 if 384 < units < 768 and records >= 256 else 768) // units, records // 4) if records >= 20 else 1
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -46,12 +46,12 @@ def test_join_of_units_wide_tiles(qe, group, dtype):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("dim,group", [(64, 32), (128, 64), (256, 64)])
 def test_join_of_units_many_sequences(qe, dim, group, dtype):
-    """From 8 sequences on: every number of splits in use from 1 to 7."""
+    """Every number of splits in use from 1 to 7; units that are more than half of the chip's, in three over long tables."""
     lens = [1000, 100, 639, 640, 800, 790, 5, 0, 960, 700]
-    assert splits(lens, [1] * 10, 40, 20, 32, 16) == 7
-    attend(qe, lens, [1] * 10, 40, 20, dim, group, 32, dtype, seed=dim)
-    assert splits(lens, [2] * 10, 160, 40, 32, 16) == 3
-    attend(qe, lens, [2] * 10, 160, 40, dim, group, 32, dtype, seed=dim + 1)
+    assert splits(lens, [1] * 10, 20, 10, 32, 16) == 7
+    attend(qe, lens, [1] * 10, 20, 10, dim, group, 32, dtype, seed=dim)
+    assert splits(lens, [2] * 10, 80, 40, 32, 16, 300) == 3
+    attend(qe, lens, [2] * 10, 80, 40, dim, group, 32, dtype, seed=dim + 1, spare=300)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
