@@ -12,12 +12,14 @@ extern template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, di
 namespace {
 
 // Workgroups of the many-row form from which it is taken: two of a CU.  Below that the few-row form is
-// faster, since its workgroups are smaller and share a row's tokens.  2048 tokens, bf16, many against
-// few, in us: 128 channels in groups of 128, 128 workgroups 67 / 39, 256 69 / 68, 384 84 / 90; 192
-// channels, 256 workgroups 110 / 80, 512 135 / 133; 256 channels, 512 workgroups 137 / 151; fp32,
-// 400 workgroups of uneven lengths 56 / 32; 2048 queries of 32 heads over 16384 tokens 681 / 802.
-// 256 channels in groups of 32 do not fit the few-row form's registers: 256 workgroups 293 / 378.
-constexpr int64_t kManyRows = 128, kManyFill = 512, kManyFillWide = 128;
+// faster, since its workgroups are smaller and share a row's tokens.  128 queries over 2048 tokens, bf16, us of the many /
+// the few at 256, 384 and 512 workgroups of the many: 64 channels in groups of 64 57 / 52, 81 / 72, 83 / 89; 96 in 64 94 / 85,
+// 126 / 119, 131 / 157; 128 in 128 74 / 75, 103 / 110, 110 / 149; in 64 97 / 89, 132 / 134, 138 / 177; in 32 87 / 84,
+// 110 / 121, 115 / 161; 192 in 64 122 / 90, 146 / 125, 149 / 166; in 32 164 / 125, 201 / 180, 205 / 239; 256 in 128 115 / 95,
+// 147 / 139, 153 / 183; in 64 148 / 109, 189 / 159, 204 / 206.  fp32, 128 in 64: 89 / 74 at 256, 117 / 130 at 512.
+// 256 channels in groups of 32 do not fit the few-row form's registers: at 128, 160 and 256 workgroups 375 / 234,
+// 373 / 403, 376 / 463 (fp32 at 128, 192 and 256 477 / 261, 481 / 481, 499 / 527).
+constexpr int64_t kManyRows = 128, kManyFill = 512, kManyFillWide = 160;
 // Workgroups of the few-row form that fill the chip, three of a CU.  Units that are more than half of that would not be
 // split; they are, in two or three, where each has kSplitLong records (8192 tokens) or more: the last ones, or the
 // long ones, are not left to the end.  29 query heads on one of 64 channels, us with 768 / 1536 workgroups:

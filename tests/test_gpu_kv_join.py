@@ -127,3 +127,10 @@ def test_rows_of_no_sequence_are_not_written(qe, many):
     check(out[2:nq + 6], lse[2:nq + 6], q[2:nq + 6], held, [nq, 4], dim ** -0.5, "bf16")
     for t in (out, lse):
         assert bool((t[:2] == 3.0).all()) and bool((t[nq + 6:] == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads", [60, 80])
+def test_wide_heads_in_groups_of_32_on_both_sides_of_their_rule(qe, heads, dtype):
+    """128 rows a key head of 256 channels: 120 workgroups of the many-row form (few rows, split) and 160 (many)."""
+    attend(qe, [700], [128], heads, heads, 256, 32, 64, dtype, seed=heads)
