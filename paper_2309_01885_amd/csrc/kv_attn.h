@@ -1259,8 +1259,9 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_unit_kernel(KvA
 // The form of a call: many rows or few, and a wave's tiles of 16 rows.
 struct KvForm { bool many; int nt; };
 
-// Tiles of a wave with many rows: what the registers hold.
+// Tiles of a wave with many rows, and of a unit with few at most: what the registers hold.
 constexpr int kv_many_nt(int dp, int group, bool f32) { return dp <= 128 && !f32 && (group > 32 || dp == 64) ? 2 : 1; }
+constexpr int kv_few_nt(int dp, int group, bool f32) { return dp <= 128 && !f32 && (group > 32 || dp < 128) ? 2 : 1; }
 
 template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm form, dim3 grid, hipStream_t s)
 {
@@ -1271,10 +1272,10 @@ template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm
             else hipLaunchKernelGGL((kv_few_kernel<DP, G, 1, 2>), grid, dim3(256), 0, s, a, plan);
         } else if (form.many) {
             hipLaunchKernelGGL((kv_many_kernel<DP, G, kv_many_nt(DP, G, false), 1>), grid, dim3(256), 0, s, a, plan);
-        } else if (DP > 128 || form.nt == 1) {
+        } else if (form.nt == 1) {
             hipLaunchKernelGGL((kv_few_kernel<DP, G, 1, 1>), grid, dim3(256), 0, s, a, plan);
         } else {
-            hipLaunchKernelGGL((kv_few_kernel<DP, G, DP <= 128 ? 2 : 1, 1>), grid, dim3(256), 0, s, a, plan);
+            hipLaunchKernelGGL((kv_few_kernel<DP, G, kv_few_nt(DP, G, false), 1>), grid, dim3(256), 0, s, a, plan);
         }
     });
     if (plan.nsplit > kKvFewSplits)

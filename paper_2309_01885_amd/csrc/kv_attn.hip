@@ -29,15 +29,17 @@ constexpr int64_t kManyRows = 128, kManyFill = 512, kManyFillWide = 160;
 constexpr int64_t kFill = 768, kSplitLong = 256;
 // Records (32 tokens of one head for one unit) from which the few-row form takes 32 rows a unit
 // instead of 16: a record's codes are then converted for twice the rows, but by half as many workgroups.
-// 128 channels, 32 against 16 rows, in us: 256 units of 64 records 38 / 33, 1024 of 32 42 / 44, 256
-// of 256 88 / 104; 64 channels: 21 of 63 15 / 14, 512 of 256 81 / 96.
+// 29 heads on one, 16 against 32 rows, in us: 128 channels in groups of 64, 256 units of 64 records 45 / 52, 512 of 64 65 /
+// 72, 1024 of 32 65 / 57, 256 of 256 118 / 114; in groups of 128, 256 of 64 37 / 47, 256 of 256 100 / 101; 64 channels:
+// 21 of 63 14 / 16, 64 of 256 30 / 32, 512 of 256 99 / 85; groups of 32: 64 channels, 256 of 256 90 / 79, 96 channels 122 / 119;
+// 128 channels in groups of 32 spill: 176 / 281, and keep 16 (kv_few_nt).
 constexpr int64_t kWideFrom = 32768;
 
 KvForm form_of(int64_t heads, int64_t rows, int64_t records, int dp, int group, bool f32)
 {
     const int nt = kv_many_nt(dp, group, f32);
     if (rows >= kManyRows && heads * cdiv(rows, 16 * nt * kKvWaves) >= (dp == 8 * group ? kManyFillWide : kManyFill)) return {true, nt};
-    return {false, rows <= 16 || f32 || dp > 128 || heads * cdiv(rows, 32) < cdiv(kWideFrom, std::max<int64_t>(records, 1)) ? 1 : 2};
+    return {false, rows <= 16 || kv_few_nt(dp, group, f32) == 1 || heads * cdiv(rows, 32) < cdiv(kWideFrom, std::max<int64_t>(records, 1)) ? 1 : 2};
 }
 
 // Splits along the tokens: as many as fill the chip, each of at least kKvMinRecords records.
