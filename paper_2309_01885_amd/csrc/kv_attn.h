@@ -12,9 +12,10 @@
 // move between lanes: token 8 (l / 16) + 4 h + r is row 4 (l / 16) + r of half h.
 //
 // What bounds it: one new token of a sequence reads the cache once (dim + 8 groups bytes a token and
-// key head); 2 x 262144 tokens of 8 heads of 128 take 110 us, 5.2 TB/s of reads, where a plain copy moves
-// 4.9 (read and written).  Chunks are bound by vector instructions: 2048 queries over 16384
-// tokens of 32 heads take 634 us, 813 TFLOP/s, with the vector units 60 % busy and the matrix cores 32 %.
+// key head); 2 x 262144 tokens of 8 heads of 128 take 112 us, 5.1 TB/s of reads, where a plain copy moves
+// 4.9 (read and written).  Chunks wait for vector instructions most: 2048 queries over 16384 tokens of 32
+// heads take 671 to 695 us, 741 to 768 TFLOP/s, with the vector units 62 % busy, the matrix cores 30 %,
+// and no more than two waves a SIMD to overlap them.
 // (A matrix product of fp16 numbers in memory reaches 1140 TFLOP/s here, and has neither an
 // exponential a score nor codes to convert.)
 #pragma once
@@ -689,8 +690,9 @@ __device__ inline float kv_lse(float top, float mass) { return mass == 0.f ? -kK
 // it) and take the unit's records in turn, so that a record is read by one wave and one wave's loads
 // wait while the others work; the waves' sums meet in LDS, the splits' in a second launch.  Two tiles
 // where rows and tokens are many: a record's conversion, half of the vector instructions, is shared.
-// 64 sequences of 2048 to 8192 tokens take 77 us with the join, for 40 us of bytes at a copy's rate: the
-// vector units are 58 % busy, the matrix cores 12 %, and the rest is waits of few waves.
+// 64 sequences of 2048 to 8192 tokens, 29 query heads on one of 64 channels, take 81 to 88 us with the join, from
+// run to run, for 40 us of bytes at a copy's rate: the vector units are 60 % busy, the matrix cores
+// 11 %, and the rest is waits of few waves.
 //
 // Workgroups of a CU that the registers are to allow.  Never one: beyond 256 registers the compiler
 // keeps the sums in accumulation registers and was seen to read one back after the last matrix
@@ -941,7 +943,7 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
 // the next is converted and the one after it is on its way.  A stage is straight code, also where a
 // wave's rows see none of it and past the last record: conversion and first products, then
 // exponentials and second products can overlap.  2048 queries over 16384 tokens of 32 heads of 128:
-// 634 us; with every wave converting its own (the few-row form) 802.
+// 682 us; with every wave converting its own (the few-row form) 831.
 constexpr int kv_stage_records(int dp) { return dp <= 128 ? 2 : 1; }
 
 template <int DP, int GROUP, int NT, int PARTS>
@@ -952,8 +954,9 @@ __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
     constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
     constexpr int KR = kv_stage_records(DP), W = kKvWaves / KR;  // records of a stage, waves that convert one
     // Records whose exponentials are taken together: all of a stage, where the registers hold them.  Two tiles
-    // of two groups spill (2048 queries of 32 heads of 128 in groups of 64 over 8192 tokens: 560 us
-    // together, 433 one by one; groups of 128 694 / 735, 64 channels in groups of 64 269 / 282).
+    // of two groups spill (2048 queries of 32 heads of 128 in groups of 64 over 8192 tokens: 547 us
+    // together, 450 one by one; 96 channels over 4096 226 / 228; groups of 128 over 16384 696 / 737, 64
+    // channels in groups of 64 over 8192 273 / 296).
     constexpr int KW = NG == 2 && NT == 2 && DP > 64 ? 1 : KR;
     constexpr int CW = KR == 2 ? NC : (NC + 1) / 2;              // key products a wave converts
     constexpr int VW = T::kHalf ? (UT + 1) / 2 : UT, VK = KR;    // unit tiles and classes

@@ -6,9 +6,10 @@
 //   s = max((hi - lo) * fp32(1 / 15), 2^-126), to 20 bits of mantissa (the zero point takes the
 //   other four), z = rint(-lo (1 / s)),  n = clamp(rint(x (1 / s)) + z, 0, 15).
 // Every step is one correctly rounded fp32 operation, so the codes depend on the group's
-// values alone.  Both kernels are bound by memory, and move each value once: 8 x 4096 tokens of 32 heads
-// of 128 in fp16 are written in 165 us and read back in 155 (680 MB each, 4.1 to 4.4 TB/s, a
-// plain copy reaches 4.9); 131072 tokens of 8 heads of 128 in bf16 are read in 169 us (4.1 TB/s).
+// values alone.  Each value is moved once: 8 x 4096 tokens of 32 heads of 128 in fp16 are written in
+// 165 us and read back in 155 (680 MB each, 4.1 to 4.4 TB/s, a plain copy reaches 4.9); 131072 tokens of 8 heads
+// of 128 in bf16 are read in 170 us (4.1 TB/s).  Reading is bound by memory (vector units 53 % busy); writing as much
+// by the vector units, which a cold call of that size (178 us and more) keeps busy throughout.
 // A few tokens cost their launch and three dependent loads: 3 to 5 us.
 #include "kv.h"
 
