@@ -401,6 +401,53 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
                      int64_t k_head_stride, int64_t v_stride, int64_t v_head_stride, int* status,
                      void* stream);
 
+/* Pages and slots of a step.  Sequence b has lengths[b] tokens, in the pages table[b * width + j],
+ * j < held = max(ceil(lengths[b] / page), keep[b]); the pages that nobody has are free_pages[0] .. [*free_count - 1], a
+ * stack whose top is its end, of the num_pages pages 0 .. num_pages - 1.  The call gives every sequence counts[b] more
+ * tokens (or takes -counts[b] back, down to none), with new = max(lengths[b] + counts[b], 0) and
+ * want = max(ceil(new / page), keep[b]):
+ *  - first the pages j = want .. held - 1 of all sequences go back onto the stack, the r-th of them (sequences and
+ *    pages in ascending order) to the place r below the new top, and their table entries become -1;
+ *  - then the pages j = held .. want - 1 are taken from the top in the same order, so that a call with
+ *    the opposite counts restores table, lengths and stack.  A sequence gets all its pages or none: those that want any
+ *    get them as long as the pages wanted up to and including theirs are there, those that want none need none.
+ *    A sequence without its pages keeps its length, and its tokens get the slot -1;
+ *  - lengths[b] = new.  keep (NULL: 0): so many of the row's first entries are the caller's, for instance a prefix that
+ *    several sequences share.  They are neither pushed, nor taken, nor changed.
+ * Out, all on the device: q_start[b] = the sum of max(counts, 0) before b (batch + 1 entries, cut off at
+ * `total`); for row i of the call, which is token lengths[b] + i - q_start[b] (the length before the call) of the
+ * sequence with q_start[b] <= i < q_start[b + 1], positions[i] = that token and slots[i] = table page * page + token %
+ * page.  Rows from q_start[batch] on, which a graph recorded for `total` rows may have, get -1 in both.
+ * lacking (NULL, or one int): the pages that were wanted and not there, 0 where every sequence has its own.
+ * Lengths below 0 or past width * page before or after the call, keep outside of 0 .. width, a stack outside
+ * of 0 .. num_pages, page numbers outside of the cache that are taken and rows past `total` set QE_ERR_ARG in the workspace's status
+ * word (never cleared here).  Such a sequence stays as it is and its rows get -1; a sequence whose rows
+ * pass `total` gets no pages.  batch up to 2^20 (QE_ERR_UNSUPPORTED beyond).  No two rows of table may be the same memory. */
+size_t qe_kv_extend_workspace_size(int64_t batch);
+qe_status qe_kv_extend(const int32_t* counts, int64_t batch, int32_t* table, int64_t width, int32_t* lengths,
+                       const int32_t* keep, int32_t* free_pages, int64_t num_pages, int32_t* free_count, int page,
+                       int64_t total, int64_t* slots, int32_t* positions, int32_t* q_start, int32_t* lacking, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* Queries and keys of new tokens, normed and rotated, and keys and values written into the slots, in one
+ * pass: out (tokens x heads x dim, may be Q itself, element for element) gets the queries, the cache what qe_kv_write would
+ * write for the keys before their rounding to dtype.  For a row x of a head's query (or key), each step one fp32 rounding:
+ *   norm (where the weight, dim floats, is not NULL): r = 1 / sqrt(sum x^2 / dim + eps), formed in fp64,
+ *     y = (x r) weight;
+ *   rotation of the first rot channels (rot even, at most dim; 0: none) by row positions[token] of cos and sin
+ *     (rows x rot / 2 floats): a' = a c - b s, b' = b c + a s for the pairs (a, b) of channels (i, i + rot / 2), or
+ *     (2 i, 2 i + 1) with interleaved, and c, s the row's entries i;
+ * queries are then rounded to dtype.  A token whose position is negative is skipped: its row of out and the
+ * cache stay; so is one whose position is not below rows, which also sets QE_ERR_ARG in `status`.  positions
+ * may be NULL without rotation.  A token whose slot is negative (or past the cache: QE_ERR_ARG) gets its query alone.
+ * Slots, group, pages, strides and status as in qe_kv_write. */
+qe_status qe_kv_append(const void* Q, const void* K, const void* V, int dtype, int64_t tokens, int heads, int kv_heads, int dim,
+                       int64_t q_stride, int64_t q_head_stride, int64_t k_stride, int64_t k_head_stride, int64_t v_stride,
+                       int64_t v_head_stride, const float* q_weight, const float* k_weight, double eps,
+                       const int32_t* positions, const float* cos, const float* sin, int64_t rows, int rot, int interleaved,
+                       const int64_t* slots, int group, void* pages, int64_t num_pages, int page, void* out, int64_t o_stride,
+                       int64_t o_head_stride, int* status, void* stream);
+
 /* Attention over the cache.  Sequence b has lengths[b] cached tokens, token t in
  * page table[b * width + t / page], and the queries q_start[b] .. q_start[b + 1] - 1
  * of the `total` rows of Q (total x heads x dim); with q_start NULL the queries

@@ -89,7 +89,7 @@ def write(pages, slots, k, v, group):
                 put(pages, int(slot), h, kc[t, h], kw[t, h], vc[t, h], vw[t, h], group)
 
 
-def attention(q, k, v, pos, scale, causal=True, window=0, slopes=None):
+def attention(q, k, v, pos, scale, causal=True, window=0, slopes=None, sinks=0):
     """q (nq, heads, dim) at positions pos over k, v (tokens, kv heads, dim), all in fp64:
     (out, lse, mass) with mass = sum_t p_t |v_t|, what an error of the p_t acts on."""
     q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
@@ -105,7 +105,7 @@ def attention(q, k, v, pos, scale, causal=True, window=0, slopes=None):
             if causal:
                 see &= t <= pos[i]
             if window:
-                see &= t > pos[i] - window
+                see &= (t > pos[i] - window) | (t < sinks)
             if not see.any():
                 continue
             s = scale * (kh[see] @ q[i, h])
@@ -118,3 +118,75 @@ def attention(q, k, v, pos, scale, causal=True, window=0, slopes=None):
             mass[i, h] = p @ np.abs(vh[see]) / total
             lse[i, h] = top + np.log(total)
     return out, lse, mass
+
+
+def extend(counts, table, lengths, free, free_count, page, total, keep=None):
+    """A step's pages and slots, sequence by sequence and token by token; in place on table, lengths and free.
+    Returns (slots, positions, q_start, free_count, lacking, bad)."""
+    width, num, batch = table.shape[1], free.size, len(counts)
+    keep = [0] * batch if keep is None else keep
+    bad = not 0 <= free_count <= num
+    free_count = min(max(free_count, 0), num)
+    plan = []
+    for b in range(batch):
+        old, k = int(lengths[b]), int(keep[b])
+        new = max(old + int(counts[b]), 0)
+        wrong = old < 0 or old > width * page or k < 0 or k > width or new > min(width * page, 2 ** 31 - 1)
+        held, want = (0, 0) if wrong else (max(-(-old // page), k), max(-(-new // page), k))
+        plan.append((old, old if wrong else new, held, want, wrong))
+        bad |= wrong
+    back = [(b, j) for b, (_, _, held, want, _) in enumerate(plan) for j in range(want, held)]
+    top = free_count + len(back)
+    for r, (b, j) in enumerate(back):
+        if top - 1 - r < num:
+            free[top - 1 - r] = table[b, j]
+        table[b, j] = -1
+    have = min(top, num)
+    bad |= top > num
+    slots, positions = np.full(total, -1, np.int64), np.full(total, -1, np.int32)
+    q_start = np.zeros(batch + 1, np.int32)
+    needed = taken = row = 0
+    for b, (old, new, held, want, wrong) in enumerate(plan):
+        n, need = max(int(counts[b]), 0), max(want - held, 0)
+        needed += need
+        got = not wrong and (need == 0 or needed <= have) and row + n <= total
+        if got:
+            for j in range(need):
+                at = top - 1 - (needed - need + j)
+                table[b, held + j] = free[at] if at < num else -1
+            taken = max(taken, needed if need else 0)
+            lengths[b] = new
+        for i in range(n):
+            if row + i >= total or wrong:
+                continue
+            positions[row + i] = old + i
+            if got:
+                p = int(table[b, (old + i) // page])
+                if 0 <= p < num:
+                    slots[row + i] = p * page + (old + i) % page
+                else:
+                    bad = True
+        row += n
+        q_start[b + 1] = min(row, total)
+    bad |= row > total
+    return slots, positions, q_start, have - taken, max(needed - have, 0), bad
+
+
+def norm_rotate(x, weight, eps, positions, cos, sin, interleaved):
+    """(tokens, heads, dim) of any float type -> fp32: every step one fp32 rounding, the sum of squares in fp64."""
+    y = np.asarray(x).astype(F)
+    with np.errstate(over="ignore", invalid="ignore", divide="ignore"):
+        if weight is not None:
+            d = y.astype(np.float64)
+            r = (1.0 / np.sqrt((d * d).sum(-1, keepdims=True) / y.shape[-1] + eps)).astype(F)
+            y = (y * r).astype(F) * weight.astype(F)
+        if cos is None:
+            return y
+        c, s = (t[np.maximum(positions, 0)][:, None] for t in (cos, sin))
+        half = cos.shape[1]
+        i = np.arange(half)
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        z = y.copy()
+        z[..., a] = y[..., a] * c - y[..., b] * s
+        z[..., b] = y[..., b] * c + y[..., a] * s
+    return z

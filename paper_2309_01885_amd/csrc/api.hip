@@ -391,6 +391,72 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
                           status, as_stream(stream));
 }
 
+size_t qe_kv_extend_workspace_size(int64_t batch)
+{
+    if (batch < 0 || batch > (1 << 20)) return 0;
+    return kv_extend_ws_bytes(batch);
+}
+
+qe_status qe_kv_extend(const int32_t* counts, int64_t batch, int32_t* table, int64_t width, int32_t* lengths,
+                       const int32_t* keep, int32_t* free_pages, int64_t num_pages, int32_t* free_count, int page,
+                       int64_t total, int64_t* slots, int32_t* positions, int32_t* q_start, int32_t* lacking, void* ws,
+                       size_t ws_bytes, void* stream)
+{
+    if (batch < 0 || width < 0 || total < 0 || num_pages < 1 || page < kKvTok || page % kKvTok || page > (1 << 30)) return QE_ERR_ARG;
+    if (total > 0x7fffffff || num_pages > 0x7fffffff || width > 0x7fffffff) return QE_ERR_ARG;
+    if (batch > (1 << 20)) return QE_ERR_UNSUPPORTED;
+    if (!free_pages || !free_count || !q_start || (batch > 0 && (!counts || !lengths)) || (batch > 0 && width > 0 && !table)) return QE_ERR_ARG;
+    if (total > 0 && (!slots || !positions)) return QE_ERR_ARG;
+    for (const void* p : {(const void*)counts, (const void*)table, (const void*)lengths, (const void*)keep, (const void*)free_pages,
+                          (const void*)free_count, (const void*)positions, (const void*)q_start, (const void*)lacking})
+        if (misaligned(p, 4)) return QE_ERR_ARG;
+    if (misaligned(slots, 8) || misaligned(ws, 16)) return QE_ERR_ARG;
+    if (!ws || ws_bytes < kv_extend_ws_bytes(batch)) return QE_ERR_WORKSPACE;
+    KvExtend a{};
+    a.counts = counts;
+    a.table = table;
+    a.lengths = lengths;
+    a.keep = keep;
+    a.free = free_pages;
+    a.free_count = free_count;
+    a.slots = slots;
+    a.positions = positions;
+    a.q_start = q_start;
+    a.lacking = lacking;
+    a.batch = batch;
+    a.width = width;
+    a.num_pages = num_pages;
+    a.total = total;
+    a.page = page;
+    a.status = static_cast<int*>(ws);
+    return launch_kv_extend(a, ws, as_stream(stream));
+}
+
+qe_status qe_kv_append(const void* Q, const void* K, const void* V, int dtype, int64_t tokens, int heads, int kv_heads, int dim,
+                       int64_t q_stride, int64_t q_head_stride, int64_t k_stride, int64_t k_head_stride, int64_t v_stride,
+                       int64_t v_head_stride, const float* q_weight, const float* k_weight, double eps,
+                       const int32_t* positions, const float* cos, const float* sin, int64_t rows, int rot, int interleaved,
+                       const int64_t* slots, int group, void* pages, int64_t num_pages, int page, void* out, int64_t o_stride,
+                       int64_t o_head_stride, int* status, void* stream)
+{
+    if (bad_dtype(dtype) || tokens < 0 || bad_kv(num_pages, page, kv_heads, dim, group)) return QE_ERR_ARG;
+    if (heads < 1 || heads > (1 << 20) || tokens > 0x7fffffff) return QE_ERR_ARG;
+    if (!(eps >= 0.) || !std::isfinite(eps) || rot < 0 || rot > dim || rot % 2) return QE_ERR_ARG;
+    const bool turn = rot > 0;
+    if (turn && (rows < 1 || !cos || !sin)) return QE_ERR_ARG;
+    if (tokens == 0) return QE_OK;
+    if (!Q || !K || !V || !out || !slots || !pages || misaligned(pages, 16) || (turn && !positions)) return QE_ERR_ARG;
+    for (const void* p : {Q, K, V, (const void*)out})
+        if (misaligned(p, dtype_bytes(dtype))) return QE_ERR_ARG;
+    for (const void* p : {(const void*)q_weight, (const void*)k_weight, (const void*)positions, (const void*)cos, (const void*)sin})
+        if (misaligned(p, 4)) return QE_ERR_ARG;
+    if (misaligned(slots, 8) || misaligned(status, 4)) return QE_ERR_ARG;
+    const int64_t strides[8] = {q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride, o_stride, o_head_stride};
+    const KvRotation r{positions, turn ? cos : nullptr, turn ? sin : nullptr, rows, rot / 2, interleaved != 0, false};
+    return launch_kv_append(Q, K, V, out, dtype, strides, tokens, heads, r, KvNorm{q_weight, k_weight, eps}, slots,
+                            kv_cache(pages, num_pages, page, kv_heads, dim), group, status, as_stream(stream));
+}
+
 size_t qe_kv_attn_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim)
 {
     if (total < 0 || batch < 0 || max_q < 0 || bad_kv(1, kKvTok, kv_heads, dim, 32)) return 0;

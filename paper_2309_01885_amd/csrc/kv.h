@@ -103,6 +103,46 @@ struct KvAttn {
     int* status;
 };
 
+// What kv_extend knows of a sequence when the tokens' slots are looked up.
+struct KvExtendSeq {
+    int32_t old, held, start;      // tokens and pages before the call; first token of the call
+    int32_t first;                 // its first wanted page's place among all that are taken; -1: none given, -2: bad arguments
+};
+struct KvExtend {
+    const int32_t* counts;
+    int32_t* table;
+    int32_t* lengths;
+    const int32_t* keep;           // or null
+    int32_t* free;
+    int32_t* free_count;
+    int64_t* slots;
+    int32_t* positions;
+    int32_t* q_start;
+    int32_t* lacking;              // or null
+    int64_t batch, width, num_pages, total, page;
+    int* status;
+    KvExtendSeq* seqs;             // in the workspace
+    int64_t* top;
+};
+
+size_t kv_extend_ws_bytes(int64_t batch);
+qe_status launch_kv_extend(const KvExtend& a, void* ws, hipStream_t s);
+
+struct KvRotation {
+    const int32_t* positions;      // or null: no rotation, every query row is taken
+    const float *cos, *sin;        // rows x half; null: no rotation
+    int64_t rows;
+    int half;                      // pairs of channels
+    bool interleaved, vec;         // vec: eight channels' cosines lie aligned and beside each other
+};
+struct KvNorm {
+    const float *q, *k;            // weights; null: no norm
+    double eps;
+};
+qe_status launch_kv_append(const void* Q, const void* K, const void* V, void* out, int dtype, const int64_t* strides, int64_t tokens,
+                           int heads, const KvRotation& r, const KvNorm& n, const int64_t* slots, const KvCache& c, int group,
+                           int* status, hipStream_t s);
+
 size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim);
 qe_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t s);
 qe_status launch_kv_write(const void* K, const void* V, int dtype, const int64_t* strides, const int64_t* slots,

@@ -90,6 +90,11 @@ SIGNATURES = {
                            _int, _vp, _vp]),
     "qe_kv_read": (_int, [_vp, _i64, _int, _vp, _i64, _int, _int, _int, _vp, _vp, _int, _i64, _i64, _i64,
                           _i64, _vp, _vp]),
+    "qe_kv_extend_workspace_size": (_sz, [_i64]),
+    "qe_kv_extend": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _int, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "qe_kv_append": (_int, [_vp, _vp, _vp, _int, _i64, _int, _int, _int, _i64, _i64, _i64, _i64, _i64, _i64, _vp, _vp,
+                            ctypes.c_double, _vp, _vp, _vp, _i64, _int, _int, _vp, _int, _vp, _i64, _int, _vp, _i64, _i64,
+                            _vp, _vp]),
     "qe_kv_attn_workspace_size": (_sz, [_i64, _i64, _i64, _int, _int, _int]),
     "qe_kv_attn": (_int, [_vp, _int, _i64, _int, _int, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _int, _int,
                           _int, _vp, _i64, _vp, _f32, _int, _int, _vp, _vp, _i64, _i64, _vp, _vp, _sz,
@@ -502,6 +507,99 @@ def kv_read(pages: torch.Tensor, slots: torch.Tensor, dim: int, group: int = 64,
     if code:
         raise QEError(code, "qe_kv_read")
     return K, V
+
+
+def kv_extend_workspace_size(batch: int) -> int:
+    return int(load().qe_kv_extend_workspace_size(batch))
+
+
+def kv_extend(counts: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, free: torch.Tensor,
+              free_count: torch.Tensor, page: int, total: int, keep: Optional[torch.Tensor] = None,
+              slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+              q_start: Optional[torch.Tensor] = None, lacking: Optional[torch.Tensor] = None,
+              ws: Optional[torch.Tensor] = None, check: bool = False, stream=None):
+    """Pages and slots for counts[b] (int32; negative: taken back) more tokens of each sequence (qe_kv_extend).
+
+    Updates table (int32, sequences x pages), lengths (int32), free (int32, one entry for each page of the cache: the
+    free pages' numbers are its first free_count entries) and free_count (int32, one element) in place.
+    Returns slots (int64) and positions (int32) of the call's `total` rows, -1 for rows that are no token's,
+    and q_start (int32, sequences + 1), into the tensors given or new ones of `stream`.  keep (int32): so many of each
+    sequence's first pages are the caller's.  lacking: None or int32 of one element, the pages that were
+    not there; a sequence without its pages stays as it is and its slots are -1.  The call does not wait for
+    the device; check=True does, and raises if it met lengths that do not fit the table."""
+    if table.dim() != 2:
+        _bad("table", table, "sequences x pages")
+    batch, width = table.shape
+    dev = table.get_device()
+    if dev < 0:
+        raise ValueError("table must be a device tensor")
+    if slots is None:
+        slots = _on(stream, lambda: torch.empty(total, dtype=torch.int64, device=table.device))
+    if positions is None:
+        positions = _on(stream, lambda: torch.empty(total, dtype=torch.int32, device=table.device))
+    if q_start is None:
+        q_start = _on(stream, lambda: torch.empty(batch + 1, dtype=torch.int32, device=table.device))
+    if ws is None:
+        ws = _on(stream, lambda: workspace(kv_extend_workspace_size(batch), table.device))
+    i32 = torch.int32
+    code = load().qe_kv_extend(_flat(counts, "counts", i32, dev, batch), batch, _flat(table, "table", i32, dev), width,
+                               _flat(lengths, "lengths", i32, dev, batch), _flat(keep, "keep", i32, dev, batch),
+                               _flat(free, "free", i32, dev), free.numel(), _flat(free_count, "free_count", i32, dev, 1),
+                               page, total, _flat(slots, "slots", torch.int64, dev, total),
+                               _flat(positions, "positions", i32, dev, total), _flat(q_start, "q_start", i32, dev, batch + 1),
+                               _flat(lacking, "lacking", i32, dev, 1), _flat(ws, "ws", torch.uint8, dev), ws.numel(),
+                               _raw_stream(dev, stream))
+    if code:
+        raise QEError(code, "qe_kv_extend")
+    if check:
+        _finish(ws, check, "qe_kv_extend", stream)
+    return slots, positions, q_start
+
+
+def kv_append(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor,
+              group: int = 64, positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+              sin: Optional[torch.Tensor] = None, interleaved: bool = False, q_weight: Optional[torch.Tensor] = None,
+              k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, out: Optional[torch.Tensor] = None,
+              status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Norm and rotation of Q (tokens x heads x dim) and K (tokens x kv_heads x dim), and the write of K and V into the
+    slots of the cache, in one pass (qe_kv_append); returns the queries, in `out` (Q itself is allowed) or a
+    new tensor of `stream`.
+
+    q_weight, k_weight: float32 of dim elements, or None for no norm.  cos, sin: float32, positions x rot / 2,
+    or None for no rotation; positions (int32) names each token's row, a negative one skips the token, whose row of the
+    output is not written.  interleaved pairs channels 2 i and 2 i + 1 instead of i and i + rot / 2.  status:
+    None or an int32 device tensor of one element, set to QE_ERR_ARG by a slot past the cache or a position past
+    the tables (never cleared).  No gradient: the output has no graph."""
+    shape, dtype = Q.shape, Q.dtype
+    if len(shape) != 3 or dtype not in _DTYPES:
+        _bad("Q", Q, "tokens x heads x dim in float32, float16 or bfloat16")
+    n, heads, dim = shape
+    num, page, kv, dev = _pages(pages, dim, group)
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin come together")
+    rows = half = 0
+    if cos is not None:
+        if cos.dim() != 2 or cos.shape != sin.shape:
+            _bad("cos", cos, "positions x rot / 2, as sin")
+        if positions is None:
+            raise ValueError("a rotation needs positions")
+        rows, half = cos.shape
+    if out is None:
+        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
+    qt, qh = _heads(Q, "Q", shape, dtype, dev)
+    kt, kh = _heads(K, "K", (n, kv, dim), dtype, dev)
+    vt, vh = _heads(V, "V", (n, kv, dim), dtype, dev)
+    ot, oh = _heads(out, "out", shape, dtype, dev)
+    f32 = torch.float32
+    code = load().qe_kv_append(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _DTYPES[dtype], n, heads, kv, dim, qt, qh, kt, kh, vt, vh,
+                               _flat(q_weight, "q_weight", f32, dev, dim), _flat(k_weight, "k_weight", f32, dev, dim), eps,
+                               _flat(positions, "positions", torch.int32, dev, n), _flat(cos, "cos", f32, dev),
+                               _flat(sin, "sin", f32, dev), rows, 2 * half, 1 if interleaved else 0,
+                               _flat(slots, "slots", torch.int64, dev, n), group, pages.data_ptr(), num, page, out.data_ptr(),
+                               ot, oh, _flat(status, "status", torch.int32, dev, 1), _raw_stream(dev, stream))
+    if code:
+        raise QEError(code, "qe_kv_append")
+    return out
 
 
 def kv_attn_workspace_size(total: int, batch: int, max_q: int, heads: int, kv_heads: int, dim: int) -> int:
