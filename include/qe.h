@@ -486,6 +486,36 @@ qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim
                      int causal, int window, const float* slopes, void* out, int64_t o_stride,
                      int64_t o_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* qe_kv_attn (the same arguments, results and workspace) with the first tokens of every sequence visible beside the window: a
+ * query sees the tokens t <= pos with t > pos - window or t < sinks, each once where both hold.  Only the records of the two
+ * ranges are read.  window = 0 hides nothing, and sinks then change nothing.  Slopes count the tokens' true distance.
+ * sinks >= 0; causal only where not 0 (QE_ERR_ARG). */
+qe_status qe_kv_attn_sinks(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                           int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                           const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                           const int32_t* table, int64_t width, const int32_t* lengths, float scale, int causal,
+                           int window, int sinks, const float* slopes, void* out, int64_t o_stride, int64_t o_head_stride,
+                           float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* qe_kv_attn without a window for sequences that begin with the same pages (one system prompt, the branches of a request):
+ * the sequences groups[g] .. groups[g + 1] - 1 (device, ngroups + 1 ascending entries from 0 to batch; sequences outside of
+ * them share nothing) have the same first shared[g] page numbers in their rows of table.  The result is qe_kv_attn's,
+ * up to the rounding of sums: the tokens of these pages that every query of the group sees (the whole records of 32 of them;
+ * sequences without queries do not count) are read through the row of the group's first sequence, once for the
+ * queries of all of them, the others sequence by sequence.  So the shared pages may be filled in part, or be
+ * longer than a sequence.  A group of one sequence shares nothing, and a call that cannot gain is qe_kv_attn itself.
+ * Beside what qe_kv_attn checks, groups that do not ascend or leave 0 .. batch (then nothing is shared) and
+ * shared[g] outside of 0 .. width set QE_ERR_ARG in the workspace's status word.  That the pages are the same is not
+ * checked.  The queries of a sequence with a bad range in q_start are not computed. */
+size_t qe_kv_attn_shared_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads,
+                                        int dim, int64_t ngroups);
+qe_status qe_kv_attn_shared(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                            int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                            const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                            const int32_t* table, int64_t width, const int32_t* lengths, const int32_t* groups,
+                            const int32_t* shared, int64_t ngroups, float scale, int causal, const float* slopes, void* out,
+                            int64_t o_stride, int64_t o_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -464,29 +464,33 @@ size_t qe_kv_attn_workspace_size(int64_t total, int64_t batch, int64_t max_q, in
     return kv_attn_ws_bytes(batch, std::min(max_q, total), heads, kv_heads, dim);
 }
 
-qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
-                     int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
-                     const void* pages, int64_t num_pages, int page, int kv_heads, int group,
-                     const int32_t* table, int64_t width, const int32_t* lengths, float scale, int causal,
-                     int window, const float* slopes, void* out, int64_t o_stride, int64_t o_head_stride,
-                     float* lse, void* ws, size_t ws_bytes, void* stream)
+}  // extern "C"
+
+namespace {
+
+// The arguments that kv_attn, kv_attn_sinks and kv_attn_shared have in common; fills a where there is something to do.
+qe_status attn_args(KvAttn& a, bool& empty, const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                    int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q, const void* pages, int64_t num_pages,
+                    int page, int kv_heads, int group, const int32_t* table, int64_t width, const int32_t* lengths, float scale,
+                    int causal, int window, int sinks, const float* slopes, void* out, int64_t o_stride, int64_t o_head_stride, float* lse,
+                    void* ws)
 {
+    empty = false;
     if (bad_dtype(dtype) || bad_kv(num_pages, page, kv_heads, dim, group)) return QE_ERR_ARG;
     if (heads < 1 || heads % kv_heads || heads > (1 << 20)) return QE_ERR_ARG;
     if (total < 0 || total > 0x7fffffff || batch < 0 || batch > 0x7fffffff || max_q < 0 || width < 0) return QE_ERR_ARG;
-    if (!std::isfinite(scale) || window < 0 || (!causal && (window || slopes))) return QE_ERR_ARG;
+    if (!std::isfinite(scale) || window < 0 || sinks < 0 || (!causal && (window || sinks || slopes))) return QE_ERR_ARG;
     if (!q_start && total != batch * max_q) return QE_ERR_ARG;
     // (tiles of 16 query rows are counted in 32 bits, and a launch takes 2^24 workgroups of 256 threads)
     const int64_t rows = std::min(max_q, total) * (heads / kv_heads);
     if (rows > (int64_t(1) << 30) || batch * kv_heads > (int64_t(1) << 23) / (rows / 16 + 1)) return QE_ERR_UNSUPPORTED;
-    if (total == 0 || batch == 0 || max_q == 0) return QE_OK;
+    empty = total == 0 || batch == 0 || max_q == 0;
+    if (empty) return QE_OK;
     if (!Q || !pages || !lengths || !out || (width > 0 && !table) || misaligned(pages, 16)) return QE_ERR_ARG;
     if (misaligned(Q, dtype_bytes(dtype)) || misaligned(out, dtype_bytes(dtype))) return QE_ERR_ARG;
     for (const void* p : {(const void*)q_start, (const void*)table, (const void*)lengths, (const void*)slopes, (const void*)lse})
         if (misaligned(p, 4)) return QE_ERR_ARG;
     if (misaligned(ws, 16)) return QE_ERR_ARG;            // (16-byte accesses, and an atomic on the status word)
-    if (!ws || ws_bytes < qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim)) return QE_ERR_WORKSPACE;
-    KvAttn a{};
     a.c = kv_cache(pages, num_pages, page, kv_heads, dim);
     a.q = Q;
     a.out = out;
@@ -506,11 +510,91 @@ qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim
     a.scale = scale;
     a.causal = causal ? 1 : 0;
     a.window = window;
+    a.sinks = sinks;
     a.slopes = slopes;
     a.dtype = dtype;
     a.group = group;
     a.status = static_cast<int*>(ws);
+    return QE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+qe_status qe_kv_attn(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                     int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                     const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                     const int32_t* table, int64_t width, const int32_t* lengths, float scale, int causal,
+                     int window, const float* slopes, void* out, int64_t o_stride, int64_t o_head_stride,
+                     float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    return qe_kv_attn_sinks(Q, dtype, total, heads, dim, q_stride, q_head_stride, q_start, batch, max_q, pages, num_pages, page, kv_heads,
+                            group, table, width, lengths, scale, causal, window, 0, slopes, out, o_stride, o_head_stride, lse, ws,
+                            ws_bytes, stream);
+}
+
+qe_status qe_kv_attn_sinks(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                           int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                           const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                           const int32_t* table, int64_t width, const int32_t* lengths, float scale, int causal,
+                           int window, int sinks, const float* slopes, void* out, int64_t o_stride, int64_t o_head_stride,
+                           float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    KvAttn a{};
+    bool empty;
+    const qe_status st = attn_args(a, empty, Q, dtype, total, heads, dim, q_stride, q_head_stride, q_start, batch, max_q, pages, num_pages,
+                                   page, kv_heads, group, table, width, lengths, scale, causal, window, sinks, slopes, out, o_stride,
+                                   o_head_stride, lse, ws);
+    if (st != QE_OK || empty) return st;
+    if (!ws || ws_bytes < qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim)) return QE_ERR_WORKSPACE;
     return launch_kv_attn(a, ws, as_stream(stream));
+}
+
+size_t qe_kv_attn_shared_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups)
+{
+    if (ngroups < 0 || ngroups > (1 << 20) || qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim) == 0) return 0;
+    return kv_attn_shared_ws_bytes(total, batch, std::min(max_q, total), heads, kv_heads, dim, ngroups);
+}
+
+qe_status qe_kv_attn_shared(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                            int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                            const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                            const int32_t* table, int64_t width, const int32_t* lengths, const int32_t* groups,
+                            const int32_t* shared, int64_t ngroups, float scale, int causal, const float* slopes, void* out,
+                            int64_t o_stride, int64_t o_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    KvAttn a{};
+    bool empty;
+    if (ngroups < 0 || ngroups > (1 << 20) || misaligned(groups, 4) || misaligned(shared, 4)) return QE_ERR_ARG;
+    const qe_status st = attn_args(a, empty, Q, dtype, total, heads, dim, q_stride, q_head_stride, q_start, batch, max_q, pages, num_pages,
+                                   page, kv_heads, group, table, width, lengths, scale, causal, 0, 0, slopes, out, o_stride,
+                                   o_head_stride, lse, ws);
+    if (st != QE_OK || empty) return st;
+    if (ngroups > 0 && (!groups || !shared)) return QE_ERR_ARG;
+    if (!ws || ws_bytes < qe_kv_attn_shared_workspace_size(total, batch, max_q, heads, kv_heads, dim, ngroups)) return QE_ERR_WORKSPACE;
+    return launch_kv_attn_shared(a, groups, shared, ngroups, ws, false, as_stream(stream));
+}
+
+// qe_kv_attn_shared by its lists also where kv_attn itself would be faster: not part of the ABI, for tests of the lists at
+// small sizes.
+qe_status qei_kv_attn_listed(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
+                             int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
+                            const void* pages, int64_t num_pages, int page, int kv_heads, int group,
+                            const int32_t* table, int64_t width, const int32_t* lengths, const int32_t* groups,
+                            const int32_t* shared, int64_t ngroups, float scale, int causal, const float* slopes, void* out,
+                             int64_t o_stride, int64_t o_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    KvAttn a{};
+    bool empty;
+    if (ngroups < 0 || ngroups > (1 << 20) || misaligned(groups, 4) || misaligned(shared, 4)) return QE_ERR_ARG;
+    const qe_status st = attn_args(a, empty, Q, dtype, total, heads, dim, q_stride, q_head_stride, q_start, batch, max_q, pages, num_pages,
+                                   page, kv_heads, group, table, width, lengths, scale, causal, 0, 0, slopes, out, o_stride,
+                                   o_head_stride, lse, ws);
+    if (st != QE_OK || empty) return st;
+    if (ngroups > 0 && (!groups || !shared)) return QE_ERR_ARG;
+    if (!ws || ws_bytes < qe_kv_attn_shared_workspace_size(total, batch, max_q, heads, kv_heads, dim, ngroups)) return QE_ERR_WORKSPACE;
+    return launch_kv_attn_shared(a, groups, shared, ngroups, ws, true, as_stream(stream));
 }
 
 }  // extern "C"

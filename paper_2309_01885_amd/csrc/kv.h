@@ -96,11 +96,39 @@ struct KvAttn {
     const int32_t* table;          // page numbers, checked on the device
     const int32_t* lengths;        // clamped on the device
     float scale;
-    int32_t causal, window;
+    int32_t causal, window, sinks;
     const float* slopes;           // or null
     int32_t dtype, group;
     bool vec_q, vec_o;             // 16-byte accesses of q and out
     int* status;
+};
+
+// What one workgroup of kv_attn_shared's kernels does (KvUnit's fields of the same names).
+struct KvItem { int32_t first, b, kvh, tile_row, rows, len, pos0, rec0, rec1, slot, ref, pad; };
+
+// What the plan of kv_attn_shared knows of a group and of a sequence.
+struct KvGroup {
+    int32_t first_seq, first, tokens;      // its first sequence; first row of Q, rows
+    int32_t records;                       // shared records, 0: none
+    int32_t tiles, splits, item;           // tiles and splits of the shared part, its first entry of list 0
+    int32_t pad;
+};
+struct KvSequence {
+    int32_t first, nq, len;                // nq < 0: rows outside of the call
+    int32_t group;                         // -1: none that shares anything
+    int32_t tiles, splits, item;           // of its own part, in list 1
+    int32_t pad;
+};
+// A call of kv_attn_shared, beside its KvAttn.
+struct KvShared {
+    const int32_t *groups, *shared;        // groups[g] .. groups[g + 1] - 1 share shared[g] pages; checked on the device
+    int32_t ngroups;
+    int32_t rows[2], fill[2], least[2];    // of the two lists: rows of a tile, entries that fill the chip, records of an entry
+    int32_t room[2];                       // entries that a list holds
+    KvGroup* group;
+    KvSequence* seq;
+    KvItem* items[2];
+    int32_t* count;
 };
 
 // What kv_extend knows of a sequence when the tokens' slots are looked up.
@@ -143,8 +171,18 @@ qe_status launch_kv_append(const void* Q, const void* K, const void* V, void* ou
                            int heads, const KvRotation& r, const KvNorm& n, const int64_t* slots, const KvCache& c, int group,
                            int* status, hipStream_t s);
 
+inline void kv_attn_vec(KvAttn& a)
+{
+    const size_t size = a.dtype == QE_F32 ? 4 : 2;
+    a.vec_q = ((uintptr_t)a.q | (uint64_t)a.qt * size | (uint64_t)a.qh * size) % 16 == 0;
+    a.vec_o = ((uintptr_t)a.out | (uint64_t)a.ot * size | (uint64_t)a.oh * size) % 16 == 0;
+}
+
 size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim);
 qe_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t s);
+size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups);
+qe_status launch_kv_attn_shared(const KvAttn& a, const int32_t* groups, const int32_t* shared, int64_t ngroups, void* ws, bool always,
+                                hipStream_t s);   // always: also where kv_attn is faster
 qe_status launch_kv_write(const void* K, const void* V, int dtype, const int64_t* strides, const int64_t* slots,
                           int64_t tokens, const KvCache& c, int group, int* status, hipStream_t s);
 qe_status launch_kv_read(const KvCache& c, int group, const int64_t* slots, int64_t tokens, void* K, void* V,

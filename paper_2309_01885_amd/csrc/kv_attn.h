@@ -42,13 +42,22 @@ struct KvPlan {
     int nsplit, rows, rows_log2, per;       // per: heads of a key head
     float* part;                            // nsplit > 1: (unit, split, row, DP) sums divided by the split's mass
     float* stat;                            // (unit, split, row, 2): a mass f 2^(e + kKvJoinLog2) as e and f
+    const KvItem* items[2];                 // kKvListed: two lists of what the workgroups do, the first wgs0 of them the first list,
+    const int32_t* count;                   // and how long the lists are
+    int wgs0;
 };
+
+// What a kernel's workgroups work on: every (unit, split) of a call; the same where first tokens stay visible beside a
+// window; or the entries of two lists, whose results are always joined by another launch.
+enum KvMode { kKvPlain, kKvSinks, kKvListed };
 
 // What a workgroup works on; the join recomputes it.
 struct KvUnit {
     int64_t first, pos0;                    // first row of Q, position of query 0
     int b, kvh, per, tile_row, rows;        // per: heads of a key head; the unit's first row; rows of the sequence
     int len, rec0, rec1, splits;            // cached tokens; records that some row sees; splits in use
+    int gap, skip;                          // kKvSinks: records from the gap on are `skip` further behind
+    int ref, slot;                          // kKvListed: what slopes count from (-1: the row's position); first row of its results
 
     // records [from(s), from(s + 1)) are split s's
     __device__ int from(int split) const
@@ -69,9 +78,12 @@ constexpr int kKvJoinLog2 = 12;
 // A value that is the same for the whole workgroup and not written by the kernel: a scalar load.
 __device__ inline int kv_scalar(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)p; }
 
+// Record r of a unit.
+template <KvMode MODE> __device__ inline int kv_place(const KvUnit& u, int r) { return MODE == kKvSinks && r >= u.gap ? r + u.skip : r; }
+
 // (Divisions are of 32 bits: units and the rows of a sequence are fewer than 2^31, checked on the
 // host, and one of 64 bits takes 130 instructions.)
-__device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, uint32_t unit, bool report)
+template <KvMode MODE> __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, uint32_t unit, bool report)
 {
     KvUnit u;
     const uint32_t bh = unit / (uint32_t)p.row_tiles, tile = unit - bh * (uint32_t)p.row_tiles;
@@ -106,9 +118,43 @@ __device__ inline KvUnit kv_unit(const KvAttn& a, const KvPlan& p, uint32_t unit
     if (r0 >= u.rows || end < begin) end = begin;
     u.rec0 = (int)(begin / kKvTok);
     u.rec1 = end > begin ? (int)((end + kKvTok - 1) / kKvTok) : u.rec0;
+    if constexpr (MODE == kKvSinks) {
+        // the first tokens' records, then the window's; where they meet, everything in between
+        u.gap = min(u.rec0, (int)((min((int64_t)a.sinks, end) + kKvTok - 1) / kKvTok));
+        if (r0 >= u.rows) u.gap = 0;
+        u.skip = u.rec0 - u.gap;
+        u.rec1 -= u.skip;
+        u.rec0 = 0;
+        if (r0 >= u.rows) u.rec1 = 0;
+    }
     const int records = u.rec1 - u.rec0;
     u.splits = records < kKvSplitFrom ? 1 : min(p.nsplit, records / kKvMinRecords);
     return u;
+}
+
+// A workgroup's entry of the lists.  Consecutive entries go to one XCD (every eighth workgroup): tiles of
+// the same records share its L2.  False: there is none.
+__device__ inline bool kv_listed(const KvPlan& p, KvUnit& u)
+{
+    const bool second = (int)blockIdx.x >= p.wgs0;
+    const uint32_t wg = second ? blockIdx.x - p.wgs0 : blockIdx.x, n = kv_scalar(p.count + (second ? 1 : 0));
+    const uint32_t x8 = wg & 7, at = x8 * (n / 8) + min(x8, n % 8) + (wg >> 3);
+    if (wg >> 3 >= n / 8 + (x8 < n % 8 ? 1 : 0)) return false;
+    const int32_t* it = reinterpret_cast<const int32_t*>((second ? p.items[1] : p.items[0]) + at);
+    u.first = kv_scalar(it);
+    u.b = kv_scalar(it + 1);
+    u.kvh = kv_scalar(it + 2);
+    u.tile_row = kv_scalar(it + 3);
+    u.rows = kv_scalar(it + 4);
+    u.len = kv_scalar(it + 5);
+    u.pos0 = kv_scalar(it + 6);
+    u.rec0 = kv_scalar(it + 7);
+    u.rec1 = kv_scalar(it + 8);
+    u.slot = kv_scalar(it + 9);
+    u.ref = kv_scalar(it + 10);
+    u.per = p.per;
+    u.splits = 1;
+    return u.tile_row < u.rows;
 }
 
 // Eight channels of out.  (Fp32 calls are the kernels with PARTS == 2.)
@@ -255,11 +301,12 @@ __device__ inline float kv_max8(const float (&x)[8])
 }
 
 // A wave's query rows, 16 a tile, and what they see.
-template <int NC, int NT, int PARTS> struct KvRows {
+template <int NC, int NT, int PARTS, KvMode MODE> struct KvRows {
     f16x8 q[PARTS][NT][NC];
     float c[NT], slope[NT];                 // score of a product: c s + slope (t - pos), in powers of two
     int lo[NT], hi[NT];                     // the tokens that the lane's row sees
     int all_lo, all_hi;                     // that every row of the wave sees
+    int sinks, ref;                         // kKvSinks: first tokens that every row sees, whatever lo is; KvUnit::ref
 
     // A row is scaled by 2^e to a largest element in [2^14, 2^15) and rounded to fp16.
     __device__ void load(const KvAttn& a, const KvUnit& u, int row0)
@@ -349,6 +396,8 @@ template <int NC, int NT, int PARTS> struct KvRows {
         }
         all_lo = 0;
         all_hi = u.len;
+        if constexpr (MODE == kKvSinks) sinks = a.sinks;
+        if constexpr (MODE == kKvListed) ref = u.ref;
         if (a.causal) {
             // the first and the last row bound the others
             const int64_t p0 = u.pos0 + row0 / u.per, p1 = u.pos0 + (min(u.rows, row0 + 16 * NT) - 1) / u.per;
@@ -356,7 +405,9 @@ template <int NC, int NT, int PARTS> struct KvRows {
             if (a.window) all_lo = (int)max((int64_t)0, p1 - a.window + 1);
         }
     }
-    __device__ bool masked(int t0) const { return t0 > all_hi - kKvTok || t0 < all_lo; }
+    __device__ bool masked(int t0) const { return t0 > all_hi - kKvTok || (t0 < all_lo && (MODE != kKvSinks || t0 > sinks - kKvTok)); }
+    static constexpr bool kSinks = MODE == kKvSinks;
+    __device__ int from(int n) const { return MODE == kKvListed && ref >= 0 ? ref : hi[n] - 1; }
 };
 
 // The running softmax and the weighted sums of a wave's rows, o[t][k][n][e]: class k, row 4 j + e of tile t.
@@ -488,8 +539,8 @@ template <class T, int NT> struct KvSums {
     // s: the products times their key scales, of KR records that start at tokens t0; on return the probabilities
     // (0 where the row does not see the token).  masked: some row does not see all of them.  scales(y, g, x) gives
     // the lane's value scales; clear() is called if NaNs among them are to be taken as 0.
-    template <int KR, int NC, int PARTS, class F, class C>
-    __device__ void weigh(float (&s)[KR][NT][8], const KvRows<NC, NT, PARTS>& r, bool slopes, const int (&t0)[KR], bool masked, F scales, C clear)
+    template <int KR, class ROWS, class F, class C>
+    __device__ void weigh(float (&s)[KR][NT][8], const ROWS& r, bool slopes, const int (&t0)[KR], bool masked, F scales, C clear)
     {
         float big[NG];
 #pragma unroll
@@ -516,11 +567,11 @@ template <class T, int NT> struct KvSums {
 #pragma unroll
                 for (int y = 0; y < KR; ++y) {
                     const int t = t0[y] + 8 * ((threadIdx.x & 63) >> 4);
-                    const float base = r.slope[n] * (float)(t - (r.hi[n] - 1));
+                    const float base = r.slope[n] * (float)(t - r.from(n));
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         s[y][n][e] = fmaf(s[y][n][e], c[n], fmaf(r.slope[n], (float)e, base));
-                        s[y][n][e] = t + e >= r.lo[n] && t + e < r.hi[n] ? s[y][n][e] : -kKvInf;
+                        s[y][n][e] = (t + e >= r.lo[n] || (ROWS::kSinks && t + e < r.sinks)) && t + e < r.hi[n] ? s[y][n][e] : -kKvInf;
                     }
                     at[n] = fmaxf(at[n], kv_max8(s[y][n]));
                 }
@@ -704,235 +755,19 @@ constexpr int kv_few_occupancy(int dp, int group, int nt, int parts)
     return 2;
 }
 
+
 template <int DP, int GROUP, int NT, int PARTS>
 __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void kv_few_kernel(KvAttn a, KvPlan plan)
 {
-    using R = KvRec<DP, GROUP>;
-    using T = KvTiles<DP, GROUP>;
-    constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
-    const uint32_t unit = blockIdx.x / (uint32_t)plan.nsplit;
-    const int split = (int)(blockIdx.x - unit * plan.nsplit);
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int i = tid & 15, j = (tid & 63) >> 4;
-    const KvUnit u = kv_unit(a, plan, unit, tid == 0 && split == 0);
-    if (split >= u.splits || u.tile_row >= u.rows) return;
-    const int r1 = u.from(split + 1);
-    int r = u.from(split) + wave;
-
-    // A record's codes, and a word of each group: a key's (lanes 0 .. 31) or a value's.  The keys' registers
-    // are free once the scores are there and take the next record's keys; the values' likewise after
-    // the weighted sum.  The words' scales and zero points reach the lanes that need them through the
-    // wave's part of LDS.  (Read from memory by each of those lanes they took 18 registers a group and
-    // 32 more instructions.)
-    struct Words {
-        float s[NG][64];                                         // scales
-        uint16_t lo[NG][64], hi[NG][64];                         // -(1024 + z), -(1024 + 16 z) in fp16
-    };
-    constexpr int kRow = DP + 4;                                 // floats of a row (16-byte aligned, spread over the banks)
-    __shared__ __align__(16) union {
-        Words words[kKvWaves];
-        float acc[kKvWaves][16 * NT][kRow];
-    } shared;
-    Words& held = shared.words[wave];
-    const int lane = tid & 63;
-    const KvBits bits;
-    uint32_t k[2][NC], v[UT][4], word[NG];
-    const int64_t pages = a.c.pages_count;
-    const int32_t* table = a.table + u.b * a.width;
-    const int per = (int)a.c.per;
-    int pg = (uint32_t)r / (uint32_t)per, rem = r - pg * per;
-    int id = r < r1 ? table[pg] : 0;
-    const uint8_t* rec = a.c.pages;
-    bool here = false;                                           // whether the record is there (else any other is read, and not used)
-    // The address of record r, whose page number was read before; reads the one after it.
-    auto find = [&](int r) {
-        int page = __builtin_amdgcn_readfirstlane(id);
-        here = page >= 0 && page < pages;
-        if (!here) {
-            set_status(a.status, QE_ERR_ARG);
-            page = 0;
-        }
-        rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
-        rem += kKvWaves;
-        while (rem >= per) {
-            rem -= per;
-            ++pg;
-        }
-        if (r + kKvWaves < r1) id = table[pg];            // (in a vector register until it is needed: a wait for it now would be one for all loads)
-    };
-    auto keys = [&] {
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-            word[g] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)((lane < 32 ? R::kKeyWords : R::kValWords) + g * (4 * kKvTok) + 4 * (lane & 31)));
-#pragma unroll
-        for (int h = 0; h < 2; ++h) kv_words<NC>(rec + (uint32_t)(T::key_token(i, h) * R::kKeyRow + j * (4 * NC)), k[h]);
-    };
-    auto values = [&] {
-#pragma unroll
-        for (int t = 0; t < UT; ++t) kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(t, i) * (2 * kKvTok) + 16 * j), v[t]);
-    };
-    // (LDS serves a wave in order: what was read before is not overwritten.)
-    auto hold = [&](int t0) {
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            // words past the sequence's end are anything: no value scale of theirs may meet a 0
-            held.s[g][lane] = lane >= 32 && t0 > u.len - 1 - (lane & 31) ? 0.f : kv_scale(word[g]);
-            held.lo[g][lane] = (uint16_t)(0xE400u | (word[g] & 15u));
-            held.hi[g][lane] = (uint16_t)(0xE400u | (word[g] & 15u) << 4);
-        }
-        __builtin_amdgcn_wave_barrier();
-    };
-    auto first_token = [&](int r) { return here ? r * kKvTok : 0x7fffff00; };    // (of no record: past every sequence's end)
-    if (r < r1) {
-        find(r);
-        keys();
-        values();
-    }
-    KvRows<NC, NT, PARTS> rows;
-    rows.load(a, u, u.tile_row);
-    KvSums<T, NT> sums;
-    sums.clear();
-
-    int t0 = first_token(r);
-    if (r < r1) hold(t0);
-    for (; r < r1; r += kKvWaves) {
-        const bool masked = rows.masked(t0), more = r + kKvWaves < r1;
-        const int at[1] = {t0};
-        float s[1][NT][8];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            f32x4 acc[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t l = held.lo[g][T::key_token(i, h)], x = held.hi[g][T::key_token(i, h)], lo = l << 16 | l, hi = x << 16 | x;
-#pragma unroll
-                for (int c = g * T::CPG; c < (g + 1) * T::CPG && c < NC; ++c) {
-                    const f16x8 f = kv_key_frag(k[h][c], lo, hi, bits);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][c], acc[n][h]);
-                }
-            }
-            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&held.s[g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&held.s[g][8 * j + 4]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float sc = e < 4 ? s0[e] : s1[e - 4];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float x = acc[n][e >> 2][e & 3];
-                    s[0][n][e] = g == 0 ? sc * x : fmaf(sc, x, s[0][n][e]);
-                }
-            }
-        }
-        if (more) {
-            find(r + kKvWaves);
-            keys();
-        }
-        KvScales<1, NG> sv;
-        sv.load([&](int, int g) { return &held.s[g][32 + 8 * j]; });
-        sums.template weigh<1>(s, rows, a.slopes != nullptr, at, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            f16x8 pr[PARTS][NT];
-            float x[8];
-            sv.get(0, g, x);
-            sums.template weights<PARTS>(s[0], g, x, pr);
-            const u32x4 lo = *reinterpret_cast<const u32x4*>(&held.lo[g][32 + 8 * j]), hi = *reinterpret_cast<const u32x4*>(&held.hi[g][32 + 8 * j]);
-#pragma unroll
-            for (int t = 0; t < UT; ++t) {
-                if (T::group_of(t) != g) continue;
-                uint32_t w[4];
-#pragma unroll
-                for (int p = 0; p < 4; ++p) w[p] = T::kHalf ? v[t][p] >> (i & 8) : v[t][p];
-#pragma unroll
-                for (int c = 0; c < CL; ++c) {
-                    uint32_t pair[4];
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) pair[p] = kv_code_pair(w[p] >> (c >= 2 ? 8 : 0), c & 1 ? bits.high : bits.low, c & 1 ? hi[p] : lo[p], bits);
-                    const f16x8 f = kv_frag(pair[0], pair[1], pair[2], pair[3]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p) sums.o[t][c][n] = kv_mfma(f, pr[p][n], sums.o[t][c][n]);
-                }
-            }
-        }
-        if (more) {
-            values();
-            t0 = first_token(r + kKvWaves);
-            hold(t0);
-        }
-        sums.pin();
-    }
-    sums.finish();
-
-    // every wave to the common maximum, divided by the common mass (sums of large values would pass the
-    // largest number before it), then sums over the waves
-    __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT], rtop[16 * NT], rmass[16 * NT];
-    auto& acc = shared.acc;                                      // (written after a barrier that ends the use of the words)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-        if (j == 0) {
-            wtop[wave][16 * n + i] = sums.top[n];
-            wmass[wave][16 * n + i] = sums.mass[n];
-        }
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        float m = -kKvInf, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kKvWaves; ++w) m = fmaxf(m, wtop[w][16 * n + i]);
-#pragma unroll
-        for (int w = 0; w < kKvWaves; ++w) {
-            const float t = wtop[w][16 * n + i];
-            l = fmaf(t == m ? 1.f : __builtin_amdgcn_exp2f(t - m), wmass[w][16 * n + i], l);
-        }
-        if (wave == 0 && j == 0) {
-            rtop[16 * n + i] = m;
-            rmass[16 * n + i] = l;
-        }
-        sums.octets(n, m == sums.top[n] ? 0.f : sums.top[n] - m, l == 0.f ? 0.f : 1.f / l, [&](int d, const float* x) {
-#pragma unroll
-            for (int y = 0; y < 8; y += 4) *reinterpret_cast<f32x4*>(&acc[wave][16 * n + i][d + y]) = f32x4{x[y], x[y + 1], x[y + 2], x[y + 3]};
-        });
-    }
-    __syncthreads();
-    for (int x = tid; x < 16 * NT * (DP / 8); x += 256) {
-        const int rr = x / (DP / 8), d = 8 * (x - rr * (DP / 8)), row = u.tile_row + rr;
-        if (row >= u.rows) break;
-        f32x4 sum[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const f32x4 s0 = *reinterpret_cast<const f32x4*>(&acc[0][rr][d + 4 * y]), s1 = *reinterpret_cast<const f32x4*>(&acc[1][rr][d + 4 * y]);
-            const f32x4 s2 = *reinterpret_cast<const f32x4*>(&acc[2][rr][d + 4 * y]), s3 = *reinterpret_cast<const f32x4*>(&acc[3][rr][d + 4 * y]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[y][e] = (s0[e] + s1[e]) + (s2[e] + s3[e]);
-        }
-        const float m = rtop[rr], l = rmass[rr];
-        if (u.splits > 1) {
-            const int64_t slot = ((int64_t)unit * plan.nsplit + split) * plan.rows + rr;
-#pragma unroll
-            for (int y = 0; y < 2; ++y) *reinterpret_cast<f32x4*>(plan.part + slot * DP + d + 4 * y) = sum[y];
-            if (d == 0) {
-                const int e = (int)(__float_as_uint(l) >> 23) - 127;      // (of no mass: m is -inf)
-                plan.stat[2 * slot] = m + (float)e;
-                plan.stat[2 * slot + 1] = l * __uint_as_float((uint32_t)(127 - kKvJoinLog2 - e) << 23);
-            }
-        } else {
-            const int qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
-            float out[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = sum[e >> 2][e & 3];
-            if (d < a.c.dim) kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, out);
-            if (a.lse && d == 0) a.lse[(u.first + qi) * a.heads + head] = kv_lse(m, l);
-        }
-    }
+    constexpr KvMode MODE = kKvPlain;
+#include "kv_attn_few.h"
+}
+// (The bodies are included: as inlined functions of the kernels' arguments they took other registers, and one instance in
+// groups of 32 spilled 27 instead of 10, another 11 instead of none.)
+template <int DP, int GROUP, int NT, int PARTS, KvMode MODE>
+__global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void kv_few_mode_kernel(KvAttn a, KvPlan plan)
+{
+#include "kv_attn_few.h"
 }
 
 // ---------------------------------------------------------------- many rows
@@ -946,229 +781,21 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
 // 682 us; with every wave converting its own (the few-row form) 831.
 constexpr int kv_stage_records(int dp) { return dp <= 128 ? 2 : 1; }
 
+
 template <int DP, int GROUP, int NT, int PARTS>
 __global__ __launch_bounds__(256, 2) void kv_many_kernel(KvAttn a, KvPlan plan)
 {
-    using R = KvRec<DP, GROUP>;
-    using T = KvTiles<DP, GROUP>;
-    constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;
-    constexpr int KR = kv_stage_records(DP), W = kKvWaves / KR;  // records of a stage, waves that convert one
-    // Records whose exponentials are taken together: all of a stage, where the registers hold them.  Two tiles
-    // of two groups spill (2048 queries of 32 heads of 128 in groups of 64 over 8192 tokens: 547 us
-    // together, 450 one by one; 96 channels over 4096 226 / 228; groups of 128 over 16384 696 / 737, 64
-    // channels in groups of 64 over 8192 273 / 296).
-    constexpr int KW = NG == 2 && NT == 2 && DP > 64 ? 1 : KR;
-    constexpr int CW = KR == 2 ? NC : (NC + 1) / 2;              // key products a wave converts
-    constexpr int VW = T::kHalf ? (UT + 1) / 2 : UT, VK = KR;    // unit tiles and classes
-    constexpr int SW = KR == 2 ? (NG + 1) / 2 : (NG + 3) / 4;    // scales a lane converts
-    constexpr int SG = SW * (KR == 2 ? 2 : 4);
-    struct Stage {
-        f16x8 k[KR][2][NC][64], v[KR][UT][CL][64];
-        float ks[KR][SG][kKvTok], vs[KR][SG][kKvTok];            // (groups past NG: what lanes without a group write)
-        int at[KR];                                              // the records' first tokens
-    };
-    __shared__ Stage stage[2];
-    // workgroups of an XCD (every eighth) get a contiguous stretch of units: rows of the same keys
-    // share its L2
-    const uint32_t wg = blockIdx.x, q8 = gridDim.x / 8, r8 = gridDim.x % 8, x8 = wg & 7;
-    const uint32_t unit = x8 * q8 + min(x8, r8) + (wg >> 3);
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int i = tid & 15, j = lane >> 4;
-    const KvUnit u = kv_unit(a, plan, unit, tid == 0);
-    if (u.tile_row >= u.rows) return;
-    const int r0 = u.rec0, r1 = u.rec1;
-    const int row0 = u.tile_row + wave * (16 * NT);
-
-    // what the wave converts: of record `part` of a stage, key half kh from channel block kc on, value
-    // classes vk .. of the unit tiles vt, vt + 2, .. (groups of 32) or all
-    const int part = wave / W, q = wave % W;
-    const int kh = q & 1, kc = KR == 2 ? 0 : (q >> 1) * CW;
-    const int vk = T::kHalf ? (KR == 2 ? 0 : q & 1) : KR == 2 ? 2 * (q & 1) : q;
-    const int vt = T::kHalf ? (KR == 2 ? q & 1 : q >> 1) : 0;
-    const KvBits bits;
-    const uint32_t vmask = vk & 1 ? bits.high : bits.low, vshift = vk & 1 ? 4 : 0;   // (KR == 1)
-    const int token = T::key_token(i, kh);
-    constexpr int VG = T::kHalf ? VW : NG;                       // value groups whose zero points the wave needs
-    uint32_t k[CW], kz[CW], v[VW][4], vw[VG][8], word[SW];
-
-    const int64_t pages = a.c.pages_count;
-    const int32_t* table = a.table + u.b * a.width;
-    const int per = (int)a.c.per;
-    // the wave's record of the next stage to be loaded, its page's place in the table and its place in the page
-    int next = max(0, min(r0 + part, r1 - 1)), pg = (uint32_t)next / (uint32_t)per, rem = next - pg * per;
-    int id = r0 < r1 ? table[pg] : 0;
-    bool here = false;                                           // whether the record is there (else any other is read, and not used)
-    // Starts the loads of the wave's share of the next stage, whose page number was read before, and reads
-    // the one after it.  Past the last record it is loaded again.
-    auto start = [&] {
-        int page = __builtin_amdgcn_readfirstlane(id);
-        here = page >= 0 && page < pages;
-        if (!here) {
-            if (lane == 0) set_status(a.status, QE_ERR_ARG);
-            page = 0;
-        }
-        const uint8_t* rec = a.c.pages + (((int64_t)page * a.c.heads + u.kvh) * per + rem) * R::kBytes;
-        kv_words<CW>(rec + (uint32_t)(token * R::kKeyRow + j * (4 * NC)) + 4 * kc, k);
-#pragma unroll
-        for (int x = 0; x < CW; ++x)
-            kz[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)(R::kKeyWords + min((kc + x) / T::CPG, NG - 1) * (4 * kKvTok) + 4 * token));
-#pragma unroll
-        for (int x = 0; x < VG; ++x)
-            kv_words<8>(rec + (uint32_t)(R::kValWords + (T::kHalf ? min(vt + 2 * x, NG - 1) : x) * (4 * kKvTok) + 32 * j), vw[x]);
-#pragma unroll
-        for (int x = 0; x < VW; ++x)
-            kv_words<4>(rec + (uint32_t)(R::kVal + T::unit(T::kHalf ? min(vt + 2 * x, UT - 1) : x, i) * (2 * kKvTok) + 16 * j), v[x]);
-#pragma unroll
-        for (int x = 0; x < SW; ++x) {
-            const bool key = KR == 2 ? kh == 0 : lane < 32;
-            const int g = KR == 2 ? min((lane >> 5) + 2 * x, NG - 1) : min(q + 4 * x, NG - 1);
-            word[x] = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)((key ? R::kKeyWords : R::kValWords) + g * (4 * kKvTok) + 4 * (lane & 31)));
-        }
-        const int step = min(KR, r1 - 1 - next);
-        next += step;
-        rem += step;
-        while (rem >= per) {
-            rem -= per;
-            ++pg;
-        }
-        id = table[pg];                                   // (in a vector register until it is needed: a wait for it now would be one for all loads)
-    };
-    // r: the first record of the stage
-    auto convert = [&](Stage& st, int r) {
-#pragma unroll
-        for (int x = 0; x < CW; ++x) {
-            if (KR == 1 && NC % 2 != 0 && kc + x >= NC) continue;
-            uint32_t lo, hi;
-            kv_key_zero(kz[x], lo, hi, bits);
-            st.k[part][kh][kc + x][lane] = kv_key_frag(k[x], lo, hi, bits);
-        }
-#pragma unroll
-        for (int x = 0; x < VW; ++x) {
-            const int t = T::kHalf ? vt + 2 * x : x;
-            if (T::kHalf && UT % 2 != 0 && t >= UT) continue;
-            uint32_t f[VK][4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const uint32_t w0 = vw[T::kHalf ? x : T::group_of(x)][2 * p], w1 = vw[T::kHalf ? x : T::group_of(x)][2 * p + 1];
-                const uint32_t w = v[x][p] >> (T::kHalf ? i & 8 : vk & 2 ? 8 : 0);
-                if constexpr (KR == 2) {
-                    uint32_t lo, hi;
-                    kv_value_zero(w0, w1, lo, hi, bits);
-                    f[0][p] = kv_code_pair(w, bits.low, lo, bits);
-                    f[1][p] = kv_code_pair(w, bits.high, hi, bits);
-                } else {
-                    const uint32_t z = ((__builtin_amdgcn_perm(w1, w0, 0x05040100u) << vshift) & vmask) | bits.z;
-                    f[0][p] = kv_code_pair(w, vmask, z, bits);
-                }
-            }
-#pragma unroll
-            for (int y = 0; y < VK; ++y) st.v[part][t][vk + y][lane] = kv_frag(f[y][0], f[y][1], f[y][2], f[y][3]);
-        }
-#pragma unroll
-        for (int x = 0; x < SW; ++x) {
-            const bool key = KR == 2 ? kh == 0 : lane < 32;
-            const int g = KR == 2 ? (lane >> 5) + 2 * x : q + 4 * x;
-            float sc = kv_scale(word[x]);
-            // (words past the sequence's end, or of a record that is not there, are anything: no scale of theirs may meet a 0)
-            sc = !key && (!here || (r + part) * kKvTok + (lane & 31) >= u.len) ? 0.f : sc;
-            (key ? st.ks : st.vs)[part][g][lane & 31] = sc;
-        }
-        // (past the last record, or on a page that is not there: past every sequence's end)
-        st.at[part] = here && r + part < r1 ? (r + part) * kKvTok : 0x7fffff00;
-    };
-
-    if (r0 < r1) start();
-    KvRows<NC, NT, PARTS> rows;
-    rows.load(a, u, min(row0, u.rows - 1));
-    KvSums<T, NT> sums;
-    sums.clear();
-    if (r0 < r1) {
-        convert(stage[0], r0);
-        start();
-    }
-    __syncthreads();
-    for (int r = r0, b = 0; r < r1; r += KR, b ^= 1) {
-        convert(stage[b ^ 1], r + KR);
-        const Stage& st = stage[b];
-#pragma unroll
-        for (int y0 = 0; y0 < KR; y0 += KW) {
-            float s[KW][NT][8];
-            int t0[KW];
-            bool masked = false;
-#pragma unroll
-            for (int y = 0; y < KW; ++y) {
-                t0[y] = __builtin_amdgcn_readfirstlane(st.at[y0 + y]);
-                masked = masked || rows.masked(t0[y]);
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    f32x4 acc[NT][2];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int c = g * T::CPG; c < (g + 1) * T::CPG && c < NC; ++c)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const f16x8 f = st.k[y0 + y][h][c][lane];
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int p = 0; p < PARTS; ++p) acc[n][h] = kv_mfma(f, rows.q[p][n][c], acc[n][h]);
-                        }
-                    const f32x4 s0 = *reinterpret_cast<const f32x4*>(&st.ks[y0 + y][g][8 * j]), s1 = *reinterpret_cast<const f32x4*>(&st.ks[y0 + y][g][8 * j + 4]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float sc = e < 4 ? s0[e] : s1[e - 4], x = acc[n][e >> 2][e & 3];
-                            s[y][n][e] = g == 0 ? sc * x : fmaf(sc, x, s[y][n][e]);
-                        }
-                }
-            }
-            if (y0 == 0) start();
-            KvScales<KW, NG> sv;
-            sv.load([&](int y, int g) { return &st.vs[y0 + y][g][8 * j]; });
-            sums.template weigh<KW>(s, rows, a.slopes != nullptr, t0, masked, [&](int y, int g, float (&x)[8]) { sv.get(y, g, x); }, [&] { sv.clear(); });
-#pragma unroll
-            for (int y = 0; y < KW; ++y)
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    f16x8 pr[PARTS][NT];
-                    float x[8];
-                    sv.get(y, g, x);
-                    sums.template weights<PARTS>(s[y], g, x, pr);
-#pragma unroll
-                    for (int t = 0; t < UT; ++t) {
-                        if (T::group_of(t) != g) continue;
-#pragma unroll
-                        for (int c = 0; c < CL; ++c) {
-                            const f16x8 f = st.v[y0 + y][t][c][lane];
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int p = 0; p < PARTS; ++p) sums.o[t][c][n] = kv_mfma(f, pr[p][n], sums.o[t][c][n]);
-                        }
-                    }
-                }
-        }
-        sums.pin();
-        __syncthreads();
-    }
-    if (row0 >= u.rows) return;
-    sums.finish();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int row = row0 + 16 * n + i, qi = row / u.per, head = u.kvh * u.per + row - qi * u.per;
-        sums.octets(n, 0.f, sums.mass[n] == 0.f ? 0.f : 1.f / sums.mass[n], [&](int d, const float* x) {
-            if (row < u.rows && d < a.c.dim) kv_out8<PARTS>(a, (u.first + qi) * a.ot + head * a.oh + d, x);
-        });
-        if (row < u.rows && j == 0 && a.lse) a.lse[(u.first + qi) * a.heads + head] = kv_lse(sums.top[n], sums.mass[n]);
-    }
+    constexpr KvMode MODE = kKvPlain;
+#include "kv_attn_many.h"
+}
+template <int DP, int GROUP, int NT, int PARTS, KvMode MODE>
+__global__ __launch_bounds__(256, 2) void kv_many_mode_kernel(KvAttn a, KvPlan plan)
+{
+#include "kv_attn_many.h"
 }
 
 // Joins the splits of a row: one workgroup a row, whose waves take the splits in turn.
-template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a, KvPlan plan)
+template <int DP, KvMode MODE> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a, KvPlan plan)
 {
     constexpr int C = (DP + 63) / 64;
     __shared__ float sum[kKvWaves][DP], mass[kKvWaves];
@@ -1178,7 +805,7 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a
     // (plan.rows is a power of two)
     const uint32_t unit = (uint32_t)(at >> plan.rows_log2);
     const int rr = (int)(at & (plan.rows - 1));
-    const KvUnit u = kv_unit(a, plan, unit, false);
+    const KvUnit u = kv_unit<MODE>(a, plan, unit, false);
     const int row = u.tile_row + rr;
     if (u.splits <= 1 || row >= u.rows) return;
     const int64_t slot = (int64_t)unit * plan.nsplit * plan.rows + rr;
@@ -1211,10 +838,10 @@ template <int DP> __global__ __launch_bounds__(256) void kv_join_kernel(KvAttn a
 
 // The same for few splits (kKvFewSplits at most) of many rows: one workgroup a unit, a thread 8 channels of a row,
 // four splits on the way at a time.
-template <int DP> __global__ __launch_bounds__(256) void kv_join_unit_kernel(KvAttn a, KvPlan plan)
+template <int DP, KvMode MODE> __global__ __launch_bounds__(256) void kv_join_unit_kernel(KvAttn a, KvPlan plan)
 {
     const uint32_t unit = blockIdx.x;
-    const KvUnit u = kv_unit(a, plan, unit, false);
+    const KvUnit u = kv_unit<MODE>(a, plan, unit, false);
     if (u.splits <= 1) return;
     const float2* const stat = reinterpret_cast<const float2*>(plan.stat);
     for (int x = threadIdx.x; x < plan.rows * (DP / 8); x += 256) {
@@ -1266,6 +893,14 @@ struct KvForm { bool many; int nt; };
 constexpr int kv_many_nt(int dp, int group, bool f32) { return dp <= 128 && !f32 && (group > 32 || dp == 64) ? 2 : 1; }
 constexpr int kv_few_nt(int dp, int group, bool f32) { return dp <= 128 && !f32 && (group > 32 || dp < 128) ? 2 : 1; }
 
+template <int DP, KvMode MODE> void kv_join_launch(const KvAttn& a, const KvPlan& plan, hipStream_t s)
+{
+    if (plan.nsplit > kKvFewSplits)
+        hipLaunchKernelGGL((kv_join_kernel<DP, MODE>), grid_xy(plan.units * plan.rows, 256), dim3(256), 0, s, a, plan);
+    else if (plan.nsplit > 1)
+        hipLaunchKernelGGL((kv_join_unit_kernel<DP, MODE>), dim3((unsigned)plan.units), dim3(256), 0, s, a, plan);
+}
+
 template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm form, dim3 grid, hipStream_t s)
 {
     kv_dispatch_group<DP>(a.group, [&](auto shape) {
@@ -1281,10 +916,7 @@ template <int DP> void kv_attn_width(const KvAttn& a, const KvPlan& plan, KvForm
             hipLaunchKernelGGL((kv_few_kernel<DP, G, kv_few_nt(DP, G, false), 1>), grid, dim3(256), 0, s, a, plan);
         }
     });
-    if (plan.nsplit > kKvFewSplits)
-        hipLaunchKernelGGL((kv_join_kernel<DP>), grid_xy(plan.units * plan.rows, 256), dim3(256), 0, s, a, plan);
-    else if (plan.nsplit > 1)
-        hipLaunchKernelGGL((kv_join_unit_kernel<DP>), dim3((unsigned)plan.units), dim3(256), 0, s, a, plan);
+    kv_join_launch<DP, kKvPlain>(a, plan, s);
 }
 
 }  // namespace qe

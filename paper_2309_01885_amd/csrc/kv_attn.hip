@@ -1,13 +1,18 @@
 // How an attention call over the 4-bit cache is cut into workgroups.
-#include "kv_attn.h"
+#include "kv_attn_modes.h"
 
 namespace qe {
 
 extern template void kv_attn_width<64>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
+extern template void kv_sinks_width<64>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
 extern template void kv_attn_width<96>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
+extern template void kv_sinks_width<96>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
 extern template void kv_attn_width<128>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
+extern template void kv_sinks_width<128>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
 extern template void kv_attn_width<192>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
+extern template void kv_sinks_width<192>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
 extern template void kv_attn_width<256>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
+extern template void kv_sinks_width<256>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
 
 namespace {
 
@@ -92,11 +97,10 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
 {
     KvAttn a = call;
     const int dp = kv_dp(a.c.dim);
-    const size_t size = a.dtype == QE_F32 ? 4 : 2;
-    a.vec_q = ((uintptr_t)a.q | (uint64_t)a.qt * size | (uint64_t)a.qh * size) % 16 == 0;
-    a.vec_o = ((uintptr_t)a.out | (uint64_t)a.ot * size | (uint64_t)a.oh * size) % 16 == 0;
+    kv_attn_vec(a);
     int64_t records = a.width * a.c.per;
-    if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2);
+    if (a.window) records = std::min<int64_t>(records, (a.window + a.max_q) / kKvTok + 2 + cdiv(a.sinks, kKvTok));
+    else a.sinks = 0;                                      // (every token is visible)
     const Sizes z = sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, records, a.dtype == QE_F32);
     KvPlan plan{};
     plan.row_tiles = z.row_tiles;
@@ -108,12 +112,16 @@ qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
     plan.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kStatusBytes);
     plan.stat = reinterpret_cast<float*>(reinterpret_cast<char*>(plan.part) + align256(part_floats(z, dp, plan.nsplit) * 4));
     const dim3 grid((unsigned)(z.units * plan.nsplit));
+    auto width = [&](auto dp) {
+        if (a.sinks) kv_sinks_width<dp>(a, plan, z.form, grid, s);
+        else kv_attn_width<dp>(a, plan, z.form, grid, s);
+    };
     switch (dp) {
-        case 64: kv_attn_width<64>(a, plan, z.form, grid, s); break;
-        case 96: kv_attn_width<96>(a, plan, z.form, grid, s); break;
-        case 128: kv_attn_width<128>(a, plan, z.form, grid, s); break;
-        case 192: kv_attn_width<192>(a, plan, z.form, grid, s); break;
-        default: kv_attn_width<256>(a, plan, z.form, grid, s);
+        case 64: width(std::integral_constant<int, 64>()); break;
+        case 96: width(std::integral_constant<int, 96>()); break;
+        case 128: width(std::integral_constant<int, 128>()); break;
+        case 192: width(std::integral_constant<int, 192>()); break;
+        default: width(std::integral_constant<int, 256>());
     }
     return hipGetLastError() == hipSuccess ? QE_OK : QE_ERR_HIP;
 }

@@ -1,0 +1,7 @@
+// Attention over the 4-bit cache with first tokens that stay visible, and by lists: heads padded to 192 channels.
+#include "kv_attn_modes.h"
+
+namespace qe {
+template void kv_sinks_width<192>(const KvAttn&, const KvPlan&, KvForm, dim3, hipStream_t);
+template void kv_listed_width<192>(const KvAttn&, const KvPlan&, const KvShared&, KvForm, KvForm, hipStream_t);
+}

@@ -7,34 +7,11 @@
 //
 // One workgroup does the sums (a thread a stretch of sequences) and the pages that go back; the tokens' slots, and with
 // them the pages that are taken (each by the token that is first on it), are a thread a token.
-#include "kv.h"
+#include "kv_scan.h"
 
 namespace qe {
 
 namespace {
-
-constexpr int kExtThreads = 1024;
-
-// The inclusive sum over the workgroup's threads; all: the sum of all.  part: 16 numbers of LDS.
-__device__ inline int64_t scan_add(int64_t x, int64_t* part, int64_t& all)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const int64_t y = __shfl_up(x, m);
-        x += lane >= m ? y : 0;
-    }
-    if (lane == 63) part[wave] = x;
-    __syncthreads();
-    int64_t before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < kExtThreads / 64; ++w) {
-        before += w < wave ? part[w] : 0;
-        all += part[w];
-    }
-    return x + before;
-}
 
 struct Change {
     int64_t tokens, give, need;
@@ -66,16 +43,10 @@ __device__ inline Change change_of(const KvExtend& a, int64_t b, bool report)
     return c;
 }
 
-// The sequence of token i (q_start[b] <= i < q_start[b + 1]); batch where it is none's.
+// The sequence of token i: the last b with q_start[b] <= i (batch where it is none's).
 template <class I> __device__ inline int64_t sequence_of(const I* q_start, int64_t batch, int64_t i)
 {
-    int64_t lo = 0, hi = batch;                          // the first b with q_start[b + 1] > i
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (q_start[mid + 1] > i) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo;
+    return last_at_most(q_start, batch + 1, i);
 }
 
 __device__ inline void place(const KvExtend& a, int64_t i, int64_t b, const KvExtendSeq* seqs, int64_t start, int64_t top)
@@ -107,13 +78,13 @@ __device__ inline void place(const KvExtend& a, int64_t i, int64_t b, const KvEx
     a.positions[i] = pos;
 }
 
-__global__ __launch_bounds__(kExtThreads) void kv_extend_kernel(KvExtend a, bool fill)
+__global__ __launch_bounds__(kScanThreads) void kv_extend_kernel(KvExtend a, bool fill)
 {
-    __shared__ int64_t part[4][kExtThreads / 64];
-    __shared__ int32_t start[kExtThreads + 1];
-    __shared__ KvExtendSeq seqs[kExtThreads];
+    __shared__ int64_t part[4][kScanThreads / 64];
+    __shared__ int32_t start[kScanThreads + 1];
+    __shared__ KvExtendSeq seqs[kScanThreads];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int64_t per = (a.batch + kExtThreads - 1) / kExtThreads;
+    const int64_t per = (a.batch + kScanThreads - 1) / kScanThreads;
     const int64_t b0 = min(tid * per, a.batch), b1 = min(b0 + per, a.batch);
     int64_t tokens = 0, give = 0, need = 0;
     Change c = {};
@@ -183,7 +154,7 @@ __global__ __launch_bounds__(kExtThreads) void kv_extend_kernel(KvExtend a, bool
     __syncthreads();                                     // (also: every thread has read free_count, and the pages that go back are there)
     if (tid == 0) {
 #pragma unroll
-        for (int w = 0; w < kExtThreads / 64; ++w) taken = max(taken, part[3][w]);
+        for (int w = 0; w < kScanThreads / 64; ++w) taken = max(taken, part[3][w]);
         const int32_t end = (int32_t)min(all_tokens, a.total);
         a.q_start[a.batch] = end;
         start[fill ? a.batch : 0] = end;
@@ -193,7 +164,7 @@ __global__ __launch_bounds__(kExtThreads) void kv_extend_kernel(KvExtend a, bool
     }
     if (!fill) return;
     __syncthreads();
-    for (int64_t i = tid; i < a.total; i += kExtThreads) {
+    for (int64_t i = tid; i < a.total; i += kScanThreads) {
         const int64_t b = sequence_of(start, a.batch, i);
         place(a, i, b, seqs, b < a.batch ? start[b] : 0, top);
     }
@@ -231,8 +202,8 @@ qe_status launch_kv_extend(const KvExtend& call, void* ws, hipStream_t s)
     KvExtend a = call;
     a.top = reinterpret_cast<int64_t*>(static_cast<char*>(ws) + kStatusBytes);
     a.seqs = reinterpret_cast<KvExtendSeq*>(static_cast<char*>(ws) + 2 * kStatusBytes);
-    const bool fill = a.batch <= kExtThreads && a.total <= kFillInPlace;
-    hipLaunchKernelGGL(kv_extend_kernel, dim3(1), dim3(kExtThreads), 0, s, a, fill);
+    const bool fill = a.batch <= kScanThreads && a.total <= kFillInPlace;
+    hipLaunchKernelGGL(kv_extend_kernel, dim3(1), dim3(kScanThreads), 0, s, a, fill);
     if (!fill && a.total > 0) hipLaunchKernelGGL(kv_fill_kernel, dim3((unsigned)cdiv(a.total, kFillTokens)), dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? QE_OK : QE_ERR_HIP;
 }

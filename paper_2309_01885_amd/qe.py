@@ -99,6 +99,13 @@ SIGNATURES = {
     "qe_kv_attn": (_int, [_vp, _int, _i64, _int, _int, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _int, _int,
                           _int, _vp, _i64, _vp, _f32, _int, _int, _vp, _vp, _i64, _i64, _vp, _vp, _sz,
                           _vp]),
+    "qe_kv_attn_sinks": (_int, [_vp, _int, _i64, _int, _int, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _int, _int,
+                                _int, _vp, _i64, _vp, _f32, _int, _int, _int, _vp, _vp, _i64, _i64, _vp, _vp, _sz,
+                                _vp]),
+    "qe_kv_attn_shared_workspace_size": (_sz, [_i64, _i64, _i64, _int, _int, _int, _i64]),
+    "qe_kv_attn_shared": (_int, [_vp, _int, _i64, _int, _int, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _int, _int,
+                                 _int, _vp, _i64, _vp, _vp, _vp, _i64, _f32, _int, _vp, _vp, _i64, _i64, _vp, _vp, _sz,
+                                 _vp]),
 }
 
 _lib = None
@@ -606,30 +613,15 @@ def kv_attn_workspace_size(total: int, batch: int, max_q: int, heads: int, kv_he
     return int(load().qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim))
 
 
-def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
-            group: int = 64, q_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None,
-            scale: Optional[float] = None, causal: bool = True, window: int = 0,
-            slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-            lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, check: bool = False,
-            stream=None) -> torch.Tensor:
-    """Attention of Q (total x heads x dim) over the 4-bit cache (qe_kv_attn).
-
-    table (int32, sequences x pages) and lengths (int32) describe the sequences; q_start (int32,
-    sequences + 1) and max_q their queries, without them total / sequences queries each.
-    scale: 1 / sqrt(dim) unless given.  window: 0 for none; one wider than every sequence hides nothing.  lse: None or float32, total x heads, written.  The call does
-    not wait for the device; check=True does, and raises if it met a bad page number, length or
-    query range (sync_status(ws) tells later otherwise).  An output or a workspace that the call makes is
-    a tensor of `stream`; rows of it that are no sequence's are not written.  The kernels cut their work for
-    sequences that fill the table, so a table much wider than they are costs time.  No gradient:
-    the output has no graph."""
-    shape, dtype = Q.shape, Q.dtype
-    if len(shape) != 3 or dtype not in _DTYPES:
+def _attn_queries(Q, pages, table, group, q_start, max_q):
+    """What kv_attn and kv_attn_shared check first: (total, heads, dim, batch, width, max_q, cache)."""
+    if len(Q.shape) != 3 or Q.dtype not in _DTYPES:
         _bad("Q", Q, "total x heads x dim in float32, float16 or bfloat16")
     if table.dim() != 2:
         _bad("table", table, "sequences x pages")
-    total, heads, dim = shape
+    total, heads, dim = Q.shape
     batch, width = table.shape
-    num, page, kv, dev = _pages(pages, dim, group)
+    cache = _pages(pages, dim, group)
     if q_start is None:
         if max_q is None:
             max_q = total // batch if batch else 0
@@ -637,9 +629,32 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
             raise ValueError(f"{total} queries are not {max_q} for each of {batch} sequences: give q_start")
     elif max_q is None:
         raise ValueError("q_start needs max_q, the largest number of queries of a sequence")
-    shape = (total, heads, dim)
+    return total, heads, dim, batch, width, max_q, cache
+
+
+def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+            group: int = 64, q_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None,
+            scale: Optional[float] = None, causal: bool = True, window: int = 0,
+            slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+            lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, check: bool = False,
+            stream=None, sinks: int = 0) -> torch.Tensor:
+    """Attention of Q (total x heads x dim) over the 4-bit cache (qe_kv_attn, qe_kv_attn_sinks).
+
+    table (int32, sequences x pages) and lengths (int32) describe the sequences; q_start (int32,
+    sequences + 1) and max_q their queries, without them total / sequences queries each.
+    scale: 1 / sqrt(dim) unless given.  window: 0 for none; one wider than every sequence hides nothing.  sinks: so many
+    first tokens stay visible beside the window.  lse: None or float32, total x heads, written.  The call does
+    not wait for the device; check=True does, and raises if it met a bad page number, length or
+    query range (sync_status(ws) tells later otherwise).  An output or a workspace that the call makes is
+    a tensor of `stream`; rows of it that are no sequence's are not written.  The kernels cut their work for
+    sequences that fill the table, so a table much wider than they are costs time.  No gradient:
+    the output has no graph."""
+    total, heads, dim, batch, width, max_q, (num, page, kv, dev) = _attn_queries(Q, pages, table, group, q_start, max_q)
+    shape, dtype = (total, heads, dim), Q.dtype
     if not -0x80000000 <= window <= 0x7fffffff:      # (a C int would take its low bits: 2^32 as no window)
         window = 0x7fffffff if window > 0 else -1
+    if not -0x80000000 <= sinks <= 0x7fffffff:
+        sinks = 0x7fffffff if sinks > 0 else -1
     if out is None:
         out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
     qt, qh = _heads(Q, "Q", shape, dtype, dev)
@@ -647,16 +662,66 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
     if ws is None:
         need = kv_attn_workspace_size(total, batch, max_q, heads, kv, dim)
         ws = _on(stream, lambda: workspace(need, pages.device))
-    code = load().qe_kv_attn(Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
-                             _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
-                             num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
-                             _flat(lengths, "lengths", torch.int32, dev, batch),
-                             dim ** -0.5 if scale is None else scale, 1 if causal else 0, window,
-                             _flat(slopes, "slopes", torch.float32, dev, heads), out.data_ptr(), ot, oh,
-                             _flat(lse, "lse", torch.float32, dev, total * heads),
-                             _flat(ws, "ws", torch.uint8, dev), ws.numel(), _raw_stream(dev, stream))
+    masks = (1 if causal else 0, window, sinks) if sinks else (1 if causal else 0, window)
+    code = (load().qe_kv_attn_sinks if sinks else load().qe_kv_attn)(
+        Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
+        _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
+        num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
+        _flat(lengths, "lengths", torch.int32, dev, batch),
+        dim ** -0.5 if scale is None else scale, *masks,
+        _flat(slopes, "slopes", torch.float32, dev, heads), out.data_ptr(), ot, oh,
+        _flat(lse, "lse", torch.float32, dev, total * heads),
+        _flat(ws, "ws", torch.uint8, dev), ws.numel(), _raw_stream(dev, stream))
     if code:
         raise QEError(code, "qe_kv_attn")
     if check:
         _finish(ws, check, "qe_kv_attn", stream)
+    return out
+
+
+def kv_attn_sinks(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, window: int,
+                  sinks: int, **more) -> torch.Tensor:
+    """kv_attn with a window beside which the first `sinks` tokens stay visible (qe_kv_attn_sinks)."""
+    return kv_attn(Q, pages, table, lengths, window=window, sinks=sinks, **more)
+
+
+def kv_attn_shared_workspace_size(total: int, batch: int, max_q: int, heads: int, kv_heads: int, dim: int,
+                                  groups: int) -> int:
+    return int(load().qe_kv_attn_shared_workspace_size(total, batch, max_q, heads, kv_heads, dim, groups))
+
+
+def kv_attn_shared(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                   groups: torch.Tensor, shared: torch.Tensor, group: int = 64, q_start: Optional[torch.Tensor] = None,
+                   max_q: Optional[int] = None, scale: Optional[float] = None, causal: bool = True,
+                   slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, check: bool = False,
+                   stream=None) -> torch.Tensor:
+    """kv_attn of sequences that begin with the same pages, which are read once for a group (qe_kv_attn_shared).
+
+    The sequences groups[g] .. groups[g + 1] - 1 (int32, groups + 1 ascending entries) have the same first shared[g]
+    (int32) entries in their rows of table; a row's lengths count the shared tokens.  The result is kv_attn's up to
+    the rounding of sums.  The other arguments are kv_attn's; kv_attn_shared_workspace_size gives the workspace."""
+    total, heads, dim, batch, width, max_q, (num, page, kv, dev) = _attn_queries(Q, pages, table, group, q_start, max_q)
+    shape, dtype = (total, heads, dim), Q.dtype
+    n = shared.numel()
+    if out is None:
+        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
+    qt, qh = _heads(Q, "Q", shape, dtype, dev)
+    ot, oh = _heads(out, "out", shape, dtype, dev)
+    if ws is None:
+        need = kv_attn_shared_workspace_size(total, batch, max_q, heads, kv, dim, n)
+        ws = _on(stream, lambda: workspace(need, pages.device))
+    code = load().qe_kv_attn_shared(
+        Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
+        _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
+        num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
+        _flat(lengths, "lengths", torch.int32, dev, batch), _flat(groups, "groups", torch.int32, dev, n + 1),
+        _flat(shared, "shared", torch.int32, dev), n, dim ** -0.5 if scale is None else scale, 1 if causal else 0,
+        _flat(slopes, "slopes", torch.float32, dev, heads), out.data_ptr(), ot, oh,
+        _flat(lse, "lse", torch.float32, dev, total * heads),
+        _flat(ws, "ws", torch.uint8, dev), ws.numel(), _raw_stream(dev, stream))
+    if code:
+        raise QEError(code, "qe_kv_attn_shared")
+    if check:
+        _finish(ws, check, "qe_kv_attn_shared", stream)
     return out
