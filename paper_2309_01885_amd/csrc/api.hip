@@ -453,7 +453,7 @@ qe_status qe_kv_append(const void* Q, const void* K, const void* V, int dtype, i
     if (misaligned(slots, 8) || misaligned(status, 4)) return QE_ERR_ARG;
     const int64_t strides[8] = {q_stride, q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride, o_stride, o_head_stride};
     const KvRotation r{positions, turn ? cos : nullptr, turn ? sin : nullptr, rows, rot / 2, interleaved != 0, false};
-    return launch_kv_append(Q, K, V, out, dtype, strides, tokens, heads, r, KvNorm{q_weight, k_weight, eps}, slots,
+    return launch_kv_append(Q, K, V, out, dtype, strides, tokens, heads, r, KvNorm{q_weight, k_weight, eps, 0., false}, slots,
                             kv_cache(pages, num_pages, page, kv_heads, dim), group, status, as_stream(stream));
 }
 

@@ -165,7 +165,8 @@ struct KvRotation {
 };
 struct KvNorm {
     const float *q, *k;            // weights; null: no norm
-    double eps;
+    double eps, inv_dim;
+    bool vec;                      // 16-byte loads of the weights
 };
 qe_status launch_kv_append(const void* Q, const void* K, const void* V, void* out, int dtype, const int64_t* strides, int64_t tokens,
                            int heads, const KvRotation& r, const KvNorm& n, const int64_t* slots, const KvCache& c, int group,

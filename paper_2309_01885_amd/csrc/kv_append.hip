@@ -20,6 +20,7 @@ struct KvAppend {
     int64_t tokens, kv_wgs;
     int heads;
     bool vec_q, vec_k, vec_v, vec_o;
+    bool narrow;                   // query rows are counted in 32 bits
     KvRotation r;
     KvNorm n;
     int* status;
@@ -37,39 +38,85 @@ __device__ inline int64_t position_of(const KvAppend& a, int64_t token)
     return p;
 }
 
-// A row's 8 channels from 8 o on, normed.  OP lanes a row.
-template <int OP> __device__ inline void norm8(float (&x)[8], const float* w, int o, int dim, double eps)
+// The sum over the OP lanes of a row, in all of them: inside 16 lanes by permutations that the vector units do themselves.
+template <int CTRL> __device__ inline double moved(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int OP> __device__ inline double row_sum(double x)
+{
+    x += moved<0xB1>(x);                                 // lanes 1 0 3 2 of four
+    x += moved<0x4E>(x);                                 // lanes 2 3 0 1 of four
+    x += moved<0x141>(x);                                // eight lanes, mirrored
+    if (OP >= 16) x += moved<0x140>(x);                  // sixteen lanes, mirrored
+    if (OP == 32) x += __shfl_xor(x, 16);
+    return x;
+}
+
+// 1 / sqrt(x) to a few units of fp64's last place: two steps of a third-order iteration on the hardware's estimate; 0, infinity
+// and NaN as the estimate has them.
+__device__ inline double root_inverse(double x)
+{
+    const double y0 = __builtin_amdgcn_rsq(x);
+    double y = y0;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const double e = __builtin_fma(-x * y, y, 1.);
+        y = __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y);
+    }
+    return y == y ? y : y0;
+}
+
+// A row's 8 channels, normed with their weights w.  OP lanes a row, zeros in those that have no channel.
+template <int OP> __device__ inline void norm8(float (&x)[8], const float (&w)[8], const KvNorm& n)
 {
 #pragma clang fp contract(off)
     double ss = 0.;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = __builtin_fma((double)x[e], (double)x[e], ss);
-#pragma unroll
-    for (int m = 1; m < OP; m *= 2) ss += __shfl_xor(ss, m);
-    const float r = (float)(1. / __builtin_sqrt(ss / (double)dim + eps));
-    if (8 * o >= dim) return;
-    float g[8];
-    kv_load8(w + 8 * o, false, g);
+    const float r = (float)root_inverse(row_sum<OP>(ss) * n.inv_dim + n.eps);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float y = x[e] * r;
-        x[e] = y * g[e];
+        x[e] = y * w[e];
     }
 }
 
-// The same, rotated.  at: the row's OP * 8 floats of LDS, used by its lanes alone.
-template <int OP> __device__ inline void rotate8(float (&x)[8], const KvRotation& r, int64_t pos, int o, float* at)
+// The cosines and sines of a row's 8 channels from 8 o on, where they lie aligned and beside each other (r.vec): with pairs of
+// halves those of channel e in c[e], the sine's sign that of its product; else those of pair e in c[e], e < 4.
+struct Turn { float c[8], s[8]; };
+__device__ inline void turn_of(Turn& t, const KvRotation& r, int64_t pos, int o)
+{
+    if (!r.vec || 8 * o >= 2 * r.half) return;
+    const int i = r.interleaved ? 4 * o : 8 * o < r.half ? 8 * o : 8 * o - r.half;
+    const float sign = !r.interleaved && 8 * o < r.half ? -1.f : 1.f;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        if (y == 1 && r.interleaved) break;
+        const f32x4 c = *reinterpret_cast<const f32x4*>(r.cos + pos * r.half + i + 4 * y);
+        const f32x4 s = *reinterpret_cast<const f32x4*>(r.sin + pos * r.half + i + 4 * y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            t.c[4 * y + e] = c[e];
+            t.s[4 * y + e] = sign * s[e];
+        }
+    }
+}
+
+// A row's 8 channels, rotated.  at: the row's OP * 8 floats of LDS, used by its lanes (of one wave) alone.
+template <int OP> __device__ inline void rotate8(float (&x)[8], const Turn& t, const KvRotation& r, int64_t pos, int o, float* at)
 {
 #pragma clang fp contract(off)
-    const float* cos = r.cos + pos * r.half;
-    const float* sin = r.sin + pos * r.half;
     if (r.interleaved) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int i = 4 * o + e;
             if (i >= r.half) continue;
-            const float c = cos[i], s = sin[i], a = x[2 * e], b = x[2 * e + 1];
-            const float ac = a * c, bs = b * s, bc = b * c, as = a * s;
+            const float c = r.vec ? t.c[e] : r.cos[pos * r.half + i], s = r.vec ? t.s[e] : r.sin[pos * r.half + i];
+            const float a = x[2 * e], b = x[2 * e + 1], ac = a * c, bs = b * s, bc = b * c, as = a * s;
             x[2 * e] = ac - bs;
             x[2 * e + 1] = bc + as;
         }
@@ -79,15 +126,27 @@ template <int OP> __device__ inline void rotate8(float (&x)[8], const KvRotation
 #pragma unroll
     for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4*>(at + 8 * o + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
     __builtin_amdgcn_wave_barrier();
+    if (r.vec) {
+        if (8 * o < 2 * r.half) {
+            const float* from = at + (8 * o < r.half ? 8 * o + r.half : 8 * o - r.half);
+            const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int d = 8 * o + e;
-        if (d >= 2 * r.half) continue;
-        const bool low = d < r.half;
-        const int i = low ? d : d - r.half;
-        const float c = cos[i], s = sin[i], other = at[low ? d + r.half : i];
-        const float own = x[e] * c, far = other * s;
-        x[e] = low ? own - far : own + far;
+            for (int e = 0; e < 8; ++e) {
+                const float own = x[e] * t.c[e], far = (e < 4 ? a[e] : b[e - 4]) * t.s[e];
+                x[e] = own + far;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int d = 8 * o + e;
+            if (d >= 2 * r.half) continue;
+            const bool low = d < r.half;
+            const int i = low ? d : d - r.half;
+            const float c = r.cos[pos * r.half + i], s = r.sin[pos * r.half + i], other = at[low ? d + r.half : i];
+            const float own = x[e] * c, far = other * s;
+            x[e] = low ? own - far : own + far;
+        }
     }
     __builtin_amdgcn_wave_barrier();
 }
@@ -103,7 +162,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* Q, const T* __r
     __shared__ __align__(16) float turn[TPP][OP * 8 + 4];
     const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int tid = threadIdx.x, o = tid % OP, row = tid / OP;
-    if (wg >= a.kv_wgs) {
+    const bool mine = 8 * o < c.dim, query = wg >= a.kv_wgs;
+    float w[8] = {};
+    if (const float* from = query ? a.n.q : a.n.k; from && mine) kv_load8(from + 8 * o, a.n.vec, w);
+    Turn t[P] = {};
+    if (query) {
         const int64_t rows = a.tokens * a.heads, r0 = (wg - a.kv_wgs) * kKvTok;
         float x[P][8];
         int64_t pos[P], token[P];
@@ -111,18 +174,22 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* Q, const T* __r
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int64_t at = r0 + p * TPP + row;
-            token[p] = at / a.heads;
+            token[p] = a.narrow ? (int64_t)((uint32_t)at / (uint32_t)a.heads) : at / a.heads;
             head[p] = (int)(at - token[p] * a.heads);
             pos[p] = at < rows ? position_of(a, token[p]) : -1;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[p][e] = 0.f;
-            if (8 * o < c.dim && pos[p] >= 0) kv_load8(Q + token[p] * a.qt + head[p] * a.qh + 8 * o, a.vec_q, x[p]);
+            if (mine && at < rows) kv_load8(Q + token[p] * a.qt + head[p] * a.qh + 8 * o, a.vec_q, x[p]);
+        }
+        if (a.r.cos) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) turn_of(t[p], a.r, max(pos[p], (int64_t)0), o);
         }
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            if (a.n.q) norm8<OP>(x[p], a.n.q, o, c.dim, a.n.eps);
-            if (a.r.cos) rotate8<OP>(x[p], a.r, max(pos[p], (int64_t)0), o, turn[row]);
-            if (8 * o < c.dim && pos[p] >= 0) kv_store8(out + token[p] * a.ot + head[p] * a.oh + 8 * o, a.vec_o, x[p]);
+            if (a.n.q) norm8<OP>(x[p], w, a.n);
+            if (a.r.cos) rotate8<OP>(x[p], t[p], a.r, max(pos[p], (int64_t)0), o, turn[row]);
+            if (mine && pos[p] >= 0) kv_store8(out + token[p] * a.ot + head[p] * a.oh + 8 * o, a.vec_o, x[p]);
         }
         return;
     }
@@ -131,28 +198,33 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* Q, const T* __r
     float k[P][8], v[P][8];
     int64_t slot[P], pos[P];
     // (a token without a position is not written: its slot is taken as none)
+    int64_t at_lane = 0;
     if (a.r.positions) {
-        const int64_t t = ch.t0 + (tid & 31);
-        if (position_of(a, t) < 0) ch.slot = -1;
+        at_lane = position_of(a, ch.t0 + (tid & 31));
+        if (at_lane < 0) ch.slot = -1;
         ch.whole = __all(ch.slot >= 0) && ch.whole;
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int t = p * TPP + row;
-        slot[p] = ch.slot_of(t);
-        pos[p] = a.r.positions && slot[p] >= 0 ? a.r.positions[ch.t0 + t] : 0;
+        const int i = p * TPP + row;
+        slot[p] = ch.slot_of(i);
+        pos[p] = max((int64_t)0, (int64_t)__shfl(at_lane, i));
 #pragma unroll
         for (int e = 0; e < 8; ++e) k[p][e] = v[p][e] = 0.f;
-        if (8 * o < c.dim && slot[p] >= 0) {
-            kv_load8(K + (ch.t0 + t) * a.kt + ch.head * a.kh + 8 * o, a.vec_k, k[p]);
-            kv_load8(V + (ch.t0 + t) * a.vt + ch.head * a.vh + 8 * o, a.vec_v, v[p]);
+        if (mine && slot[p] >= 0) {
+            kv_load8(K + (ch.t0 + i) * a.kt + ch.head * a.kh + 8 * o, a.vec_k, k[p]);
+            kv_load8(V + (ch.t0 + i) * a.vt + ch.head * a.vh + 8 * o, a.vec_v, v[p]);
         }
+    }
+    if (a.r.cos) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) turn_of(t[p], a.r, pos[p], o);
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int t = p * TPP + row;
-        if (a.n.k) norm8<OP>(k[p], a.n.k, o, c.dim, a.n.eps);
-        if (a.r.cos) rotate8<OP>(k[p], a.r, pos[p], o, turn[row]);
+        const int i = p * TPP + row;
+        if (a.n.k) norm8<OP>(k[p], w, a.n);
+        if (a.r.cos) rotate8<OP>(k[p], t[p], a.r, pos[p], o, turn[row]);
         uint32_t kw, vw;
         const uint32_t k8 = quantize8<LANES>(k[p], kw), v8 = quantize8<LANES>(v[p], vw);
         if (slot[p] < 0 || 8 * o >= DP) continue;
@@ -163,8 +235,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* Q, const T* __r
             reinterpret_cast<uint32_t*>(rec + R::kValWords)[o / LANES * kKvTok + at] = vw;
         }
         reinterpret_cast<uint32_t*>(rec + at * R::kKeyRow)[(o & 3) * R::NC + (o >> 2)] = k8;
-        tile[(2 * o) * kRowHalves + t] = (uint16_t)v8;
-        tile[(2 * o + 1) * kRowHalves + t] = (uint16_t)(v8 >> 16);
+        tile[(2 * o) * kRowHalves + i] = (uint16_t)v8;
+        tile[(2 * o + 1) * kRowHalves + i] = (uint16_t)(v8 >> 16);
     }
     __syncthreads();
     if (ch.whole) {
@@ -213,6 +285,10 @@ qe_status launch_kv_append(const void* Q, const void* K, const void* V, void* ou
     a.heads = heads;
     a.r = r;
     a.n = n;
+    a.n.inv_dim = 1. / c.dim;
+    a.n.vec = ((uintptr_t)n.q | (uintptr_t)n.k) % 16 == 0;
+    a.r.vec = ((uintptr_t)r.cos | (uintptr_t)r.sin) % 16 == 0 && r.half % (r.interleaved ? 4 : 8) == 0;
+    a.narrow = tokens * heads < (int64_t(1) << 31);
     a.status = status;
     if (dtype == QE_F32) return append_typed<float>(Q, K, V, out, a, slots, c, group, s);
     if (dtype == QE_F16) return append_typed<_Float16>(Q, K, V, out, a, slots, c, group, s);
