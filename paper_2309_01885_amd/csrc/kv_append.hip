@@ -5,10 +5,9 @@
 // of the sum shows after the rounding to fp32:
 //   r = fp32(1 / sqrt(sum x^2 / dim + eps)), y = fp32(fp32(x r) w),
 //   a' = fp32(fp32(a c) - fp32(b s)), b' = fp32(fp32(b c) + fp32(a s)).
-// A thread has 8 channels of a row, 8 to 32 lanes of a wave a row; a channel's partner in the rotation comes
-// through the row's own stretch of LDS, where any number of rotated channels is right.
-// The first workgroups take 32 tokens' keys and values of a head each, as the plain write does; the others 32 query
-// rows in the order of memory.
+// A channel's partner in the rotation comes through the row's own stretch of LDS, where any number of rotated channels is
+// right.  The first workgroups take 32 tokens' keys and values of a head each, as the plain write does (a thread
+// has 8 channels of a row), the others queries.
 #include "kv_codes.h"
 
 namespace qe {
@@ -20,7 +19,7 @@ struct KvAppend {
     int64_t tokens, kv_wgs;
     int heads;
     bool vec_q, vec_k, vec_v, vec_o;
-    bool narrow;                   // query rows are counted in 32 bits
+    int head_run, head_groups;     // heads that a workgroup goes through
     KvRotation r;
     KvNorm n;
     int* status;
@@ -50,7 +49,7 @@ template <int OP> __device__ inline double row_sum(double x)
 {
     x += moved<0xB1>(x);                                 // lanes 1 0 3 2 of four
     x += moved<0x4E>(x);                                 // lanes 2 3 0 1 of four
-    x += moved<0x141>(x);                                // eight lanes, mirrored
+    if (OP >= 8) x += moved<0x141>(x);                   // eight lanes, mirrored
     if (OP >= 16) x += moved<0x140>(x);                  // sixteen lanes, mirrored
     if (OP == 32) x += __shfl_xor(x, 16);
     return x;
@@ -70,16 +69,16 @@ __device__ inline double root_inverse(double x)
     return y == y ? y : y0;
 }
 
-// A row's 8 channels, normed with their weights w.  OP lanes a row, zeros in those that have no channel.
-template <int OP> __device__ inline void norm8(float (&x)[8], const float (&w)[8], const KvNorm& n)
+// N channels of a row, normed with their weights w.  OP lanes a row, zeros in those that have no channel.
+template <int OP, int N> __device__ inline void norm(float (&x)[N], const float (&w)[N], const KvNorm& n)
 {
 #pragma clang fp contract(off)
     double ss = 0.;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss = __builtin_fma((double)x[e], (double)x[e], ss);
+    for (int e = 0; e < N; ++e) ss = __builtin_fma((double)x[e], (double)x[e], ss);
     const float r = (float)root_inverse(row_sum<OP>(ss) * n.inv_dim + n.eps);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < N; ++e) {
         const float y = x[e] * r;
         x[e] = y * w[e];
     }
@@ -90,7 +89,7 @@ template <int OP> __device__ inline void norm8(float (&x)[8], const float (&w)[8
 struct Turn { float c[8], s[8]; };
 __device__ inline void turn_of(Turn& t, const KvRotation& r, int64_t pos, int o)
 {
-    if (!r.vec || 8 * o >= 2 * r.half) return;
+    if (8 * o >= 2 * r.half) return;
     const int i = r.interleaved ? 4 * o : 8 * o < r.half ? 8 * o : 8 * o - r.half;
     const float sign = !r.interleaved && 8 * o < r.half ? -1.f : 1.f;
 #pragma unroll
@@ -106,96 +105,174 @@ __device__ inline void turn_of(Turn& t, const KvRotation& r, int64_t pos, int o)
     }
 }
 
-// A row's 8 channels, rotated.  at: the row's OP * 8 floats of LDS, used by its lanes (of one wave) alone.
-template <int OP> __device__ inline void rotate8(float (&x)[8], const Turn& t, const KvRotation& r, int64_t pos, int o, float* at)
+// N octets of a row, o + n step, rotated.  at: the row's floats of LDS, used by its lanes (of one wave) alone.  here: the
+// lane has channels.
+template <int N, bool VEC> __device__ inline void rotate(float (&x)[8 * N], const Turn (&t)[N], const KvRotation& r, int64_t pos, int o, int step, bool here, float* at)
 {
 #pragma clang fp contract(off)
     if (r.interleaved) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = 4 * o + e;
-            if (i >= r.half) continue;
-            const float c = r.vec ? t.c[e] : r.cos[pos * r.half + i], s = r.vec ? t.s[e] : r.sin[pos * r.half + i];
-            const float a = x[2 * e], b = x[2 * e + 1], ac = a * c, bs = b * s, bc = b * c, as = a * s;
-            x[2 * e] = ac - bs;
-            x[2 * e + 1] = bc + as;
-        }
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 4 * (o + n * step) + e;
+                if (i >= r.half || !here) continue;
+                const float c = VEC ? t[n].c[e] : r.cos[pos * r.half + i], s = VEC ? t[n].s[e] : r.sin[pos * r.half + i];
+                const float a = x[8 * n + 2 * e], b = x[8 * n + 2 * e + 1], ac = a * c, bs = b * s, bc = b * c, as = a * s;
+                x[8 * n + 2 * e] = ac - bs;
+                x[8 * n + 2 * e + 1] = bc + as;
+            }
         return;
     }
     // (LDS serves a wave in order)
+    if (here) {
 #pragma unroll
-    for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4*>(at + 8 * o + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) *reinterpret_cast<f32x4*>(at + 8 * (o + n * step) + e) = f32x4{x[8 * n + e], x[8 * n + e + 1], x[8 * n + e + 2], x[8 * n + e + 3]};
+    }
     __builtin_amdgcn_wave_barrier();
-    if (r.vec) {
-        if (8 * o < 2 * r.half) {
-            const float* from = at + (8 * o < r.half ? 8 * o + r.half : 8 * o - r.half);
-            const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 4);
+    if (here) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float own = x[e] * t.c[e], far = (e < 4 ? a[e] : b[e - 4]) * t.s[e];
-                x[e] = own + far;
+        for (int n = 0; n < N; ++n) {
+            const int d0 = 8 * (o + n * step);
+            if (d0 >= 2 * r.half) continue;
+            if constexpr (VEC) {
+                const float* from = at + (d0 < r.half ? d0 + r.half : d0 - r.half);
+                const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float own = x[8 * n + e] * t[n].c[e], far = (e < 4 ? a[e] : b[e - 4]) * t[n].s[e];
+                    x[8 * n + e] = own + far;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int d = d0 + e;
+                    if (d >= 2 * r.half) continue;
+                    const bool low = d < r.half;
+                    const int i = low ? d : d - r.half;
+                    const float c = r.cos[pos * r.half + i], s = r.sin[pos * r.half + i], other = at[low ? d + r.half : i];
+                    const float own = x[8 * n + e] * c, far = other * s;
+                    x[8 * n + e] = low ? own - far : own + far;
+                }
             }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int d = 8 * o + e;
-            if (d >= 2 * r.half) continue;
-            const bool low = d < r.half;
-            const int i = low ? d : d - r.half;
-            const float c = r.cos[pos * r.half + i], s = r.sin[pos * r.half + i], other = at[low ? d + r.half : i];
-            const float own = x[e] * c, far = other * s;
-            x[e] = low ? own - far : own + far;
         }
     }
     __builtin_amdgcn_wave_barrier();
 }
 
-template <class T, int DP, int GROUP>
-__global__ __launch_bounds__(256) void kv_append_kernel(const T* Q, const T* __restrict__ K, const T* __restrict__ V, T* out,
+// Eight channels as they lie in memory.
+template <class T> struct Raw8 {
+    u32x4 at[sizeof(T) / 2];
+    __device__ void load(const T* p, bool vec)
+    {
+        if (vec) {
+#pragma unroll
+            for (int u = 0; u < (int)sizeof(T) / 2; ++u) at[u] = reinterpret_cast<const u32x4*>(p)[u];
+        } else {
+            T v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = p[e];
+            __builtin_memcpy(at, v, sizeof(v));
+        }
+    }
+    __device__ void get(float* x) const
+    {
+        T v[8];
+        __builtin_memcpy(v, at, sizeof(v));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+    }
+};
+
+// The queries of some tokens and heads.  A lane has two octets of a token's channels, o and o + step, half as many lanes a row
+// as for the keys: the norm's sum and root, which every lane of a row forms, are shared by twice the channels, and where all
+// channels are rotated by halves the partners lie in one lane.  It goes through its heads with one set of
+// cosines and sines, the next head's loads on the way.
+template <class T, int DP, bool VEC>
+__device__ inline void kv_queries(const T* Q, T* out, int dim, const KvAppend& a, int64_t wg, float* turn)
+{
+#pragma clang fp contract(off)
+    constexpr int OQ = kOctets<DP> / 2, ROWS = 256 / OQ;
+    const int64_t chunk = wg / a.head_groups;
+    const int h0 = (int)(wg - chunk * a.head_groups) * a.head_run, h1 = min(h0 + a.head_run, a.heads);
+    const int tid = threadIdx.x, o = tid % OQ, row = tid / OQ;
+    const int step = (dim / 8 + 1) / 2;
+    const int64_t token = chunk * ROWS + row;
+    const int64_t pos = token < a.tokens ? position_of(a, token) : -1;
+    const bool here[2] = {pos >= 0 && o < step, pos >= 0 && 8 * (o + step) < dim && o < step};
+    const int at[2] = {8 * o, 8 * (o + step)};
+    const T* from = Q + token * a.qt + h0 * a.qh;
+    T* to = out + token * a.ot + h0 * a.oh;
+    Raw8<T> next[2] = {};
+    float w[16] = {};
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+        if (here[y] && h0 < h1) next[y].load(from + at[y], a.vec_q);
+    if (a.n.q) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            if (here[y]) kv_load8(a.n.q + at[y], a.n.vec, w + 8 * y);
+    }
+    // by halves, all of an even number of octets: channel e of the one octet and of the other are a pair
+    const bool paired = VEC && !a.r.interleaved && 2 * a.r.half == dim;
+    Turn t[2] = {};
+    if (VEC && a.r.cos && pos >= 0 && o < step) {
+        turn_of(t[0], a.r, pos, o);
+        if (!paired) turn_of(t[1], a.r, pos, o + step);
+    }
+    float* const mine = turn + row * (kOctets<DP> * 8 + 8);
+    for (int h = h0; h < h1; ++h) {
+        float x[16];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) next[y].get(x + 8 * y);
+        from += a.qh;
+        if (h + 1 < h1) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                if (here[y]) next[y].load(from + at[y], a.vec_q);
+        }
+        if (a.n.q) norm<OQ>(x, w, a.n);
+        if (paired) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // (t[0].s is the sine with the sign of the first of a pair)
+                const float ac = x[e] * t[0].c[e], bs = x[8 + e] * t[0].s[e], bc = x[8 + e] * t[0].c[e], as = x[e] * t[0].s[e];
+                x[e] = ac + bs;
+                x[8 + e] = bc - as;
+            }
+        } else if (a.r.cos) {
+            rotate<2, VEC>(x, t, a.r, max(pos, (int64_t)0), o, step, o < step, mine);
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            if (here[y]) kv_store8(to + at[y], a.vec_o, x + 8 * y);
+        to += a.oh;
+    }
+}
+
+template <class T, int DP, int GROUP, bool VEC>
+__global__ __launch_bounds__(256, !VEC ? 2 : sizeof(T) == 4 && DP > 128 ? 3 : 4) void kv_append_kernel(const T* Q, const T* __restrict__ K, const T* __restrict__ V, T* out,
                                                         const int64_t* __restrict__ slots, KvCache c, KvAppend a)
 {
     using R = KvRec<DP, GROUP>;
     constexpr int OP = kOctets<DP>, TPP = 256 / OP, P = OP / 8;      // rows of a pass, passes
     constexpr int LANES = GROUP / 8 < OP ? GROUP / 8 : OP;
     __shared__ __align__(16) uint16_t tile[(DP / 4) * kRowHalves];
-    __shared__ __align__(16) float turn[TPP][OP * 8 + 4];
+    __shared__ __align__(16) float turn[TPP][2 * (OP * 8 + 8)];      // (the queries have twice the rows)
     const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int tid = threadIdx.x, o = tid % OP, row = tid / OP;
-    const bool mine = 8 * o < c.dim, query = wg >= a.kv_wgs;
-    float w[8] = {};
-    if (const float* from = query ? a.n.q : a.n.k; from && mine) kv_load8(from + 8 * o, a.n.vec, w);
-    Turn t[P] = {};
-    if (query) {
-        const int64_t rows = a.tokens * a.heads, r0 = (wg - a.kv_wgs) * kKvTok;
-        float x[P][8];
-        int64_t pos[P], token[P];
-        int head[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int64_t at = r0 + p * TPP + row;
-            token[p] = a.narrow ? (int64_t)((uint32_t)at / (uint32_t)a.heads) : at / a.heads;
-            head[p] = (int)(at - token[p] * a.heads);
-            pos[p] = at < rows ? position_of(a, token[p]) : -1;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[p][e] = 0.f;
-            if (mine && at < rows) kv_load8(Q + token[p] * a.qt + head[p] * a.qh + 8 * o, a.vec_q, x[p]);
-        }
-        if (a.r.cos) {
-#pragma unroll
-            for (int p = 0; p < P; ++p) turn_of(t[p], a.r, max(pos[p], (int64_t)0), o);
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (a.n.q) norm8<OP>(x[p], w, a.n);
-            if (a.r.cos) rotate8<OP>(x[p], t[p], a.r, max(pos[p], (int64_t)0), o, turn[row]);
-            if (mine && pos[p] >= 0) kv_store8(out + token[p] * a.ot + head[p] * a.oh + 8 * o, a.vec_o, x[p]);
-        }
+    const bool mine = 8 * o < c.dim;
+    if (wg >= a.kv_wgs) {
+        kv_queries<T, DP, VEC>(Q, out, c.dim, a, wg - a.kv_wgs, &turn[0][0]);
         return;
     }
+    float w[8] = {};
+    if (a.n.k && mine) kv_load8(a.n.k + 8 * o, a.n.vec, w);
     Chunk ch;
     if (!ch.open(wg, c, slots, a.tokens, a.status)) return;
-    float k[P][8], v[P][8];
+    Raw8<T> k[P] = {}, v[P] = {};
     int64_t slot[P], pos[P];
     // (a token without a position is not written: its slot is taken as none)
     int64_t at_lane = 0;
@@ -209,24 +286,23 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* Q, const T* __r
         const int i = p * TPP + row;
         slot[p] = ch.slot_of(i);
         pos[p] = max((int64_t)0, (int64_t)__shfl(at_lane, i));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) k[p][e] = v[p][e] = 0.f;
         if (mine && slot[p] >= 0) {
-            kv_load8(K + (ch.t0 + i) * a.kt + ch.head * a.kh + 8 * o, a.vec_k, k[p]);
-            kv_load8(V + (ch.t0 + i) * a.vt + ch.head * a.vh + 8 * o, a.vec_v, v[p]);
+            k[p].load(K + (ch.t0 + i) * a.kt + ch.head * a.kh + 8 * o, a.vec_k);
+            v[p].load(V + (ch.t0 + i) * a.vt + ch.head * a.vh + 8 * o, a.vec_v);
         }
-    }
-    if (a.r.cos) {
-#pragma unroll
-        for (int p = 0; p < P; ++p) turn_of(t[p], a.r, pos[p], o);
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         const int i = p * TPP + row;
-        if (a.n.k) norm8<OP>(k[p], w, a.n);
-        if (a.r.cos) rotate8<OP>(k[p], t[p], a.r, pos[p], o, turn[row]);
+        Turn t[1] = {};
+        if (VEC && a.r.cos) turn_of(t[0], a.r, pos[p], o);
+        float x[8], y[8];
+        k[p].get(x);
+        v[p].get(y);
+        if (a.n.k) norm<OP>(x, w, a.n);
+        if (a.r.cos) rotate<1, VEC>(x, t, a.r, pos[p], o, 0, true, turn[row]);
         uint32_t kw, vw;
-        const uint32_t k8 = quantize8<LANES>(k[p], kw), v8 = quantize8<LANES>(v[p], vw);
+        const uint32_t k8 = quantize8<LANES>(x, kw), v8 = quantize8<LANES>(y, vw);
         if (slot[p] < 0 || 8 * o >= DP) continue;
         uint8_t* rec = kv_record<R::kBytes>(c, slot[p], ch.head);
         const int at = (int)(slot[p] & 31);
@@ -258,10 +334,18 @@ qe_status append_typed(const void* Q, const void* K, const void* V, void* out, K
     a.vec_v = vec_ok(V, a.vt, a.vh, sizeof(T));
     a.vec_o = vec_ok(out, a.ot, a.oh, sizeof(T));
     a.kv_wgs = cdiv(a.tokens, kKvTok) * c.heads;
-    const dim3 grid = grid_xy(a.kv_wgs + cdiv(a.tokens * a.heads, kKvTok), 256);
     kv_dispatch(c.dim, group, [&](auto shape) {
-        hipLaunchKernelGGL((kv_append_kernel<T, shape.DP, shape.GROUP>), grid, dim3(256), 0, s, (const T*)Q, (const T*)K, (const T*)V,
-                           (T*)out, slots, c, a);
+        // (as many heads a workgroup as leave four of them for a compute unit)
+        const int64_t chunks = cdiv(a.tokens, 512 / kOctets<shape.DP>);
+        a.head_run = (int)std::max<int64_t>(1, std::min<int64_t>(8, chunks * a.heads / 1024));
+        a.head_groups = (int)cdiv(a.heads, a.head_run);
+        const dim3 grid = grid_xy(a.kv_wgs + chunks * a.head_groups, 256);
+        if (a.r.vec)
+            hipLaunchKernelGGL((kv_append_kernel<T, shape.DP, shape.GROUP, true>), grid, dim3(256), 0, s, (const T*)Q, (const T*)K,
+                               (const T*)V, (T*)out, slots, c, a);
+        else
+            hipLaunchKernelGGL((kv_append_kernel<T, shape.DP, shape.GROUP, false>), grid, dim3(256), 0, s, (const T*)Q, (const T*)K,
+                               (const T*)V, (T*)out, slots, c, a);
     });
     return hipGetLastError() == hipSuccess ? QE_OK : QE_ERR_HIP;
 }
@@ -288,7 +372,6 @@ qe_status launch_kv_append(const void* Q, const void* K, const void* V, void* ou
     a.n.inv_dim = 1. / c.dim;
     a.n.vec = ((uintptr_t)n.q | (uintptr_t)n.k) % 16 == 0;
     a.r.vec = ((uintptr_t)r.cos | (uintptr_t)r.sin) % 16 == 0 && r.half % (r.interleaved ? 4 : 8) == 0;
-    a.narrow = tokens * heads < (int64_t(1) << 31);
     a.status = status;
     if (dtype == QE_F32) return append_typed<float>(Q, K, V, out, a, slots, c, group, s);
     if (dtype == QE_F16) return append_typed<_Float16>(Q, K, V, out, a, slots, c, group, s);
