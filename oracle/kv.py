@@ -156,9 +156,7 @@ def extend(counts, table, lengths, free, free_count, page, total, keep=None):
                 table[b, held + j] = free[at] if at < num else -1
             taken = max(taken, needed if need else 0)
             lengths[b] = new
-        for i in range(n):
-            if row + i >= total or wrong:
-                continue
+        for i in range(0 if wrong else max(0, min(n, total - row))):
             positions[row + i] = old + i
             if got:
                 p = int(table[b, (old + i) // page])

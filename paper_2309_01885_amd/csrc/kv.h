@@ -123,8 +123,12 @@ struct KvSequence {
 struct KvShared {
     const int32_t *groups, *shared;        // groups[g] .. groups[g + 1] - 1 share shared[g] pages; checked on the device
     int32_t ngroups;
-    int32_t rows[2], fill[2], least[2];    // of the two lists: rows of a tile, entries that fill the chip, records of an entry
+    int32_t rows[2], rows_log2[2];         // of the two lists: rows of a tile,
+    int32_t fill[2], least[2];             // entries that fill the chip, records of an entry at least
+    int32_t weight[2];                     // joint: what a record of a tile costs, relative to each other
+    double part_of_fill[2];                // 1 / (fill weight)
     int32_t room[2];                       // entries that a list holds
+    bool joint;                            // both lists in one launch (equal fill)
     KvGroup* group;
     KvSequence* seq;
     KvItem* items[2];
@@ -161,7 +165,7 @@ struct KvRotation {
     const float *cos, *sin;        // rows x half; null: no rotation
     int64_t rows;
     int half;                      // pairs of channels
-    bool interleaved, vec;         // vec: eight channels' cosines lie aligned and beside each other
+    bool interleaved, vec;         // vec: pairs of halves, whole octets in each half
 };
 struct KvNorm {
     const float *q, *k;            // weights; null: no norm
@@ -181,6 +185,7 @@ inline void kv_attn_vec(KvAttn& a)
 
 size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, int dim);
 qe_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t s);
+bool kv_attn_many(const KvAttn& a);               // whether the call takes the many-row form
 size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups);
 qe_status launch_kv_attn_shared(const KvAttn& a, const int32_t* groups, const int32_t* shared, int64_t ngroups, void* ws, bool always,
                                 hipStream_t s);   // always: also where kv_attn is faster

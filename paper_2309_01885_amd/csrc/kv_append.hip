@@ -84,30 +84,52 @@ template <int OP, int N> __device__ inline void norm(float (&x)[N], const float 
     }
 }
 
-// The cosines and sines of a row's 8 channels from 8 o on, where they lie aligned and beside each other (r.vec): with pairs of
-// halves those of channel e in c[e], the sine's sign that of its product; else those of pair e in c[e], e < 4.
+// The cosines and sines of a row's 8 channels from 8 o on: with pairs of halves those of channel e in c[e], the sine with the
+// sign of its product; else those of pair e in c[e], e < 4.  (Read once for all heads of a token; from rows that are
+// aligned to 4 bytes alone, 16 at a time where they are pairs of an octet.)
 struct Turn { float c[8], s[8]; };
+typedef float f32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
 __device__ inline void turn_of(Turn& t, const KvRotation& r, int64_t pos, int o)
 {
+    const float *cos = r.cos + pos * r.half, *sin = r.sin + pos * r.half;
     if (8 * o >= 2 * r.half) return;
-    const int i = r.interleaved ? 4 * o : 8 * o < r.half ? 8 * o : 8 * o - r.half;
-    const float sign = !r.interleaved && 8 * o < r.half ? -1.f : 1.f;
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        if (y == 1 && r.interleaved) break;
-        const f32x4 c = *reinterpret_cast<const f32x4*>(r.cos + pos * r.half + i + 4 * y);
-        const f32x4 s = *reinterpret_cast<const f32x4*>(r.sin + pos * r.half + i + 4 * y);
+    auto four = [&](int y, int i, float sign) {
+        const f32x4 c = *reinterpret_cast<const f32x4a4*>(cos + i), s = *reinterpret_cast<const f32x4a4*>(sin + i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             t.c[4 * y + e] = c[e];
             t.s[4 * y + e] = sign * s[e];
+        }
+    };
+    if (r.interleaved) {
+        if (4 * o + 4 <= r.half) {
+            four(0, 4 * o, 1.f);
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (4 * o + e < r.half) {
+                t.c[e] = cos[4 * o + e];
+                t.s[e] = sin[4 * o + e];
+            }
+    } else if (r.vec) {
+        const int i = 8 * o < r.half ? 8 * o : 8 * o - r.half;
+        four(0, i, 8 * o < r.half ? -1.f : 1.f);
+        four(1, i + 4, 8 * o < r.half ? -1.f : 1.f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int d = 8 * o + e, i = d < r.half ? d : d - r.half;
+            if (d >= 2 * r.half) continue;
+            t.c[e] = cos[i];
+            t.s[e] = d < r.half ? -sin[i] : sin[i];
         }
     }
 }
 
 // N octets of a row, o + n step, rotated.  at: the row's floats of LDS, used by its lanes (of one wave) alone.  here: the
 // lane has channels.
-template <int N, bool VEC> __device__ inline void rotate(float (&x)[8 * N], const Turn (&t)[N], const KvRotation& r, int64_t pos, int o, int step, bool here, float* at)
+template <int N> __device__ inline void rotate(float (&x)[8 * N], const Turn (&t)[N], const KvRotation& r, int o, int step, bool here, float* at)
 {
 #pragma clang fp contract(off)
     if (r.interleaved) {
@@ -115,12 +137,11 @@ template <int N, bool VEC> __device__ inline void rotate(float (&x)[8 * N], cons
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int i = 4 * (o + n * step) + e;
-                if (i >= r.half || !here) continue;
-                const float c = VEC ? t[n].c[e] : r.cos[pos * r.half + i], s = VEC ? t[n].s[e] : r.sin[pos * r.half + i];
-                const float a = x[8 * n + 2 * e], b = x[8 * n + 2 * e + 1], ac = a * c, bs = b * s, bc = b * c, as = a * s;
-                x[8 * n + 2 * e] = ac - bs;
-                x[8 * n + 2 * e + 1] = bc + as;
+                const float a = x[8 * n + 2 * e], b = x[8 * n + 2 * e + 1], c = t[n].c[e], s = t[n].s[e];
+                const float ac = a * c, bs = b * s, bc = b * c, as = a * s;
+                const bool turned = 4 * (o + n * step) + e < r.half;
+                x[8 * n + 2 * e] = turned ? ac - bs : a;
+                x[8 * n + 2 * e + 1] = turned ? bc + as : b;
             }
         return;
     }
@@ -137,25 +158,21 @@ template <int N, bool VEC> __device__ inline void rotate(float (&x)[8 * N], cons
         for (int n = 0; n < N; ++n) {
             const int d0 = 8 * (o + n * step);
             if (d0 >= 2 * r.half) continue;
-            if constexpr (VEC) {
+            float other[8];
+            if (r.vec) {
                 const float* from = at + (d0 < r.half ? d0 + r.half : d0 - r.half);
                 const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 4);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float own = x[8 * n + e] * t[n].c[e], far = (e < 4 ? a[e] : b[e - 4]) * t[n].s[e];
-                    x[8 * n + e] = own + far;
-                }
+                for (int e = 0; e < 8; ++e) other[e] = e < 4 ? a[e] : b[e - 4];
             } else {
+                // (past the rotated channels: any of the row's)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int d = d0 + e;
-                    if (d >= 2 * r.half) continue;
-                    const bool low = d < r.half;
-                    const int i = low ? d : d - r.half;
-                    const float c = r.cos[pos * r.half + i], s = r.sin[pos * r.half + i], other = at[low ? d + r.half : i];
-                    const float own = x[8 * n + e] * c, far = other * s;
-                    x[8 * n + e] = low ? own - far : own + far;
-                }
+                for (int e = 0; e < 8; ++e) other[e] = at[d0 + e < r.half ? d0 + e + r.half : d0 + e - r.half];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float own = x[8 * n + e] * t[n].c[e], far = other[e] * t[n].s[e];
+                x[8 * n + e] = d0 + e < 2 * r.half ? own + far : x[8 * n + e];
             }
         }
     }
@@ -190,7 +207,7 @@ template <class T> struct Raw8 {
 // as for the keys: the norm's sum and root, which every lane of a row forms, are shared by twice the channels, and where all
 // channels are rotated by halves the partners lie in one lane.  It goes through its heads with one set of
 // cosines and sines, the next head's loads on the way.
-template <class T, int DP, bool VEC>
+template <class T, int DP>
 __device__ inline void kv_queries(const T* Q, T* out, int dim, const KvAppend& a, int64_t wg, float* turn)
 {
 #pragma clang fp contract(off)
@@ -216,9 +233,9 @@ __device__ inline void kv_queries(const T* Q, T* out, int dim, const KvAppend& a
             if (here[y]) kv_load8(a.n.q + at[y], a.n.vec, w + 8 * y);
     }
     // by halves, all of an even number of octets: channel e of the one octet and of the other are a pair
-    const bool paired = VEC && !a.r.interleaved && 2 * a.r.half == dim;
+    const bool paired = a.r.vec && !a.r.interleaved && 2 * a.r.half == dim;
     Turn t[2] = {};
-    if (VEC && a.r.cos && pos >= 0 && o < step) {
+    if (a.r.cos && pos >= 0 && o < step) {
         turn_of(t[0], a.r, pos, o);
         if (!paired) turn_of(t[1], a.r, pos, o + step);
     }
@@ -243,7 +260,7 @@ __device__ inline void kv_queries(const T* Q, T* out, int dim, const KvAppend& a
                 x[8 + e] = bc - as;
             }
         } else if (a.r.cos) {
-            rotate<2, VEC>(x, t, a.r, max(pos, (int64_t)0), o, step, o < step, mine);
+            rotate<2>(x, t, a.r, o, step, o < step, mine);
         }
 #pragma unroll
         for (int y = 0; y < 2; ++y)
@@ -252,8 +269,8 @@ __device__ inline void kv_queries(const T* Q, T* out, int dim, const KvAppend& a
     }
 }
 
-template <class T, int DP, int GROUP, bool VEC>
-__global__ __launch_bounds__(256, !VEC ? 2 : sizeof(T) == 4 && DP > 128 ? 3 : 4) void kv_append_kernel(const T* Q, const T* __restrict__ K, const T* __restrict__ V, T* out,
+template <class T, int DP, int GROUP>
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void kv_append_kernel(const T* Q, const T* __restrict__ K, const T* __restrict__ V, T* out,
                                                         const int64_t* __restrict__ slots, KvCache c, KvAppend a)
 {
     using R = KvRec<DP, GROUP>;
@@ -265,7 +282,7 @@ __global__ __launch_bounds__(256, !VEC ? 2 : sizeof(T) == 4 && DP > 128 ? 3 : 4)
     const int tid = threadIdx.x, o = tid % OP, row = tid / OP;
     const bool mine = 8 * o < c.dim;
     if (wg >= a.kv_wgs) {
-        kv_queries<T, DP, VEC>(Q, out, c.dim, a, wg - a.kv_wgs, &turn[0][0]);
+        kv_queries<T, DP>(Q, out, c.dim, a, wg - a.kv_wgs, &turn[0][0]);
         return;
     }
     float w[8] = {};
@@ -295,12 +312,12 @@ __global__ __launch_bounds__(256, !VEC ? 2 : sizeof(T) == 4 && DP > 128 ? 3 : 4)
     for (int p = 0; p < P; ++p) {
         const int i = p * TPP + row;
         Turn t[1] = {};
-        if (VEC && a.r.cos) turn_of(t[0], a.r, pos[p], o);
+        if (a.r.cos) turn_of(t[0], a.r, pos[p], o);
         float x[8], y[8];
         k[p].get(x);
         v[p].get(y);
         if (a.n.k) norm<OP>(x, w, a.n);
-        if (a.r.cos) rotate<1, VEC>(x, t, a.r, pos[p], o, 0, true, turn[row]);
+        if (a.r.cos) rotate<1>(x, t, a.r, o, 0, true, turn[row]);
         uint32_t kw, vw;
         const uint32_t k8 = quantize8<LANES>(x, kw), v8 = quantize8<LANES>(y, vw);
         if (slot[p] < 0 || 8 * o >= DP) continue;
@@ -340,12 +357,8 @@ qe_status append_typed(const void* Q, const void* K, const void* V, void* out, K
         a.head_run = (int)std::max<int64_t>(1, std::min<int64_t>(8, chunks * a.heads / 1024));
         a.head_groups = (int)cdiv(a.heads, a.head_run);
         const dim3 grid = grid_xy(a.kv_wgs + chunks * a.head_groups, 256);
-        if (a.r.vec)
-            hipLaunchKernelGGL((kv_append_kernel<T, shape.DP, shape.GROUP, true>), grid, dim3(256), 0, s, (const T*)Q, (const T*)K,
-                               (const T*)V, (T*)out, slots, c, a);
-        else
-            hipLaunchKernelGGL((kv_append_kernel<T, shape.DP, shape.GROUP, false>), grid, dim3(256), 0, s, (const T*)Q, (const T*)K,
-                               (const T*)V, (T*)out, slots, c, a);
+        hipLaunchKernelGGL((kv_append_kernel<T, shape.DP, shape.GROUP>), grid, dim3(256), 0, s, (const T*)Q, (const T*)K, (const T*)V,
+                           (T*)out, slots, c, a);
     });
     return hipGetLastError() == hipSuccess ? QE_OK : QE_ERR_HIP;
 }
@@ -371,7 +384,7 @@ qe_status launch_kv_append(const void* Q, const void* K, const void* V, void* ou
     a.n = n;
     a.n.inv_dim = 1. / c.dim;
     a.n.vec = ((uintptr_t)n.q | (uintptr_t)n.k) % 16 == 0;
-    a.r.vec = ((uintptr_t)r.cos | (uintptr_t)r.sin) % 16 == 0 && r.half % (r.interleaved ? 4 : 8) == 0;
+    a.r.vec = !r.interleaved && r.half % 8 == 0;
     a.status = status;
     if (dtype == QE_F32) return append_typed<float>(Q, K, V, out, a, slots, c, group, s);
     if (dtype == QE_F16) return append_typed<_Float16>(Q, K, V, out, a, slots, c, group, s);

@@ -756,10 +756,25 @@ constexpr int kv_few_occupancy(int dp, int group, int nt, int parts)
 }
 
 
+template <int DP, int GROUP, int NT> struct KvFewLds {
+    static constexpr int NG = KvTiles<DP, GROUP>::NG;
+    struct Words {
+        float s[NG][64];                                         // scales
+        uint16_t lo[NG][64], hi[NG][64];                         // -(1024 + z), -(1024 + 16 z) in fp16
+    };
+    static constexpr int kRow = DP + 4;                          // floats of a row (16-byte aligned, spread over the banks)
+    __align__(16) union {
+        Words words[kKvWaves];
+        float acc[kKvWaves][16 * NT][kRow];
+    };
+    float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT], rtop[16 * NT], rmass[16 * NT];
+};
+
 template <int DP, int GROUP, int NT, int PARTS>
 __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void kv_few_kernel(KvAttn a, KvPlan plan)
 {
     constexpr KvMode MODE = kKvPlain;
+    __shared__ KvFewLds<DP, GROUP, NT> lds;
 #include "kv_attn_few.h"
 }
 // (The bodies are included: as inlined functions of the kernels' arguments they took other registers, and one instance in
@@ -767,6 +782,7 @@ __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void k
 template <int DP, int GROUP, int NT, int PARTS, KvMode MODE>
 __global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, NT, PARTS)) void kv_few_mode_kernel(KvAttn a, KvPlan plan)
 {
+    __shared__ KvFewLds<DP, GROUP, NT> lds;
 #include "kv_attn_few.h"
 }
 

@@ -93,6 +93,11 @@ size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, i
     return kStatusBytes + need;
 }
 
+bool kv_attn_many(const KvAttn& a)
+{
+    return sizes_of(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, a.width * a.c.per, a.dtype == QE_F32).form.many;
+}
+
 qe_status launch_kv_attn(const KvAttn& call, void* ws, hipStream_t s)
 {
     KvAttn a = call;

@@ -21,16 +21,7 @@
     // the weighted sum.  The words' scales and zero points reach the lanes that need them through the
     // wave's part of LDS.  (Read from memory by each of those lanes they took 18 registers a group and
     // 32 more instructions.)
-    struct Words {
-        float s[NG][64];                                         // scales
-        uint16_t lo[NG][64], hi[NG][64];                         // -(1024 + z), -(1024 + 16 z) in fp16
-    };
-    constexpr int kRow = DP + 4;                                 // floats of a row (16-byte aligned, spread over the banks)
-    __shared__ __align__(16) union {
-        Words words[kKvWaves];
-        float acc[kKvWaves][16 * NT][kRow];
-    } shared;
-    Words& held = shared.words[wave];
+    typename KvFewLds<DP, GROUP, NT>::Words& held = lds.words[wave];
     const int lane = tid & 63;
     const KvBits bits;
     uint32_t k[2][NC], v[UT][4], word[NG];
@@ -177,8 +168,9 @@
 
     // every wave to the common maximum, divided by the common mass (sums of large values would pass the
     // largest number before it), then sums over the waves
-    __shared__ float wtop[kKvWaves][16 * NT], wmass[kKvWaves][16 * NT], rtop[16 * NT], rmass[16 * NT];
-    auto& acc = shared.acc;                                      // (written after a barrier that ends the use of the words)
+    auto &wtop = lds.wtop, &wmass = lds.wmass;
+    auto &rtop = lds.rtop, &rmass = lds.rmass;
+    auto& acc = lds.acc;                                      // (written after a barrier that ends the use of the words)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
         if (j == 0) {

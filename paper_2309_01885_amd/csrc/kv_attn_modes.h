@@ -23,6 +23,28 @@ template <int DP, KvMode MODE> void kv_mode_launch(const KvAttn& a, const KvPlan
     });
 }
 
+// Both lists at once where the shared part's tiles have 32 rows and the own part's 16: the short own parts fill what the
+// others leave.
+template <int DP, int GROUP> union KvPairLds {
+    KvFewLds<DP, GROUP, 2> shared;
+    KvFewLds<DP, GROUP, 1> own;
+};
+template <int DP, int GROUP>
+__global__ __launch_bounds__(256, kv_few_occupancy(DP, GROUP, 2, 1)) void kv_pair_kernel(KvAttn a, KvPlan plan)
+{
+    constexpr KvMode MODE = kKvListed;
+    constexpr int PARTS = 1;
+    __shared__ KvPairLds<DP, GROUP> both;
+    if ((int)blockIdx.x < plan.wgs0) {
+        constexpr int NT = 2;
+        auto& lds = both.shared;
+#include "kv_attn_few.h"
+    } else {
+        constexpr int NT = 1;
+        auto& lds = both.own;
+#include "kv_attn_few.h"
+    }
+}
 // Joins what the lists' entries found for a row: the parts of the group's shared records, then those of the sequence's
 // own.  A thread has 8 channels of a row and every SUB-th of its parts.
 template <int DP, int SUB> __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttn a, KvPlan plan, KvShared sh, uint32_t tiles)
@@ -51,8 +73,8 @@ template <int DP, int SUB> __global__ __launch_bounds__(256) void kv_shared_join
     const int qi = row / plan.per, head = kvh * plan.per + row - qi * plan.per;
     const int all = mine ? shared + own : 0;
     const int at_a = before + row;
-    const int64_t from_a = (int64_t)(shared_item + (kvh * shared_tiles + at_a / sh.rows[0]) * shared) * sh.rows[0] + at_a % sh.rows[0];
-    const int64_t from_b = (int64_t)sh.room[0] * sh.rows[0] + (int64_t)(own_item + (kvh * own_tiles + row / sh.rows[1]) * own) * sh.rows[1] + row % sh.rows[1];
+    const int64_t from_a = (int64_t)(shared_item + (kvh * shared_tiles + (at_a >> sh.rows_log2[0])) * shared) * sh.rows[0] + (at_a & (sh.rows[0] - 1));
+    const int64_t from_b = (int64_t)sh.room[0] * sh.rows[0] + (int64_t)(own_item + (kvh * own_tiles + (row >> sh.rows_log2[1])) * own) * sh.rows[1] + (row & (sh.rows[1] - 1));
     // (the shared parts' slopes count from their last token)
     const float shift = mine && a.slopes && shared ? a.slopes[head] * kLog2e * (float)(records * kKvTok - 1 - (len - nq + qi)) : 0.f;
     auto place = [&](int s) { return s < shared ? from_a + (int64_t)s * sh.rows[0] : from_b + (int64_t)(s - shared) * sh.rows[1]; };
@@ -122,8 +144,14 @@ template <int DP> void kv_sinks_width(const KvAttn& a, const KvPlan& plan, KvFor
 template <int DP> void kv_listed_width(const KvAttn& a, const KvPlan& plan, const KvShared& sh, KvForm shared, KvForm own, hipStream_t s)
 {
     KvPlan p = plan;
-    if (shared.many == own.many && shared.nt == own.nt) {
-        kv_mode_launch<DP, kKvListed>(a, p, own, dim3((unsigned)(sh.room[0] + sh.room[1])), s);
+    const dim3 all((unsigned)(sh.room[0] + sh.room[1]));
+    if (sh.joint && shared.nt != own.nt) {
+        kv_dispatch_group<DP>(a.group, [&](auto shape) {
+            constexpr int G = decltype(shape)::GROUP;
+            if constexpr (kv_few_nt(DP, G, false) == 2) hipLaunchKernelGGL((kv_pair_kernel<DP, G>), all, dim3(256), 0, s, a, p);
+        });
+    } else if (sh.joint) {
+        kv_mode_launch<DP, kKvListed>(a, p, own, all, s);
     } else {
         kv_mode_launch<DP, kKvListed>(a, p, shared, dim3((unsigned)sh.room[0]), s);
         p.wgs0 = 0;

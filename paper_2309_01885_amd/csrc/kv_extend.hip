@@ -14,8 +14,8 @@ namespace qe {
 namespace {
 
 struct Change {
-    int64_t tokens, give, need;
-    int32_t old, now, held, want, keep;
+    int64_t tokens;
+    int32_t old, now, held, want, give, need;
     bool wrong;
 };
 
@@ -32,11 +32,11 @@ __device__ inline Change change_of(const KvExtend& a, int64_t b, bool report)
     if (c.wrong && report) set_status(a.status, QE_ERR_ARG);
     c.old = (int32_t)old;
     c.now = (int32_t)(c.wrong ? old : now);
-    c.keep = (int32_t)keep;
     c.held = c.want = 0;
     if (!c.wrong) {
-        c.held = (int32_t)max((old + a.page - 1) / a.page, keep);
-        c.want = (int32_t)max((now + a.page - 1) / a.page, keep);
+        // (32 bits: lengths are)
+        c.held = max((int32_t)(((uint32_t)old + (uint32_t)a.page - 1) / (uint32_t)a.page), (int32_t)keep);
+        c.want = max((int32_t)(((uint32_t)now + (uint32_t)a.page - 1) / (uint32_t)a.page), (int32_t)keep);
     }
     c.give = max(c.held - c.want, 0);
     c.need = max(c.want - c.held, 0);
@@ -80,47 +80,66 @@ __device__ inline void place(const KvExtend& a, int64_t i, int64_t b, const KvEx
 
 __global__ __launch_bounds__(kScanThreads) void kv_extend_kernel(KvExtend a, bool fill)
 {
-    __shared__ int64_t part[4][kScanThreads / 64];
+    __shared__ ScanLds<3> lds;
+    __shared__ int64_t wave_taken[kScanThreads / 64];
     __shared__ int32_t start[kScanThreads + 1];
     __shared__ KvExtendSeq seqs[kScanThreads];
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int64_t per = (a.batch + kScanThreads - 1) / kScanThreads;
+    __shared__ int2 back[kScanThreads];                  // pages that go back before a sequence's, and the first of its own
+    const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x;
+    const int64_t per = (a.batch + threads - 1) / threads;
     const int64_t b0 = min(tid * per, a.batch), b1 = min(b0 + per, a.batch);
-    int64_t tokens = 0, give = 0, need = 0;
+    int64_t free_count = *a.free_count;
+    int64_t sum[3] = {0, 0, 0}, own[3], all[3];          // tokens, pages that go back, pages wanted
     Change c = {};
     for (int64_t b = b0; b < b1; ++b) {
         c = change_of(a, b, true);
-        tokens += c.tokens;
-        give += c.give;
-        need += c.need;
+        sum[0] += c.tokens;
+        sum[1] += c.give;
+        sum[2] += c.need;
     }
-    int64_t all_tokens, all_give, all_need;
-    int64_t token = scan_add(tokens, part[0], all_tokens) - tokens;
-    int64_t given = scan_add(give, part[1], all_give) - give;
-    int64_t needed = scan_add(need, part[2], all_need) - need;
-    int64_t held_free = *a.free_count;
-    const bool bad = held_free < 0 || held_free > a.num_pages;
-    held_free = max((int64_t)0, min(held_free, a.num_pages));
-    const int64_t top = held_free + all_give, have = min(top, a.num_pages);
-    if (tid == 0 && (bad || top > a.num_pages || all_tokens > a.total)) set_status(a.status, QE_ERR_ARG);
+#pragma unroll
+    for (int n = 0; n < 3; ++n) own[n] = sum[n];
+    scan_add(sum, lds, all);
+    int64_t token = sum[0] - own[0], given = sum[1] - own[1], needed = sum[2] - own[2];
+    const bool bad = free_count < 0 || free_count > a.num_pages;
+    free_count = max((int64_t)0, min(free_count, a.num_pages));
+    const int64_t top = free_count + all[1], have = min(top, a.num_pages);
+    if (tid == 0 && (bad || top > a.num_pages || all[0] > a.total)) set_status(a.status, QE_ERR_ARG);
 
-    // pages that go back: a wave moves its threads' pages together, a sequence after the other
-    for (int64_t n = 0; n < per; ++n) {
-        const int64_t b = b0 + n;
-        if (per > 1 && b < b1) c = change_of(a, b, false);
-        const int64_t mine = b < b1 ? c.give : 0;
-        uint64_t left = __ballot(mine > 0);
-        while (left) {
-            const int l = __builtin_ctzll(left);
-            left &= left - 1;
-            const int64_t row = __shfl(b, l) * a.width, rank = __shfl(given, l), from = __shfl(c.want, l), count = __shfl(mine, l);
-            for (int64_t j = lane; j < count; j += 64) {
-                const int64_t at = top - 1 - (rank + j);
-                if (at < a.num_pages) a.free[at] = a.table[row + from + j];
-                a.table[row + from + j] = -1;
+    // pages that go back: a thread a page; of more sequences than threads a wave's together, a sequence after the other
+    if (all[1] > 0 && per == 1 && all[1] <= 0x7fffffff) {
+        back[tid] = make_int2((int32_t)given, c.want);
+        __syncthreads();
+        for (int32_t r = tid; r < (int32_t)all[1]; r += threads) {
+            int lo = 0, hi = (int)a.batch;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (back[mid].x <= r) lo = mid;
+                else hi = mid;
             }
+            int32_t* const page = a.table + lo * a.width + back[lo].y + (r - back[lo].x);
+            if (top - 1 - r < a.num_pages) a.free[top - 1 - r] = *page;
+            *page = -1;
         }
-        given += mine;
+    } else {
+        for (int64_t n = 0; all[1] > 0 && n < per; ++n) {
+            const int64_t b = b0 + n;
+            if (per > 1 && b < b1) c = change_of(a, b, false);
+            const int32_t mine = b < b1 ? c.give : 0;
+            uint64_t left = __ballot(mine > 0);
+            while (left) {
+                const int l = __builtin_ctzll(left);
+                left &= left - 1;
+                int32_t* const row = a.table + __shfl(b, l) * a.width + __shfl(c.want, l);
+                const int64_t at = top - 1 - __shfl(given, l);
+                const int32_t count = __shfl(mine, l);
+                for (int32_t j = lane; j < count; j += 64) {
+                    if (at - j < a.num_pages) a.free[at - j] = row[j];
+                    row[j] = -1;
+                }
+            }
+            given += mine;
+        }
     }
 
     // who gets the pages
@@ -134,14 +153,13 @@ __global__ __launch_bounds__(kScanThreads) void kv_extend_kernel(KvExtend a, boo
         s.old = c.old;
         s.held = c.held;
         s.first = got ? (int32_t)min(needed, (int64_t)0x7fffffff) : c.wrong ? -2 : -1;
-        if (got) taken = max(taken, c.need ? last : 0);
-        const int32_t from = (int32_t)min(token, a.total);
-        s.start = from;
-        a.q_start[b] = from;
+        if (got && c.need) taken = last;
+        s.start = (int32_t)min(token, a.total);
+        a.q_start[b] = s.start;
         if (got) a.lengths[b] = c.now;
         if (fill) {
             seqs[b] = s;
-            start[b] = from;
+            start[b] = s.start;
         } else {
             a.seqs[b] = s;
         }
@@ -150,44 +168,37 @@ __global__ __launch_bounds__(kScanThreads) void kv_extend_kernel(KvExtend a, boo
     }
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) taken = max(taken, __shfl_xor(taken, m));
-    if (lane == 0) part[3][tid >> 6] = taken;
-    __syncthreads();                                     // (also: every thread has read free_count, and the pages that go back are there)
+    if (lane == 0) wave_taken[tid >> 6] = taken;
+    if (tid == 0 && fill) start[a.batch] = (int32_t)min(all[0], a.total);
+    __syncthreads();                                     // (also: the pages that go back are there)
     if (tid == 0) {
-#pragma unroll
-        for (int w = 0; w < kScanThreads / 64; ++w) taken = max(taken, part[3][w]);
-        const int32_t end = (int32_t)min(all_tokens, a.total);
-        a.q_start[a.batch] = end;
-        start[fill ? a.batch : 0] = end;
-        if (a.lacking) *a.lacking = (int32_t)min(max(all_need - have, (int64_t)0), (int64_t)0x7fffffff);
+        for (int w = 1; w < threads / 64; ++w) taken = max(taken, wave_taken[w]);
+        a.q_start[a.batch] = (int32_t)min(all[0], a.total);
+        if (a.lacking) *a.lacking = (int32_t)min(max(all[2] - have, (int64_t)0), (int64_t)0x7fffffff);
         *a.free_count = (int32_t)(have - taken);
         if (!fill) *a.top = top;
     }
     if (!fill) return;
-    __syncthreads();
-    for (int64_t i = tid; i < a.total; i += kScanThreads) {
+    for (int64_t i = tid; i < a.total; i += threads) {
         const int64_t b = sequence_of(start, a.batch, i);
         place(a, i, b, seqs, b < a.batch ? start[b] : 0, top);
     }
 }
 
-// The tokens of larger calls: 1024 a workgroup.
-constexpr int kFillTokens = 1024, kFillStarts = 4096;
-__global__ __launch_bounds__(256) void kv_fill_kernel(KvExtend a)
+// The tokens of larger calls.
+constexpr int kFillTokens = 256, kFillStarts = 4096;
+__global__ __launch_bounds__(kFillTokens) void kv_fill_kernel(KvExtend a)
 {
     __shared__ int32_t start[kFillStarts + 1];
     const bool near = a.batch <= kFillStarts;
     if (near) {
-        for (int64_t b = threadIdx.x; b <= a.batch; b += 256) start[b] = a.q_start[b];
+        for (int64_t b = threadIdx.x; b <= a.batch; b += kFillTokens) start[b] = a.q_start[b];
         __syncthreads();
     }
-    const int64_t top = *a.top, first = (int64_t)blockIdx.x * kFillTokens;
-#pragma unroll
-    for (int n = 0; n < kFillTokens / 256; ++n) {
-        const int64_t i = first + 256 * n + threadIdx.x;
-        if (i >= a.total) return;
-        const int64_t b = near ? sequence_of(start, a.batch, i) : sequence_of(a.q_start, a.batch, i);
-        place(a, i, b, a.seqs, b < a.batch ? (near ? start[b] : a.q_start[b]) : 0, top);
-    }
+    const int64_t top = *a.top, i = (int64_t)blockIdx.x * kFillTokens + threadIdx.x;
+    if (i >= a.total) return;
+    const int64_t b = near ? sequence_of(start, a.batch, i) : sequence_of(a.q_start, a.batch, i);
+    place(a, i, b, a.seqs, b < a.batch ? (near ? start[b] : a.q_start[b]) : 0, top);
 }
 
 // Calls of at most this many tokens (and a sequence a thread) are one launch.
@@ -203,8 +214,8 @@ qe_status launch_kv_extend(const KvExtend& call, void* ws, hipStream_t s)
     a.top = reinterpret_cast<int64_t*>(static_cast<char*>(ws) + kStatusBytes);
     a.seqs = reinterpret_cast<KvExtendSeq*>(static_cast<char*>(ws) + 2 * kStatusBytes);
     const bool fill = a.batch <= kScanThreads && a.total <= kFillInPlace;
-    hipLaunchKernelGGL(kv_extend_kernel, dim3(1), dim3(kScanThreads), 0, s, a, fill);
-    if (!fill && a.total > 0) hipLaunchKernelGGL(kv_fill_kernel, dim3((unsigned)cdiv(a.total, kFillTokens)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(kv_extend_kernel, dim3(1), dim3(scan_threads(std::max(std::min(a.batch * a.width, a.batch + kScanThreads), fill ? a.total : 0))), 0, s, a, fill);
+    if (!fill && a.total > 0) hipLaunchKernelGGL(kv_fill_kernel, dim3((unsigned)cdiv(a.total, kFillTokens)), dim3(kFillTokens), 0, s, a);
     return hipGetLastError() == hipSuccess ? QE_OK : QE_ERR_HIP;
 }
 

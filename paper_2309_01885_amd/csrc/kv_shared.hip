@@ -10,6 +10,8 @@
 #include "kv_attn_modes.h"
 #include "kv_scan.h"
 
+#include <algorithm>
+
 namespace qe {
 
 extern template void kv_listed_width<64>(const KvAttn&, const KvPlan&, const KvShared&, KvForm, KvForm, hipStream_t);
@@ -22,226 +24,241 @@ namespace {
 
 // Position of query 0 of a shared part: behind every token (and so that a position stays an int).
 constexpr int32_t kBehind = 1 << 29;
-constexpr int kNear = 4096;                              // lists whose starts are searched in LDS
+constexpr int kMaxGroups = kScanThreads;                 // a thread a group
 
-__device__ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__device__ inline int32_t div_up(int32_t a, int32_t b) { return (int32_t)(((uint32_t)a + (uint32_t)b - 1) / (uint32_t)b); }
 
-// Entries: splits of n records in pieces of about `size`, at most as many as the lists were made for.
-__device__ inline int32_t splits_of(int64_t n, int64_t size) { return n == 0 ? 0 : (int32_t)max(n / size, (int64_t)1); }
+// Pieces of about `size` (or up to twice that) that n records are cut into: no more in all than the sizes were made for.
+__device__ inline int32_t pieces(int32_t n, int32_t size) { return n == 0 ? 0 : max(n / size, 1); }
+// The first record of piece k of m.
+__device__ inline int32_t piece(int32_t n, int32_t m, int32_t k)
+{
+    const uint32_t q = (uint32_t)n / (uint32_t)m;
+    return (int32_t)(q * (uint32_t)k + min((uint32_t)k, (uint32_t)n - q * (uint32_t)m));
+}
 
+// A thread has a group, and a stretch of sequences.  What one needs of the other goes through LDS; the entries are written
+// last, one after the other by all threads.
 __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, KvShared sh)
 {
-    __shared__ int64_t part[3][kScanThreads / 64];
-    __shared__ int32_t start[kNear + 1];
-    __shared__ int wrong_groups;
-    const int tid = threadIdx.x, lane = tid & 63, per = a.heads / a.c.heads;
-    const int64_t width = a.width, room = width * (int64_t)a.c.per * kKvTok;
-    if (tid == 0) wrong_groups = 0;
-    __syncthreads();
-    // the sequences
-    for (int64_t b = tid; b < a.batch; b += kScanThreads) {
-        int64_t first = b * a.max_q, nq = a.max_q, len = a.lengths[b];
-        bool bad = len < 0 || len > room;
+    __shared__ ScanLds<2> lds;
+    __shared__ ScanLds<2> lds2;
+    __shared__ int32_t bound[kMaxGroups + 1];            // first sequences
+    __shared__ int32_t sees[kMaxGroups], first[kMaxGroups], active[kMaxGroups], records[kMaxGroups], item[kMaxGroups + 1];
+    __shared__ unsigned long long tokens[kMaxGroups];
+    __shared__ KvGroup group[kMaxGroups];
+    __shared__ KvSequence seq[kScanThreads];              // (of more sequences than threads: in memory alone)
+    __shared__ int wrong, end_b;
+    const int tid = threadIdx.x, threads = blockDim.x, per = a.heads / a.c.heads;
+    const int64_t room = min(a.width * (int64_t)a.c.per * kKvTok, (int64_t)0x7fffffff);
+    const int64_t run = (a.batch + threads - 1) / threads, b0 = min((int64_t)tid * run, (int64_t)a.batch), b1 = min(b0 + run, (int64_t)a.batch);
+    const int ngroups = sh.ngroups;
+    int32_t shared_pages = 0;
+    if (tid == 0) {
+        wrong = 0;
+        end_b = 0x7fffffff;
+    }
+    if (tid <= ngroups) bound[tid] = sh.groups[tid];
+    if (tid == 0 && threads == ngroups) bound[ngroups] = sh.groups[ngroups];
+    if (tid < ngroups) {
+        shared_pages = sh.shared[tid];
+        sees[tid] = 0x7fffffff;
+        first[tid] = 0;
+        active[tid] = 0;
+        tokens[tid] = 0;
+    }
+    // a sequence's rows and length
+    auto sequence = [&](int64_t b, bool report) {
         KvSequence s = {};
+        int64_t at = b * a.max_q, nq = a.max_q;
+        const int64_t len = a.lengths[b];
+        bool bad = len < 0 || len > a.width * (int64_t)a.c.per * kKvTok;
         if (a.q_start) {
-            first = a.q_start[b];
-            nq = (int64_t)a.q_start[b + 1] - first;
-            if (first < 0 || nq < 0 || nq > a.max_q || first + nq > a.total) {
+            at = a.q_start[b];
+            nq = (int64_t)a.q_start[b + 1] - at;
+            if (at < 0 || nq < 0 || nq > a.max_q || at + nq > a.total) {
                 bad = true;
-                first = 0;
+                at = 0;
                 nq = -1;
             }
         }
-        if (bad) set_status(a.status, QE_ERR_ARG);
-        s.first = (int32_t)first;
+        if (bad && report) set_status(a.status, QE_ERR_ARG);
+        s.first = (int32_t)at;
         s.nq = (int32_t)nq;
         s.len = (int32_t)max((int64_t)0, min(len, room));
         s.group = -1;
-        sh.seq[b] = s;
-    }
-    for (int g = tid; g < sh.ngroups; g += kScanThreads) {
-        const int32_t s0 = sh.groups[g], s1 = sh.groups[g + 1], n = sh.shared[g];
-        if (s0 < 0 || s1 < s0 || s1 > a.batch) wrong_groups = 1;
-        if (n < 0 || n > width) set_status(a.status, QE_ERR_ARG);
+        return s;
+    };
+    KvSequence s = {};
+    if (b0 < b1) s = sequence(b0, true);
+    __syncthreads();
+    if (tid < ngroups && (bound[tid] < 0 || bound[tid + 1] < bound[tid] || bound[tid + 1] > a.batch)) wrong = 1;
+    // what all queries of a group see
+    auto group_of = [&](int64_t b) {
+        if (b < bound[0] || b >= bound[ngroups]) return -1;
+        return (int)last_at_most(bound, ngroups, b);
+    };
+    for (int64_t b = b0; b < b1; ++b) {
+        if (b > b0) s = sequence(b, true);
+        const int g = group_of(b);
+        if (g < 0) continue;
+        if (b == bound[g]) first[g] = s.first;
+        if (s.nq < 0) atomicMin(&sees[g], 0);            // (its rows are not where the group's are)
+        if (s.nq <= 0) continue;
+        atomicMin(&sees[g], max(0, a.causal ? (int32_t)max((int64_t)s.len - s.nq + 1, (int64_t)0) : s.len));
+        atomicAdd(&active[g], 1);
+        atomicAdd(&tokens[g], (unsigned long long)s.nq);
     }
     __syncthreads();
-    if (wrong_groups && tid == 0) set_status(a.status, QE_ERR_ARG);
-    const int ngroups = wrong_groups ? 0 : sh.ngroups;
+    const bool none = wrong != 0;
+    if (none && tid == 0) set_status(a.status, QE_ERR_ARG);
+    KvGroup gr = {};
+    if (tid < ngroups) {
+        if (shared_pages < 0 || shared_pages > a.width) set_status(a.status, QE_ERR_ARG);
+        const int64_t most = max((int64_t)0, min((int64_t)shared_pages, a.width)) * a.c.per;
+        const bool gains = !none && active[tid] > 1 && tokens[tid] <= (unsigned long long)a.total;
+        gr.first_seq = bound[tid];
+        gr.first = first[tid];
+        gr.tokens = gains ? (int32_t)tokens[tid] : 0;
+        gr.records = gains ? (int32_t)min(most, (int64_t)(sees[tid] / kKvTok)) : 0;
+        gr.tiles = gr.records ? (gr.tokens * per + sh.rows[0] - 1) >> sh.rows_log2[0] : 0;
+        records[tid] = gr.records;
+    }
+    __syncthreads();
 
-    // the groups, a wave each: the records that all of their queries see
-    for (int g = tid >> 6; g < ngroups; g += kScanThreads / 64) {
-        const int32_t s0 = sh.groups[g], s1 = sh.groups[g + 1];
-        int64_t sees = max(0, min(sh.shared[g], (int32_t)min(width, (int64_t)0x7fffffff))) * (int64_t)a.c.per * kKvTok;
-        int64_t tokens = 0;
-        int active = 0;
-        for (int64_t b = s0 + lane; b < s1; b += 64) {
-            const KvSequence s = sh.seq[b];
-            if (s.nq < 0) sees = 0;                      // (its rows are not where the group's are)
-            if (s.nq <= 0) continue;
-            sees = min(sees, max((int64_t)0, a.causal ? (int64_t)s.len - s.nq + 1 : (int64_t)s.len));
-            tokens += s.nq;
-            ++active;
+    // the sizes of the lists' entries: what fills the chip; once more without sharing where the first list would overflow (rows
+    // that several groups claim, with a bad q_start between them)
+    int64_t all[2], at[2], own[2];
+    int32_t size[2], items_a;
+    bool share = !none;
+    for (;;) {
+        auto own_records = [&](const KvSequence& q) { return max(0, div_up(q.len, kKvTok) - (q.group >= 0 ? records[q.group] : 0)); };
+        auto place = [&](KvSequence& q, int64_t b) {
+            const int g = share ? group_of(b) : -1;
+            q.group = g >= 0 && records[g] ? g : -1;
+            q.tiles = q.nq > 0 ? (q.nq * per + sh.rows[1] - 1) >> sh.rows_log2[1] : 0;
+        };
+        at[0] = share ? (int64_t)gr.tiles * gr.records : 0;
+        at[1] = 0;
+        for (int64_t b = b0; b < b1; ++b) {
+            if (run > 1) s = sequence(b, false);
+            place(s, b);
+            at[1] += (int64_t)s.tiles * own_records(s);
         }
+        scan_add(at, lds, all);
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            sees = min(sees, __shfl_xor(sees, m));
-            tokens += __shfl_xor(tokens, m);
-            active += __shfl_xor(active, m);
+        for (int y = 0; y < 2; ++y) {
+            const int64_t work = sh.joint ? all[0] * sh.weight[0] + all[1] * sh.weight[1] : all[y] * sh.weight[y];
+            size[y] = max(sh.least[y], (int32_t)fmin(2147483647., ceil((double)(work * a.c.heads) * sh.part_of_fill[y])));
         }
-        KvGroup gr = {};
-        gr.first_seq = s0;
-        gr.tokens = (int32_t)min(tokens, a.total);
-        gr.records = active < 2 || tokens > a.total ? 0 : (int32_t)(sees / kKvTok);
-        gr.tiles = gr.records ? (int32_t)div_up((int64_t)gr.tokens * per, sh.rows[0]) : 0;
-        if (s0 < s1) gr.first = sh.seq[s0].first;
-        if (lane == 0) sh.group[g] = gr;
-        if (gr.records)
-            for (int64_t b = s0 + lane; b < s1; b += 64) sh.seq[b].group = g;
-    }
-    __syncthreads();
-
-    // a piece's size: what fills the chip
-    int64_t work[2] = {0, 0}, all[2], size[2];
-    for (int g = tid; g < ngroups; g += kScanThreads) work[0] += (int64_t)sh.group[g].tiles * sh.group[g].records;
-    for (int64_t b = tid; b < a.batch; b += kScanThreads) {
-        const KvSequence s = sh.seq[b];
-        const int64_t own = div_up(s.len, kKvTok) - (s.group >= 0 ? sh.group[s.group].records : 0);
-        work[1] += div_up((int64_t)max(s.nq, 0) * per, sh.rows[1]) * max(own, (int64_t)0);
-    }
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        scan_add(work[y], part[y], all[y]);
-        size[y] = max((int64_t)sh.least[y], div_up(all[y] * a.c.heads, sh.fill[y]));
-    }
-
-    // where the entries lie
-    int64_t next = 0, sum;
-    for (int64_t g0 = 0; g0 < ngroups; g0 += kScanThreads) {
-        const int64_t g = g0 + tid;
-        KvGroup gr = {};
-        if (g < ngroups) gr = sh.group[g];
-        gr.splits = splits_of(gr.records, size[0]);
-        const int64_t n = (int64_t)gr.tiles * gr.splits * a.c.heads;
-        __syncthreads();
-        const int64_t end = next + scan_add(n, part[0], sum);
-        gr.item = (int32_t)min(end - n, (int64_t)sh.room[0]);
-        if (g < ngroups) {
-            sh.group[g] = gr;
-            if (g <= kNear) start[g] = gr.item;
-        }
-        next += sum;
-    }
-    __syncthreads();
-    // (rows that several groups claim, with a bad q_start between them, can be more than the list holds: then nothing is shared)
-    const bool fits = next <= sh.room[0];
-    const int64_t items_a = fits ? next : 0;
-    if (!fits) {
-        if (tid == 0) set_status(a.status, QE_ERR_ARG);
-        for (int64_t b = tid; b < a.batch; b += kScanThreads) sh.seq[b].group = -1;
-    }
-    for (int64_t i = tid; i < items_a; i += kScanThreads) {
-        int64_t g;
-        if (ngroups <= kNear) {
-            g = last_at_most(start, ngroups, i);
-        } else {
-            int64_t lo = 0, hi = ngroups;
-            while (hi - lo > 1) {
-                const int64_t mid = (lo + hi) >> 1;
-                if (sh.group[mid].item <= i) lo = mid;
-                else hi = mid;
+        gr.splits = share && gr.records ? pieces(gr.records, size[0]) : 0;
+        own[0] = at[0] = (int64_t)gr.tiles * gr.splits * a.c.heads;
+        at[1] = 0;
+        for (int64_t b = b0; b < b1; ++b) {
+            if (run > 1) {
+                s = sequence(b, false);
+                place(s, b);
             }
-            g = lo;
+            s.splits = s.tiles ? pieces(own_records(s), size[1]) : 0;
+            at[1] += (int64_t)s.tiles * s.splits * a.c.heads;
         }
-        const KvGroup gr = sh.group[g];
+        own[1] = at[1];
+        scan_add(at, lds2, all);
+        items_a = (int32_t)all[0];
+        if (all[0] <= sh.room[0]) break;
+        if (tid == 0) set_status(a.status, QE_ERR_ARG);
+        share = false;
+        gr.records = gr.tiles = 0;
+        __syncthreads();
+    }
+    if (tid < ngroups) {
+        gr.item = (int32_t)(at[0] - own[0]);
+        item[tid] = gr.item;
+        group[tid] = gr;
+    }
+    int64_t next = at[1] - own[1];
+    for (int64_t b = b0; b < b1; ++b) {
+        if (run > 1) {
+            s = sequence(b, false);
+            const int g = share ? group_of(b) : -1;
+            s.group = g >= 0 && records[g] ? g : -1;
+            s.tiles = s.nq > 0 ? (s.nq * per + sh.rows[1] - 1) >> sh.rows_log2[1] : 0;
+            s.splits = s.tiles ? pieces(max(0, div_up(s.len, kKvTok) - (s.group >= 0 ? records[s.group] : 0)), size[1]) : 0;
+        }
+        const int64_t n = (int64_t)s.tiles * s.splits * a.c.heads;
+        s.item = (int32_t)min(next, (int64_t)sh.room[1]);
+        next += n;
+        if (next > sh.room[1]) {
+            // (rows that several sequences claim, with a bad q_start between them: the last of these get nothing)
+            set_status(a.status, QE_ERR_ARG);
+            atomicMin(&end_b, s.item);
+            s.nq = -1;
+            s.splits = 0;
+        }
+        if (run == 1) seq[tid] = s;
+        else sh.seq[b] = s;
+    }
+    __syncthreads();
+    const int32_t items_b = (int32_t)min(all[1], (int64_t)end_b);
+    if (tid == 0) {
+        sh.count[0] = items_a;
+        sh.count[1] = items_b;
+    }
+    for (int32_t i = tid; i < items_a; i += threads) {
+        const KvGroup q = group[last_at_most(item, ngroups, i)];
         // tiles of the same records side by side
-        const uint32_t at = (uint32_t)(i - gr.item), tile = at % (uint32_t)gr.tiles, rest = at / (uint32_t)gr.tiles;
-        const uint32_t split = rest % (uint32_t)gr.splits, kvh = rest / (uint32_t)gr.splits;
+        const uint32_t n = (uint32_t)(i - q.item), tile = n % (uint32_t)q.tiles, rest = n / (uint32_t)q.tiles;
+        const int32_t split = (int32_t)(rest % (uint32_t)q.splits), kvh = (int32_t)(rest / (uint32_t)q.splits);
         KvItem it = {};
-        it.first = gr.first;
-        it.b = gr.first_seq;
-        it.kvh = (int32_t)kvh;
-        it.tile_row = (int32_t)(tile * sh.rows[0]);
-        it.rows = gr.tokens * per;
-        it.len = gr.records * kKvTok;
+        it.first = q.first;
+        it.b = q.first_seq;
+        it.kvh = kvh;
+        it.tile_row = (int32_t)tile * sh.rows[0];
+        it.rows = q.tokens * per;
+        it.len = q.records * kKvTok;
         it.pos0 = kBehind;
-        it.rec0 = (int32_t)((int64_t)gr.records * split / gr.splits);
-        it.rec1 = (int32_t)((int64_t)gr.records * (split + 1) / gr.splits);
-        it.slot = (int32_t)((gr.item + (kvh * gr.tiles + tile) * gr.splits + split) * sh.rows[0]);
+        it.rec0 = piece(q.records, q.splits, split);
+        it.rec1 = piece(q.records, q.splits, split + 1);
+        it.slot = (q.item + (kvh * q.tiles + (int32_t)tile) * q.splits + split) * sh.rows[0];
         it.ref = it.len - 1;
         sh.items[0][i] = it;
     }
-    __syncthreads();
-    next = 0;
-    for (int64_t b0 = 0; b0 < a.batch; b0 += kScanThreads) {
-        const int64_t b = b0 + tid;
-        KvSequence s = {};
-        int64_t own = 0;
-        if (b < a.batch) {
-            s = sh.seq[b];
-            own = max((int64_t)0, div_up(s.len, kKvTok) - (s.group >= 0 ? sh.group[s.group].records : 0));
-        }
-        s.tiles = (int32_t)div_up((int64_t)max(s.nq, 0) * per, sh.rows[1]);
-        s.splits = s.tiles ? splits_of(own, size[1]) : 0;
-        const int64_t n = (int64_t)s.tiles * s.splits * a.c.heads;
-        __syncthreads();
-        const int64_t end = next + scan_add(n, part[0], sum);
-        s.item = (int32_t)min(end - n, (int64_t)sh.room[1]);
-        if (b < a.batch) {
-            if (end > sh.room[1]) {
-                // (rows that several sequences claim, with a bad q_start between them: the last of these get nothing)
-                set_status(a.status, QE_ERR_ARG);
-                s.nq = -1;
-                s.splits = 0;
-            }
-            sh.seq[b] = s;
-            if (b <= kNear) start[b] = s.item;
-        }
-        next += sum;
-    }
-    __syncthreads();
-    const int64_t items_b = min(next, (int64_t)sh.room[1]);
-    for (int64_t i = tid; i < items_b; i += kScanThreads) {
-        int64_t b;
-        if (a.batch <= kNear) {
-            b = last_at_most(start, a.batch, i);
-        } else {
-            int64_t lo = 0, hi = a.batch;
-            while (hi - lo > 1) {
-                const int64_t mid = (lo + hi) >> 1;
-                if (sh.seq[mid].item <= i) lo = mid;
-                else hi = mid;
-            }
-            b = lo;
-        }
-        const KvSequence s = sh.seq[b];
+    // a thread a sequence and key head
+    for (int64_t p = tid; p < (int64_t)a.batch * a.c.heads; p += threads) {
+        const uint32_t b = (uint32_t)p / (uint32_t)a.c.heads;
+        const int32_t kvh = (int32_t)((uint32_t)p - b * (uint32_t)a.c.heads);
+        const KvSequence q = run == 1 ? seq[b] : sh.seq[b];
+        if (q.nq <= 0 || q.splits == 0) continue;
+        const int32_t from = q.group >= 0 ? records[q.group] : 0, count = div_up(q.len, kKvTok) - from;
+        KvItem* to = sh.items[1] + q.item + kvh * q.tiles * q.splits;
         KvItem it = {};
-        if (s.splits > 0) {
-            const uint32_t at = (uint32_t)(i - s.item), tile = at % (uint32_t)s.tiles, rest = at / (uint32_t)s.tiles;
-            const uint32_t split = rest % (uint32_t)s.splits, kvh = rest / (uint32_t)s.splits;
-            const int32_t from = s.group >= 0 ? sh.group[s.group].records : 0, n = (int32_t)div_up(s.len, kKvTok) - from;
-            it.first = s.first;
-            it.b = (int32_t)b;
-            it.kvh = (int32_t)kvh;
-            it.tile_row = (int32_t)(tile * sh.rows[1]);
-            it.rows = s.nq * per;
-            it.len = s.len;
-            it.pos0 = s.len - s.nq;
-            it.rec0 = from + (int32_t)((int64_t)n * split / s.splits);
-            it.rec1 = from + (int32_t)((int64_t)n * (split + 1) / s.splits);
-            if (a.causal) {
-                // (what the tile's last row does not see)
-                const int32_t last = (min(it.rows, it.tile_row + sh.rows[1]) - 1) / per, end = max(0, it.pos0 + last + 1);
-                it.rec1 = max(it.rec0, min(it.rec1, (end + kKvTok - 1) / kKvTok));
+        it.first = q.first;
+        it.b = (int32_t)b;
+        it.kvh = kvh;
+        it.rows = q.nq * per;
+        it.len = q.len;
+        it.pos0 = q.len - q.nq;
+        it.ref = -1;
+        const int32_t slot = sh.room[0] * sh.rows[0] + (q.item + kvh * q.tiles * q.splits) * sh.rows[1];
+        for (int32_t split = 0; split < q.splits; ++split) {
+            const int32_t r0 = from + piece(count, q.splits, split), r1 = from + piece(count, q.splits, split + 1);
+            for (int32_t tile = 0; tile < q.tiles; ++tile) {
+                it.tile_row = tile * sh.rows[1];
+                it.rec0 = r0;
+                it.rec1 = r1;
+                if (a.causal && q.tiles > 1) {
+                    // (what the tile's last row does not see)
+                    const int32_t last = (min(it.rows, it.tile_row + sh.rows[1]) - 1) / per, end = max(0, it.pos0 + last + 1);
+                    it.rec1 = max(r0, min(r1, div_up(end, kKvTok)));
+                }
+                it.slot = slot + (tile * q.splits + split) * sh.rows[1];
+                *to++ = it;
             }
-            it.slot = sh.room[0] * sh.rows[0] + (int32_t)((s.item + (kvh * s.tiles + tile) * s.splits + split) * sh.rows[1]);
-            it.ref = -1;
         }
-        sh.items[1][i] = it;
     }
-    if (tid == 0) {
-        sh.count[0] = (int32_t)items_a;
-        sh.count[1] = (int32_t)items_b;
-    }
+    // (what the join reads; before the barrier, everything would wait for these stores)
+    if (tid < ngroups) sh.group[tid] = gr;
+    if (run == 1 && b0 < b1) sh.seq[b0] = s;
 }
 
 struct Lists {
@@ -250,20 +267,38 @@ struct Lists {
     int64_t slots;                                       // rows of partial results
 };
 
+// Rows, and records of its tiles, from which a part takes the many-row form: entries of 48 records on 512 workgroups.  Shorter
+// ones lose to its start and the 64 KB of results that an entry writes.  One query each, us of the few rows' form / the
+// many's: 64 sequences behind 8192 tokens, 32 heads on 8 of 128 channels (8 records an entry) 54 / 69, behind 32768 (32) 96 /
+// 110; 32 behind 8192, 232 heads on 8 of 64 (29) 56 / 74; 7 queries of 48 behind 8192 to 16384 in five groups, 58 heads on 2
+// of 64 (94) 118 / 111; chunks of 256 of 4 behind 8192, 32 heads on 8 of 128 (136) 199 / 145.
+constexpr int64_t kManyRows = 128, kManyRecords = 48 * 512;
+// Records of 16-row tiles that sharing has to save before it is taken: what its two more launches cost.  One query each, us of
+// kv_attn / the lists: 4 sequences behind 1000 tokens, 20 heads on 5 of 80, fp32 (saves 1000) 13.8 / 20.1; 32 heads on 8 of
+// 128: 16 behind 4096 (15000) 25.4 / 25.4, 8 behind 16384 (26000) 35.6 / 32.9, 64 behind 8192 (106000) 103 / 54.
+constexpr int64_t kSaves = 20000;
+
 // The forms of the shared and the own part, and the sizes of their lists.
-Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int group, bool f32, int64_t ngroups)
+Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int group, bool f32, int64_t ngroups, int64_t records)
 {
     Lists z{};
     const int dp = kv_dp(dim), per = heads / kv_heads;
     const int64_t rows = total * per, group_rows = rows / std::max<int64_t>(ngroups, 1), own_rows = max_q * per;
     const int many = kv_many_nt(dp, group, f32), few = kv_few_nt(dp, group, f32);
-    z.form[0] = group_rows >= 64 ? KvForm{true, many} : KvForm{false, group_rows > 16 ? few : 1};
-    z.form[1] = KvForm{false, own_rows > 16 ? few : 1};
+    const int64_t many_units = kv_heads * cdiv(rows, 16 * many * kKvWaves);
+    z.form[0] = group_rows >= kManyRows && many_units * std::min<int64_t>(records, 1 << 24) >= kManyRecords ? KvForm{true, many} : KvForm{false, group_rows > 16 ? few : 1};
+    z.form[1] = own_rows >= kManyRows ? KvForm{true, many} : KvForm{false, own_rows > 16 ? few : 1};
+    const bool pair = !z.form[0].many && !z.form[1].many && z.form[0].nt > z.form[1].nt;
+    z.sh.joint = pair || (z.form[0].many == z.form[1].many && z.form[0].nt == z.form[1].nt);
     int64_t units[2];
     for (int y = 0; y < 2; ++y) {
+        const KvForm form = pair ? z.form[0] : z.form[y];
         z.sh.rows[y] = 16 * z.form[y].nt * (z.form[y].many ? kKvWaves : 1);
-        z.sh.fill[y] = z.form[y].many ? 512 : 768;
+        z.sh.rows_log2[y] = __builtin_ctz((unsigned)z.sh.rows[y]);
+        z.sh.fill[y] = 256 * (form.many ? 2 : kv_few_occupancy(dp, dp <= 64 ? std::min(group, 64) : group, form.nt, f32 ? 2 : 1));
+        z.sh.weight[y] = pair && y == 0 ? 8 : pair ? 5 : 1;
         z.sh.least[y] = kKvMinRecords;
+        z.sh.part_of_fill[y] = 1. / ((double)z.sh.fill[y] * z.sh.weight[y]);
         units[y] = kv_heads * (cdiv(rows, z.sh.rows[y]) + (y == 0 ? ngroups : batch));
     }
     units[1] = std::min(units[1], kv_heads * batch * cdiv(own_rows, z.sh.rows[1]));
@@ -280,11 +315,18 @@ Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_he
 // Where the lists and the partial results do not fit 32-bit numbers, or nothing can be shared, the call is kv_attn's.
 bool listed(const Lists& z, int64_t batch, int64_t rows)
 {
-    return batch > 1 && z.sh.ngroups > 0 && rows < kBehind && z.slots < (int64_t(1) << 31) && (int64_t)z.sh.room[0] + z.sh.room[1] < (int64_t(1) << 23);
+    return batch > 1 && z.sh.ngroups > 0 && z.sh.ngroups <= kMaxGroups && rows < kBehind && z.slots < (int64_t(1) << 31) && (int64_t)z.sh.room[0] + z.sh.room[1] < (int64_t(1) << 23);
 }
 
-// Whether sharing can gain what its launches cost.
-bool gains(const KvAttn&) { return true; }
+// Whether sharing can gain what its launches cost.  (Where a sequence's rows fill tiles by themselves it saves no tile, but
+// the lists' many-row form has splits, and kv_attn's does not.)
+bool gains(const Lists& z, const KvAttn& a)
+{
+    const int64_t per = a.heads / a.c.heads, records = a.width * a.c.per, groups = z.sh.ngroups;
+    if (z.form[0].many && !kv_attn_many(a)) return true;
+    const int64_t tiles = a.batch * cdiv(a.max_q * per, 16) - groups * cdiv(a.total * per, 16 * groups);
+    return tiles > 0 && tiles * a.c.heads >= cdiv(kSaves, std::max<int64_t>(records, 1));
+}
 
 struct Layout {
     size_t group, seq, items[2], count, part, stat, end;
@@ -314,10 +356,11 @@ size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int 
 {
     size_t need = kv_attn_ws_bytes(batch, max_q, heads, kv_heads, dim);
     for (int group : {32, 64, 128})
-        for (int f32 = 0; f32 < 2; ++f32) {
-            const Lists z = lists_of(total, batch, max_q, heads, kv_heads, dim, group, f32 != 0, ngroups);
-            if (listed(z, batch, total * (heads / kv_heads))) need = std::max(need, layout_of(z, batch, kv_dp(dim)).end);
-        }
+        for (int f32 = 0; f32 < 2; ++f32)
+            for (int64_t records : {(int64_t)1, (int64_t)INT32_MAX}) {
+                const Lists z = lists_of(total, batch, max_q, heads, kv_heads, dim, group, f32 != 0, ngroups, records);
+                if (listed(z, batch, total * (heads / kv_heads))) need = std::max(need, layout_of(z, batch, kv_dp(dim)).end);
+            }
     return need;
 }
 
@@ -325,8 +368,8 @@ qe_status launch_kv_attn_shared(const KvAttn& call, const int32_t* groups, const
 {
     KvAttn a = call;
     const int dp = kv_dp(a.c.dim);
-    Lists z = lists_of(a.total, a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, a.dtype == QE_F32, ngroups);
-    if (!listed(z, a.batch, a.total * (a.heads / a.c.heads)) || !(always || gains(a))) return launch_kv_attn(a, ws, s);
+    Lists z = lists_of(a.total, a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, a.dtype == QE_F32, ngroups, a.width * a.c.per);
+    if (!listed(z, a.batch, a.total * (a.heads / a.c.heads)) || !(always || gains(z, a))) return launch_kv_attn(a, ws, s);
     kv_attn_vec(a);
     const Layout l = layout_of(z, a.batch, dp);
     char* const base = static_cast<char*>(ws);
@@ -345,7 +388,7 @@ qe_status launch_kv_attn_shared(const KvAttn& call, const int32_t* groups, const
     for (int y = 0; y < 2; ++y) plan.items[y] = sh.items[y];
     plan.count = sh.count;
     plan.wgs0 = sh.room[0];
-    hipLaunchKernelGGL(kv_shared_plan_kernel, dim3(1), dim3(kScanThreads), 0, s, a, sh);
+    hipLaunchKernelGGL(kv_shared_plan_kernel, dim3(1), dim3(scan_threads(std::max<int64_t>({a.batch, ngroups, 512}))), 0, s, a, sh);
     switch (dp) {
         case 64: kv_listed_width<64>(a, plan, sh, z.form[0], z.form[1], s); break;
         case 96: kv_listed_width<96>(a, plan, sh, z.form[0], z.form[1], s); break;
