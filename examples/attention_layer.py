@@ -3,9 +3,10 @@
     python examples/attention_layer.py [--hidden 4096 --heads 32 --kv-heads 8 --steps 16]
 
 The layer's projection is quantized to 4 bits on calibration activations (gram, grid_minmax,
-cd_sweep).  Prompts of different lengths are then read in chunks, which are written to the cache and
-attend to what it holds (kv_write, kv_attn with q_start), and every sequence goes on a token at a
-time, recorded once as a HIP graph and replayed.  Prints what the cache holds per token and how far
+cd_sweep).  Prompts of different lengths are then read in chunks: their tokens get pages and slots
+(kv_extend), queries and keys are rotated by their positions on the way into the cache (kv_append)
+and attend to what it holds (kv_attn with q_start).  Every sequence goes on a token at a
+time, all three calls recorded once as a HIP graph and replayed.  Prints what the cache holds per token and how far
 the layer's outputs lie from those of an unquantized cache and of the unquantized layer.  Weights
 and activations are synthetic.
 """
@@ -33,48 +34,53 @@ def quantize_weight(W, X, bits=4, sweeps=5):
 
 
 class PagedCache:
-    """Sequences of one layer in fixed-size pages of a pool, taken as the sequences grow."""
+    """Sequences of one layer in fixed-size pages of a pool, taken on the GPU as the sequences grow."""
 
     def __init__(self, sequences, max_len, kv_heads, dim, group=64, page=64):
         width = -(-max_len // page)
         self.pages = P.kv_pages(sequences * width, kv_heads, dim, group, page)
-        self.free = torch.randperm(sequences * width).tolist()
-        self.table = torch.full((sequences, width), -1, dtype=torch.int32)
-        self.device_table = self.table.cuda()
+        self.free = torch.randperm(sequences * width, device="cuda").int()
+        self.free_count = torch.full((1,), sequences * width, dtype=torch.int32, device="cuda")
+        self.table = torch.full((sequences, width), -1, dtype=torch.int32, device="cuda")
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device="cuda")
-        self.held = [0] * sequences
+        self.lacking = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.ws = P.workspace(P.kv_extend_workspace_size(sequences), "cuda")
         self.group, self.page = group, page
 
-    def extend(self, counts):
-        """Takes the pages for counts[b] more tokens of sequence b; the slots that they go to."""
-        slots = []
-        for b, n in enumerate(counts):
-            t = torch.arange(self.held[b], self.held[b] + n)
-            self.held[b] += n
-            for p in range(-(-self.held[b] // self.page)):
-                if self.table[b, p] < 0:
-                    self.table[b, p] = self.free.pop()
-            slots.append(self.table[b, t // self.page].long() * self.page + t % self.page)
-        self.device_table.copy_(self.table)
-        self.lengths.copy_(torch.tensor(self.held, dtype=torch.int32))
-        return torch.cat(slots).cuda()
+    def extend(self, counts, total):
+        """Pages for counts[b] (int32, device) more tokens of sequence b: slots, positions and q_start of the `total` tokens."""
+        return P.kv_extend(counts, self.table, self.lengths, self.free, self.free_count, self.page, total, lacking=self.lacking,
+                           ws=self.ws)
+
+
+def rotation(positions, dim):
+    """Cosines and sines of the positions' angles (fp32)."""
+    turn = 10000.0 ** (-torch.arange(0, dim, 2, dtype=torch.float64, device="cuda") / dim)
+    angle = torch.arange(positions, dtype=torch.float64, device="cuda")[:, None] * turn
+    return angle.cos().float(), angle.sin().float()
 
 
 class AttentionLayer:
-    def __init__(self, W, heads, kv_heads, dim, dtype):
+    def __init__(self, W, heads, kv_heads, dim, dtype, positions):
         self.W, self.heads, self.kv_heads, self.dim = W.to(dtype), heads, kv_heads, dim
+        self.cos, self.sin = rotation(positions, dim)
 
     def project(self, x):
         """Query, keys and values as slices of the fused projection (no copies)."""
         y = (x @ self.W.t()).unflatten(1, (self.heads + 2 * self.kv_heads, self.dim))
         return y.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
 
-    def attend(self, x, cache, slots, q_start=None, max_q=None, ws=None):
-        """Writes the tokens x into the cache and lets them attend to their sequences."""
+    def attend(self, x, cache, counts, max_q, ws=None):
+        """Writes the tokens x, counts[b] of sequence b, into the cache and lets them attend to their sequences."""
+        slots, positions, q_start = cache.extend(counts, x.shape[0])
         q, k, v = self.project(x)
-        P.kv_write(k, v, slots, cache.pages, group=cache.group)
-        return P.kv_attn(q, cache.pages, cache.device_table, cache.lengths, group=cache.group, q_start=q_start,
-                         max_q=max_q, ws=ws)
+        q = P.kv_append(q, k, v, slots, cache.pages, group=cache.group, positions=positions, cos=self.cos, sin=self.sin)
+        return P.kv_attn(q, cache.pages, cache.table, cache.lengths, group=cache.group, q_start=q_start, max_q=max_q, ws=ws)
+
+
+def turned(x, cos, sin):
+    a, b = x.chunk(2, dim=-1)
+    return torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
 
 
 def plain(layer, xs):
@@ -82,6 +88,7 @@ def plain(layer, xs):
     outs = []
     for x in xs:
         q, k, v = (t.float() for t in layer.project(x))
+        q, k = (turned(t, layer.cos[:x.shape[0], None], layer.sin[:x.shape[0], None]) for t in (q, k))
         k, v = (t.repeat_interleave(layer.heads // layer.kv_heads, dim=1) for t in (k, v))
         n = x.shape[0]
         s = torch.einsum("qhd,thd->hqt", q, k) / layer.dim ** 0.5
@@ -98,35 +105,34 @@ def serve(layer, xs, prompts, chunk, group=64, page=64):
     """Outputs of all tokens of xs: prompts[b] of them read in chunks, the others one by one."""
     n_seq, total = len(xs), [x.shape[0] for x in xs]
     cache = PagedCache(n_seq, max(total), layer.kv_heads, layer.dim, group, page)
-    outs = [[] for _ in xs]
-    while any(h < p for h, p in zip(cache.held, prompts)):
-        at = list(cache.held)
-        counts = [min(chunk, p - h) for h, p in zip(at, prompts)]
-        slots = cache.extend(counts)
-        start = torch.tensor([0] + counts, dtype=torch.int32).cumsum(0).int().cuda()
-        y = layer.attend(torch.cat([x[h:h + c] for x, h, c in zip(xs, at, counts)]), cache, slots, start, max(counts))
+    outs, held = [[] for _ in xs], [0] * n_seq
+    while any(h < p for h, p in zip(held, prompts)):
+        counts = [min(chunk, p - h) for h, p in zip(held, prompts)]
+        y = layer.attend(torch.cat([x[h:h + c] for x, h, c in zip(xs, held, counts)]), cache,
+                         torch.tensor(counts, dtype=torch.int32, device="cuda"), max(counts))
+        held = [h + c for h, c in zip(held, counts)]
         for b, part in enumerate(y.split(counts)):
             outs[b].append(part)
-    # decoding: the graph reads its tokens, slots, lengths and page table from fixed buffers
+    # decoding: the graph reads its tokens and counts from fixed buffers and moves lengths and pages itself
     x_in = torch.stack([x[p] for x, p in zip(xs, prompts)])
-    slots = torch.full((n_seq,), -1, dtype=torch.int64, device="cuda")      # the warm-up writes nothing
+    counts = torch.zeros(n_seq, dtype=torch.int32, device="cuda")           # the warm-up adds no token
     ws = P.workspace(P.kv_attn_workspace_size(n_seq, n_seq, 1, layer.heads, layer.kv_heads, layer.dim), "cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        layer.attend(x_in, cache, slots, ws=ws)
+        layer.attend(x_in, cache, counts, 1, ws=ws)
     torch.cuda.current_stream().wait_stream(side)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        y = layer.attend(x_in, cache, slots, ws=ws)
+        y = layer.attend(x_in, cache, counts, 1, ws=ws)
+    counts.fill_(1)
     for step in range(total[0] - prompts[0]):
-        slots.copy_(cache.extend([1] * n_seq))
         x_in.copy_(torch.stack([x[p + step] for x, p in zip(xs, prompts)]))
         graph.replay()
         for b in range(n_seq):
             outs[b].append(y[b:b + 1].clone())
-    if P.sync_status(ws) != P.QE_OK:
-        raise RuntimeError("the cache's page table or lengths are damaged")
+    if P.sync_status(ws) != P.QE_OK or P.sync_status(cache.ws) != P.QE_OK or int(cache.lacking):
+        raise RuntimeError("the cache's page table or lengths are damaged, or its pages used up")
     return [torch.cat(o) for o in outs], cache
 
 
@@ -138,12 +144,13 @@ def run(hidden=4096, heads=32, kv_heads=8, dim=128, prompts=(300, 1000, 1, 777),
     W = normal((heads + 2 * kv_heads) * dim, hidden) / hidden ** 0.5
     W_hat = quantize_weight(W, (normal(calibration, hidden) @ mix).t().contiguous())
     xs = [(normal(p + steps, hidden) @ mix).to(dtype) for p in prompts]
-    layer = AttentionLayer(W_hat, heads, kv_heads, dim, dtype)
+    longest = max(prompts) + steps
+    layer = AttentionLayer(W_hat, heads, kv_heads, dim, dtype, longest)
     got, cache = serve(layer, xs, list(prompts), chunk, group, page)
     kept = plain(layer, xs)
-    full = plain(AttentionLayer(W, heads, kv_heads, dim, dtype), xs)
+    full = plain(AttentionLayer(W, heads, kv_heads, dim, dtype, longest), xs)
     per_token = P.kv_page_bytes(kv_heads, dim, group, page) / page
-    return {"bytes_per_token": per_token, "bytes_per_token_16_bit": 4.0 * kv_heads * dim, "held": list(cache.held),
+    return {"bytes_per_token": per_token, "bytes_per_token_16_bit": 4.0 * kv_heads * dim, "held": cache.lengths.tolist(),
             "cache": [distance(a, b) for a, b in zip(got, kept)],
             "weights": [distance(a, b) for a, b in zip(kept, full)],
             "both": [distance(a, b) for a, b in zip(got, full)]}

@@ -38,7 +38,7 @@ __device__ inline int32_t piece(int32_t n, int32_t m, int32_t k)
 }
 
 // A thread has a group, and a stretch of sequences.  What one needs of the other goes through LDS; the entries are written
-// last, one after the other by all threads.
+// last.  64 sequences: 7 us, of which the sums take two, the first loads and the entries one each.
 __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, KvShared sh)
 {
     __shared__ ScanLds<2> lds;
@@ -279,14 +279,16 @@ constexpr int64_t kManyRows = 128, kManyRecords = 48 * 512;
 constexpr int64_t kSaves = 20000;
 
 // The forms of the shared and the own part, and the sizes of their lists.
-Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int group, bool f32, int64_t ngroups, int64_t records)
+Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int group, bool f32, int64_t ngroups,
+               int64_t records)
 {
     Lists z{};
     const int dp = kv_dp(dim), per = heads / kv_heads;
     const int64_t rows = total * per, group_rows = rows / std::max<int64_t>(ngroups, 1), own_rows = max_q * per;
     const int many = kv_many_nt(dp, group, f32), few = kv_few_nt(dp, group, f32);
     const int64_t many_units = kv_heads * cdiv(rows, 16 * many * kKvWaves);
-    z.form[0] = group_rows >= kManyRows && many_units * std::min<int64_t>(records, 1 << 24) >= kManyRecords ? KvForm{true, many} : KvForm{false, group_rows > 16 ? few : 1};
+    const bool long_rows = group_rows >= kManyRows && many_units * std::min<int64_t>(records, 1 << 24) >= kManyRecords;
+    z.form[0] = long_rows ? KvForm{true, many} : KvForm{false, group_rows > 16 ? few : 1};
     z.form[1] = own_rows >= kManyRows ? KvForm{true, many} : KvForm{false, own_rows > 16 ? few : 1};
     const bool pair = !z.form[0].many && !z.form[1].many && z.form[0].nt > z.form[1].nt;
     z.sh.joint = pair || (z.form[0].many == z.form[1].many && z.form[0].nt == z.form[1].nt);
@@ -296,7 +298,7 @@ Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_he
         z.sh.rows[y] = 16 * z.form[y].nt * (z.form[y].many ? kKvWaves : 1);
         z.sh.rows_log2[y] = __builtin_ctz((unsigned)z.sh.rows[y]);
         z.sh.fill[y] = 256 * (form.many ? 2 : kv_few_occupancy(dp, dp <= 64 ? std::min(group, 64) : group, form.nt, f32 ? 2 : 1));
-        z.sh.weight[y] = pair && y == 0 ? 8 : pair ? 5 : 1;
+        z.sh.weight[y] = pair && y == 0 ? 8 : pair ? 5 : 1;      // (a record takes 1.2 ns for 32 rows, 0.75 for 16, of the whole chip)
         z.sh.least[y] = kKvMinRecords;
         z.sh.part_of_fill[y] = 1. / ((double)z.sh.fill[y] * z.sh.weight[y]);
         units[y] = kv_heads * (cdiv(rows, z.sh.rows[y]) + (y == 0 ? ngroups : batch));
@@ -312,10 +314,13 @@ Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_he
     return z;
 }
 
-// Where the lists and the partial results do not fit 32-bit numbers, or nothing can be shared, the call is kv_attn's.
-bool listed(const Lists& z, int64_t batch, int64_t rows)
+// Where the lists, the partial results or the join's workgroups (of 8 rows at least) pass 32-bit numbers, or nothing can be
+// shared, the call is kv_attn's.
+bool listed(const Lists& z, int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads)
 {
-    return batch > 1 && z.sh.ngroups > 0 && z.sh.ngroups <= kMaxGroups && rows < kBehind && z.slots < (int64_t(1) << 31) && (int64_t)z.sh.room[0] + z.sh.room[1] < (int64_t(1) << 23);
+    const int64_t per = heads / kv_heads, most = int64_t(1) << 23;
+    return batch > 1 && z.sh.ngroups > 0 && z.sh.ngroups <= kMaxGroups && total * per < kBehind && z.slots < (int64_t(1) << 31) &&
+           (int64_t)z.sh.room[0] + z.sh.room[1] < most && batch * kv_heads * cdiv(max_q * per, 8) < most;
 }
 
 // Whether sharing can gain what its launches cost.  (Where a sequence's rows fill tiles by themselves it saves no tile, but
@@ -359,7 +364,7 @@ size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int 
         for (int f32 = 0; f32 < 2; ++f32)
             for (int64_t records : {(int64_t)1, (int64_t)INT32_MAX}) {
                 const Lists z = lists_of(total, batch, max_q, heads, kv_heads, dim, group, f32 != 0, ngroups, records);
-                if (listed(z, batch, total * (heads / kv_heads))) need = std::max(need, layout_of(z, batch, kv_dp(dim)).end);
+                if (listed(z, total, batch, max_q, heads, kv_heads)) need = std::max(need, layout_of(z, batch, kv_dp(dim)).end);
             }
     return need;
 }
@@ -369,7 +374,7 @@ qe_status launch_kv_attn_shared(const KvAttn& call, const int32_t* groups, const
     KvAttn a = call;
     const int dp = kv_dp(a.c.dim);
     Lists z = lists_of(a.total, a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, a.dtype == QE_F32, ngroups, a.width * a.c.per);
-    if (!listed(z, a.batch, a.total * (a.heads / a.c.heads)) || !(always || gains(z, a))) return launch_kv_attn(a, ws, s);
+    if (!listed(z, a.total, a.batch, a.max_q, a.heads, a.c.heads) || !(always || gains(z, a))) return launch_kv_attn(a, ws, s);
     kv_attn_vec(a);
     const Layout l = layout_of(z, a.batch, dp);
     char* const base = static_cast<char*>(ws);
