@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
     __shared__ KvSequence seq[kScanThreads];              // (of more sequences than threads: in memory alone)
     __shared__ int wrong, end_b;
     const int tid = threadIdx.x, threads = blockDim.x, per = a.heads / a.c.heads;
-    const int64_t room = min(a.width * (int64_t)a.c.per * kKvTok, (int64_t)0x7fffffff);
+    const int64_t room = a.width * (int64_t)a.c.per * kKvTok;
     const int64_t run = (a.batch + threads - 1) / threads, b0 = min((int64_t)tid * run, (int64_t)a.batch), b1 = min(b0 + run, (int64_t)a.batch);
     const int ngroups = sh.ngroups;
     int32_t shared_pages = 0;
@@ -67,12 +67,18 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
         active[tid] = 0;
         tokens[tid] = 0;
     }
-    // a sequence's rows and length
-    auto sequence = [&](int64_t b, bool report) {
+    // the thread's sequences: one in registers, more in memory
+    KvSequence mine = {};
+    auto get = [&](int64_t b) { return run == 1 ? mine : sh.seq[b]; };
+    auto put = [&](int64_t b, const KvSequence& s) {
+        if (run == 1) mine = s;
+        else sh.seq[b] = s;
+    };
+    for (int64_t b = b0; b < b1; ++b) {
         KvSequence s = {};
         int64_t at = b * a.max_q, nq = a.max_q;
         const int64_t len = a.lengths[b];
-        bool bad = len < 0 || len > a.width * (int64_t)a.c.per * kKvTok;
+        bool bad = len < 0 || len > room;
         if (a.q_start) {
             at = a.q_start[b];
             nq = (int64_t)a.q_start[b + 1] - at;
@@ -82,25 +88,20 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
                 nq = -1;
             }
         }
-        if (bad && report) set_status(a.status, QE_ERR_ARG);
+        if (bad) set_status(a.status, QE_ERR_ARG);
         s.first = (int32_t)at;
         s.nq = (int32_t)nq;
         s.len = (int32_t)max((int64_t)0, min(len, room));
-        s.group = -1;
-        return s;
-    };
-    KvSequence s = {};
-    if (b0 < b1) s = sequence(b0, true);
+        s.tiles = nq > 0 ? (s.nq * per + sh.rows[1] - 1) >> sh.rows_log2[1] : 0;
+        put(b, s);
+    }
     __syncthreads();
     if (tid < ngroups && (bound[tid] < 0 || bound[tid + 1] < bound[tid] || bound[tid + 1] > a.batch)) wrong = 1;
     // what all queries of a group see
-    auto group_of = [&](int64_t b) {
-        if (b < bound[0] || b >= bound[ngroups]) return -1;
-        return (int)last_at_most(bound, ngroups, b);
-    };
     for (int64_t b = b0; b < b1; ++b) {
-        if (b > b0) s = sequence(b, true);
-        const int g = group_of(b);
+        KvSequence s = get(b);
+        const int g = s.group = b < bound[0] || b >= bound[ngroups] ? -1 : (int)last_at_most(bound, ngroups, b);
+        put(b, s);
         if (g < 0) continue;
         if (b == bound[g]) first[g] = s.first;
         if (s.nq < 0) atomicMin(&sees[g], 0);            // (its rows are not where the group's are)
@@ -130,20 +131,16 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
     // that several groups claim, with a bad q_start between them)
     int64_t all[2], at[2], own[2];
     int32_t size[2], items_a;
-    bool share = !none;
+    bool share = !none;                                  // (gr.records is 0 where none)
+    auto own_records = [&](const KvSequence& s) { return max(0, div_up(s.len, kKvTok) - (s.group >= 0 ? records[s.group] : 0)); };
     for (;;) {
-        auto own_records = [&](const KvSequence& q) { return max(0, div_up(q.len, kKvTok) - (q.group >= 0 ? records[q.group] : 0)); };
-        auto place = [&](KvSequence& q, int64_t b) {
-            const int g = share ? group_of(b) : -1;
-            q.group = g >= 0 && records[g] ? g : -1;
-            q.tiles = q.nq > 0 ? (q.nq * per + sh.rows[1] - 1) >> sh.rows_log2[1] : 0;
-        };
-        at[0] = share ? (int64_t)gr.tiles * gr.records : 0;
+        at[0] = (int64_t)gr.tiles * gr.records;
         at[1] = 0;
         for (int64_t b = b0; b < b1; ++b) {
-            if (run > 1) s = sequence(b, false);
-            place(s, b);
+            KvSequence s = get(b);
+            if (s.group >= 0 && !(share && records[s.group])) s.group = -1;
             at[1] += (int64_t)s.tiles * own_records(s);
+            put(b, s);
         }
         scan_add(at, lds, all);
 #pragma unroll
@@ -151,16 +148,14 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
             const int64_t work = sh.joint ? all[0] * sh.weight[0] + all[1] * sh.weight[1] : all[y] * sh.weight[y];
             size[y] = max(sh.least[y], (int32_t)fmin(2147483647., ceil((double)(work * a.c.heads) * sh.part_of_fill[y])));
         }
-        gr.splits = share && gr.records ? pieces(gr.records, size[0]) : 0;
+        gr.splits = pieces(gr.records, size[0]);
         own[0] = at[0] = (int64_t)gr.tiles * gr.splits * a.c.heads;
         at[1] = 0;
         for (int64_t b = b0; b < b1; ++b) {
-            if (run > 1) {
-                s = sequence(b, false);
-                place(s, b);
-            }
+            KvSequence s = get(b);
             s.splits = s.tiles ? pieces(own_records(s), size[1]) : 0;
             at[1] += (int64_t)s.tiles * s.splits * a.c.heads;
+            put(b, s);
         }
         own[1] = at[1];
         scan_add(at, lds2, all);
@@ -178,16 +173,9 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
     }
     int64_t next = at[1] - own[1];
     for (int64_t b = b0; b < b1; ++b) {
-        if (run > 1) {
-            s = sequence(b, false);
-            const int g = share ? group_of(b) : -1;
-            s.group = g >= 0 && records[g] ? g : -1;
-            s.tiles = s.nq > 0 ? (s.nq * per + sh.rows[1] - 1) >> sh.rows_log2[1] : 0;
-            s.splits = s.tiles ? pieces(max(0, div_up(s.len, kKvTok) - (s.group >= 0 ? records[s.group] : 0)), size[1]) : 0;
-        }
-        const int64_t n = (int64_t)s.tiles * s.splits * a.c.heads;
+        KvSequence s = get(b);
         s.item = (int32_t)min(next, (int64_t)sh.room[1]);
-        next += n;
+        next += (int64_t)s.tiles * s.splits * a.c.heads;
         if (next > sh.room[1]) {
             // (rows that several sequences claim, with a bad q_start between them: the last of these get nothing)
             set_status(a.status, QE_ERR_ARG);
@@ -195,8 +183,8 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
             s.nq = -1;
             s.splits = 0;
         }
+        put(b, s);
         if (run == 1) seq[tid] = s;
-        else sh.seq[b] = s;
     }
     __syncthreads();
     const int32_t items_b = (int32_t)min(all[1], (int64_t)end_b);
@@ -258,7 +246,7 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
     }
     // (what the join reads; before the barrier, everything would wait for these stores)
     if (tid < ngroups) sh.group[tid] = gr;
-    if (run == 1 && b0 < b1) sh.seq[b0] = s;
+    if (run == 1 && b0 < b1) sh.seq[b0] = mine;
 }
 
 struct Lists {
