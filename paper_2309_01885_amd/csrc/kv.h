@@ -125,10 +125,8 @@ struct KvShared {
     int32_t ngroups;
     int32_t rows[2], rows_log2[2];         // of the two lists: rows of a tile,
     int32_t fill[2], least[2];             // entries that fill the chip, records of an entry at least
-    int32_t weight[2];                     // joint: what a record of a tile costs, relative to each other
-    double part_of_fill[2];                // 1 / (fill weight)
     int32_t room[2];                       // entries that a list holds
-    bool joint;                            // both lists in one launch (equal fill)
+    bool joint, pair;                      // both lists in one launch (equal fill); with tiles of 32 rows and of 16
     KvGroup* group;
     KvSequence* seq;
     KvItem* items[2];

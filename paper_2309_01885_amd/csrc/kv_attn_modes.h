@@ -145,7 +145,7 @@ template <int DP> void kv_listed_width(const KvAttn& a, const KvPlan& plan, cons
 {
     KvPlan p = plan;
     const dim3 all((unsigned)(sh.room[0] + sh.room[1]));
-    if (sh.joint && shared.nt != own.nt) {
+    if (sh.pair) {
         kv_dispatch_group<DP>(a.group, [&](auto shape) {
             constexpr int G = decltype(shape)::GROUP;
             if constexpr (kv_few_nt(DP, G, false) == 2) hipLaunchKernelGGL((kv_pair_kernel<DP, G>), all, dim3(256), 0, s, a, p);

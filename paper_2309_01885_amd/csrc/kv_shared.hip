@@ -145,8 +145,15 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
         scan_add(at, lds, all);
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-            const int64_t work = sh.joint ? all[0] * sh.weight[0] + all[1] * sh.weight[1] : all[y] * sh.weight[y];
-            size[y] = max(sh.least[y], (int32_t)fmin(2147483647., ceil((double)(work * a.c.heads) * sh.part_of_fill[y])));
+            // In one launch, long shared entries start first and short own ones fill the rest of the chip: a record of 32 shared
+            // rows then counts as 4 of 5 parts of a record of 16 own ones (both wait more than they compute), as 8 where the own part
+            // is a small rest.  us with 4 / 8, one query each of 32 heads on 8 of 128: 64 sequences behind 8192 tokens (1.6 times
+            // the own records) 50.8 / 54.2, 16 behind 4096 (0.8) 24.4 / 25.4, 8 behind 16384 (3.2) 30.9 / 32.9, 64 behind 32768
+            // (6.4) 107 / 96.
+            const int64_t shared_weight = !sh.pair ? 5 : all[0] > 5 * all[1] ? 8 : 4;
+            const int64_t work = sh.joint ? all[0] * shared_weight + all[1] * 5 : 5 * all[y];
+            const double by = 1. / (double)(sh.fill[y] * (sh.joint && y == 0 ? shared_weight : 5));
+            size[y] = max(sh.least[y], (int32_t)fmin(2147483647., ceil((double)(work * a.c.heads) * by)));
         }
         gr.splits = pieces(gr.records, size[0]);
         own[0] = at[0] = (int64_t)gr.tiles * gr.splits * a.c.heads;
@@ -278,7 +285,7 @@ Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_he
     const bool long_rows = group_rows >= kManyRows && many_units * std::min<int64_t>(records, 1 << 24) >= kManyRecords;
     z.form[0] = long_rows ? KvForm{true, many} : KvForm{false, group_rows > 16 ? few : 1};
     z.form[1] = own_rows >= kManyRows ? KvForm{true, many} : KvForm{false, own_rows > 16 ? few : 1};
-    const bool pair = !z.form[0].many && !z.form[1].many && z.form[0].nt > z.form[1].nt;
+    const bool pair = z.sh.pair = !z.form[0].many && !z.form[1].many && z.form[0].nt > z.form[1].nt;
     z.sh.joint = pair || (z.form[0].many == z.form[1].many && z.form[0].nt == z.form[1].nt);
     int64_t units[2];
     for (int y = 0; y < 2; ++y) {
@@ -286,9 +293,7 @@ Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_he
         z.sh.rows[y] = 16 * z.form[y].nt * (z.form[y].many ? kKvWaves : 1);
         z.sh.rows_log2[y] = __builtin_ctz((unsigned)z.sh.rows[y]);
         z.sh.fill[y] = 256 * (form.many ? 2 : kv_few_occupancy(dp, dp <= 64 ? std::min(group, 64) : group, form.nt, f32 ? 2 : 1));
-        z.sh.weight[y] = pair && y == 0 ? 8 : pair ? 5 : 1;      // (a record takes 1.2 ns for 32 rows, 0.75 for 16, of the whole chip)
         z.sh.least[y] = kKvMinRecords;
-        z.sh.part_of_fill[y] = 1. / ((double)z.sh.fill[y] * z.sh.weight[y]);
         units[y] = kv_heads * (cdiv(rows, z.sh.rows[y]) + (y == 0 ? ngroups : batch));
     }
     units[1] = std::min(units[1], kv_heads * batch * cdiv(own_rows, z.sh.rows[1]));
