@@ -8,6 +8,12 @@
 // A channel's partner in the rotation comes through the row's own stretch of LDS, where any number of rotated channels is
 // right.  The first workgroups take 32 tokens' keys and values of a head each, as the plain write does (a thread
 // has 8 channels of a row), the others queries.
+//
+// What bounds it: 16384 tokens of 32 + 8 + 8 heads of 128 in bf16, all channels rotated, take 84 us for 371 MB,
+// 4.4 TB/s (a plain copy moves 4.9 to 5.1), with the vector units 65 % busy; without norm and rotation 76 us.  With the
+// queries as the keys are, 8 channels a thread and a workgroup per 32 rows, the norm's sum through LDS and its weights
+// and cosines a word a load, it took 234; wide loads and sums inside the vector units made it 149.  A few tokens
+// cost their launch and three dependent loads: 5.6 us up to 64 tokens, 8 at 1024.
 #include "kv_codes.h"
 
 namespace qe {
@@ -352,9 +358,11 @@ qe_status append_typed(const void* Q, const void* K, const void* V, void* out, K
     a.vec_o = vec_ok(out, a.ot, a.oh, sizeof(T));
     a.kv_wgs = cdiv(a.tokens, kKvTok) * c.heads;
     kv_dispatch(c.dim, group, [&](auto shape) {
-        // (as many heads a workgroup as leave four of them for a compute unit)
+        // Heads that a workgroup goes through: as many as leave two workgroups for a compute unit, four at most.  32 heads of
+        // 128, us with 1, 2, 4 and 8: 256 tokens 6.2, 6.2, 6.2, 8.9; 1024 8.7, 7.8, 8.0, 11.5; 2048 15.6, 13.6, 13.1,
+        // 14.8; 16384 105, 88, 84, 87.
         const int64_t chunks = cdiv(a.tokens, 512 / kOctets<shape.DP>);
-        a.head_run = (int)std::max<int64_t>(1, std::min<int64_t>(8, chunks * a.heads / 1024));
+        a.head_run = (int)std::max<int64_t>(1, std::min<int64_t>(4, chunks * a.heads / 512));
         a.head_groups = (int)cdiv(a.heads, a.head_run);
         const dim3 grid = grid_xy(a.kv_wgs + chunks * a.head_groups, 256);
         hipLaunchKernelGGL((kv_append_kernel<T, shape.DP, shape.GROUP>), grid, dim3(256), 0, s, (const T*)Q, (const T*)K, (const T*)V,

@@ -49,6 +49,10 @@ struct KvPlan {
 
 // What a kernel's workgroups work on: every (unit, split) of a call; the same where first tokens stay visible beside a
 // window; or the entries of two lists, whose results are always joined by another launch.
+// First tokens cost their records alone: a unit's records are the first tokens' and the window's, counted through, so
+// that splits and both forms are the plain call's.  2048 queries of 32 heads on 8 of 128 channels at the end of 32768 tokens,
+// a window of 4096 and 128 first tokens: 193 us, 733 TFLOP/s, the rate of a plain chunk; one token of 64 sequences, 71 heads
+// on one of 64 channels, 4000 and 100 tokens: 31 us, of which 11 are what any call with a join takes; vector units 40 % busy.
 enum KvMode { kKvPlain, kKvSinks, kKvListed };
 
 // What a workgroup works on; the join recomputes it.
