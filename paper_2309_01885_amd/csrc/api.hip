@@ -554,7 +554,7 @@ qe_status qe_kv_attn_sinks(const void* Q, int dtype, int64_t total, int heads, i
 size_t qe_kv_attn_shared_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups)
 {
     if (ngroups < 0 || ngroups > (1 << 20) || qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim) == 0) return 0;
-    return kv_attn_shared_ws_bytes(total, batch, std::min(max_q, total), heads, kv_heads, dim, ngroups);
+    return kv_attn_shared_ws_bytes(total, batch, std::min(max_q, total), heads, kv_heads, dim, ngroups, false);
 }
 
 qe_status qe_kv_attn_shared(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
@@ -576,8 +576,14 @@ qe_status qe_kv_attn_shared(const void* Q, int dtype, int64_t total, int heads, 
     return launch_kv_attn_shared(a, groups, shared, ngroups, ws, false, as_stream(stream));
 }
 
-// qe_kv_attn_shared by its lists also where kv_attn itself would be faster: not part of the ABI, for tests of the lists at
-// small sizes.
+// qe_kv_attn_shared by its lists also where kv_attn itself would be faster, and its workspace: not part of the ABI, for tests
+// of the lists at small sizes.
+size_t qei_kv_attn_listed_workspace_size(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups)
+{
+    if (ngroups < 0 || ngroups > (1 << 20) || qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim) == 0) return 0;
+    return kv_attn_shared_ws_bytes(total, batch, std::min(max_q, total), heads, kv_heads, dim, ngroups, true);
+}
+
 qe_status qei_kv_attn_listed(const void* Q, int dtype, int64_t total, int heads, int dim, int64_t q_stride,
                              int64_t q_head_stride, const int32_t* q_start, int64_t batch, int64_t max_q,
                             const void* pages, int64_t num_pages, int page, int kv_heads, int group,
@@ -593,7 +599,7 @@ qe_status qei_kv_attn_listed(const void* Q, int dtype, int64_t total, int heads,
                                    o_head_stride, lse, ws);
     if (st != QE_OK || empty) return st;
     if (ngroups > 0 && (!groups || !shared)) return QE_ERR_ARG;
-    if (!ws || ws_bytes < qe_kv_attn_shared_workspace_size(total, batch, max_q, heads, kv_heads, dim, ngroups)) return QE_ERR_WORKSPACE;
+    if (!ws || ws_bytes < qei_kv_attn_listed_workspace_size(total, batch, max_q, heads, kv_heads, dim, ngroups)) return QE_ERR_WORKSPACE;
     return launch_kv_attn_shared(a, groups, shared, ngroups, ws, true, as_stream(stream));
 }
 

@@ -355,15 +355,30 @@ Layout layout_of(const Lists& z, int64_t batch, int dp)
 
 }  // namespace
 
-size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups)
+// (always: of the lists, also where kv_attn itself would be taken whatever the table's width.)
+size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups, bool always)
 {
     size_t need = kv_attn_ws_bytes(batch, max_q, heads, kv_heads, dim);
+    KvAttn a{};
+    a.total = total;
+    a.batch = (int32_t)std::min<int64_t>(batch, INT32_MAX);
+    a.max_q = max_q;
+    a.heads = heads;
+    a.c.heads = kv_heads;
+    a.c.dim = dim;
+    a.c.per = 1;
+    a.width = INT32_MAX;                                 // (a wider table makes sharing gain more)
     for (int group : {32, 64, 128})
-        for (int f32 = 0; f32 < 2; ++f32)
-            for (int64_t records : {(int64_t)1, (int64_t)INT32_MAX}) {
+        for (int f32 = 0; f32 < 2; ++f32) {
+            a.group = group;
+            a.dtype = f32 ? QE_F32 : QE_BF16;
+            for (int64_t records : {(int64_t)1, a.width}) {
                 const Lists z = lists_of(total, batch, max_q, heads, kv_heads, dim, group, f32 != 0, ngroups, records);
-                if (listed(z, total, batch, max_q, heads, kv_heads)) need = std::max(need, layout_of(z, batch, kv_dp(dim)).end);
+                if (!listed(z, total, batch, max_q, heads, kv_heads)) continue;
+                const Lists wide = lists_of(total, batch, max_q, heads, kv_heads, dim, group, f32 != 0, ngroups, a.width);
+                if (always || gains(wide, a)) need = std::max(need, layout_of(z, batch, kv_dp(dim)).end);
             }
+        }
     return need;
 }
 

@@ -450,6 +450,13 @@ def _flat(t: Optional[torch.Tensor], name: str, dtype, dev: int, numel: Optional
     return t.data_ptr()
 
 
+def _gpu(t: torch.Tensor, name: str) -> int:
+    """Index of a device tensor's GPU."""
+    if not t.is_cuda:
+        _bad(name, t, "a device tensor")
+    return t.get_device()
+
+
 def _raw_stream(dev: int, stream):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
@@ -537,9 +544,7 @@ def kv_extend(counts: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, 
     if table.dim() != 2:
         _bad("table", table, "sequences x pages")
     batch, width = table.shape
-    dev = table.get_device()
-    if dev < 0:
-        raise ValueError("table must be a device tensor")
+    dev = _gpu(table, "table")
     if slots is None:
         slots = _on(stream, lambda: torch.empty(total, dtype=torch.int64, device=table.device))
     if positions is None:

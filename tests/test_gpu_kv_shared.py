@@ -19,9 +19,11 @@ class Always:
 
     def __init__(self, lib):
         self.lib = lib
-        self.qe_kv_attn_shared = lib.qei_kv_attn_listed
-        self.qe_kv_attn_shared.argtypes = lib.qe_kv_attn_shared.argtypes
-        self.qe_kv_attn_shared.restype = lib.qe_kv_attn_shared.restype
+        for public, own in (("qe_kv_attn_shared", "qei_kv_attn_listed"),
+                            ("qe_kv_attn_shared_workspace_size", "qei_kv_attn_listed_workspace_size")):
+            call = getattr(lib, own)
+            call.argtypes, call.restype = getattr(lib, public).argtypes, getattr(lib, public).restype
+            setattr(self, public, call)
 
     def __getattr__(self, name):
         return getattr(self.lib, name)

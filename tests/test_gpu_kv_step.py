@@ -380,3 +380,62 @@ def test_append_refusals(qe):
         qe.kv_append(q, k.half(), k, slots, pages, **ok)
     with pytest.raises(ValueError):
         qe.kv_append(q, k, k, slots.int(), pages, **ok)
+
+
+def test_extend_refusals(qe):
+    p = Pool([5, 50], 32, 4, 6)
+    counts = dev(i32([1, 1]))
+    args = (p.dtable, p.dlengths, p.dfree, p.dcount, 32, 2)
+    for bad in ((counts.long(),) + args, (counts[:1],) + args, (counts.cpu(),) + args, (counts, p.dtable.cpu()) + args[1:],
+                (counts, p.dtable[:, ::2]) + args[1:], (counts, p.dtable.flatten()) + args[1:], (counts, p.dtable, p.dlengths.long()) + args[2:],
+                (counts, p.dtable, p.dlengths, p.dfree.long()) + args[3:], (counts,) + args[:3] + (p.dfree,) + args[4:]):
+        with pytest.raises(ValueError):
+            qe.kv_extend(*bad)
+    for more in (dict(keep=counts.long()), dict(slots=counts), dict(positions=counts[:1]), dict(q_start=counts), dict(lacking=counts)):
+        with pytest.raises(ValueError):
+            qe.kv_extend(counts, *args, **more)
+    for bad in ((48, 2), (0, 2), (32, -1)):
+        with pytest.raises((qe.QEError, RuntimeError)):
+            qe.kv_extend(counts, *args[:4], *bad)
+    with pytest.raises(qe.QEError):
+        qe.kv_extend(counts, *args, ws=torch.zeros(256, dtype=torch.uint8, device="cuda"))
+    assert np.array_equal(host(p.dlengths), p.lengths) and np.array_equal(host(p.dtable), p.table)
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_append_on_a_stream(qe, graph):
+    """A call on a stream of its own, and a recorded one whose tokens change between the replays."""
+    tokens, dtype = 40, "bf16"
+    q, k, v = (draw((tokens, h, 64), h, dtype).cuda() for h in (4, 2, 3))
+    v = v[:, :2]
+    cos, sin = tables(100, 64)
+    w = np.linspace(0.5, 2.0, 64, dtype=np.float32)
+    pages = qe.kv_pages(3, 2, 64, 32, 32)
+    slots, positions = dev(np.arange(tokens) + 9), dev(i32(np.arange(tokens)))
+    d = [dev(x) for x in (cos, sin, w)]
+    call = lambda s=None: qe.kv_append(q, k, v, slots, pages, group=32, positions=positions, cos=d[0], sin=d[1], q_weight=d[2], k_weight=d[2],  # noqa: E731
+                                       stream=s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = call(side)
+    torch.cuda.current_stream().wait_stream(side)
+    out.record_stream(torch.cuda.current_stream())
+    if graph:
+        rec = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(rec):
+            out = call()
+    for n in range(3 if graph else 1):
+        if graph:
+            q.copy_(draw(q.shape, 50 + n, dtype).cuda())
+            positions.copy_(dev(i32((np.arange(tokens) * 7 + n) % 100 - (np.arange(tokens) == n))))
+            rec.replay()
+            torch.cuda.synchronize()
+        pos = host(positions)
+        there = torch.from_numpy(pos >= 0)
+        want = rounded(okv.norm_rotate(f64(q), w, 1e-6, pos, cos, sin, False), dtype)
+        assert np.array_equal(bits(out.cpu()[there]), bits(want[there]))
+        if n == 0:
+            expect = np.zeros_like(host(pages))
+        okv.write(expect, np.where(pos < 0, -1, np.arange(tokens) + 9), okv.norm_rotate(f64(k), w, 1e-6, pos, cos, sin, False), f64(v), 32)
+        if not graph:
+            assert np.array_equal(host(pages), expect)
