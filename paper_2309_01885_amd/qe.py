@@ -545,22 +545,26 @@ def kv_extend(counts: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, 
         _bad("table", table, "sequences x pages")
     batch, width = table.shape
     dev = _gpu(table, "table")
-    if slots is None:
-        slots = _on(stream, lambda: torch.empty(total, dtype=torch.int64, device=table.device))
-    if positions is None:
-        positions = _on(stream, lambda: torch.empty(total, dtype=torch.int32, device=table.device))
-    if q_start is None:
-        q_start = _on(stream, lambda: torch.empty(batch + 1, dtype=torch.int32, device=table.device))
+    i32 = torch.int32
+
+    def made(t, name, dtype, n):
+        """An output, given (checked) or new, and its pointer."""
+        if t is None:
+            t = _on(stream, lambda: table.new_empty(n, dtype=dtype))
+            return t, t.data_ptr()
+        return t, _flat(t, name, dtype, dev, n)
+
+    slots, to_slots = made(slots, "slots", torch.int64, total)
+    positions, to_positions = made(positions, "positions", i32, total)
+    q_start, to_start = made(q_start, "q_start", i32, batch + 1)
     if ws is None:
         ws = _on(stream, lambda: workspace(kv_extend_workspace_size(batch), table.device))
-    i32 = torch.int32
     code = load().qe_kv_extend(_flat(counts, "counts", i32, dev, batch), batch, _flat(table, "table", i32, dev), width,
-                               _flat(lengths, "lengths", i32, dev, batch), _flat(keep, "keep", i32, dev, batch),
+                               _flat(lengths, "lengths", i32, dev, batch), None if keep is None else _flat(keep, "keep", i32, dev, batch),
                                _flat(free, "free", i32, dev), free.numel(), _flat(free_count, "free_count", i32, dev, 1),
-                               page, total, _flat(slots, "slots", torch.int64, dev, total),
-                               _flat(positions, "positions", i32, dev, total), _flat(q_start, "q_start", i32, dev, batch + 1),
-                               _flat(lacking, "lacking", i32, dev, 1), _flat(ws, "ws", torch.uint8, dev), ws.numel(),
-                               _raw_stream(dev, stream))
+                               page, total, to_slots, to_positions, to_start,
+                               None if lacking is None else _flat(lacking, "lacking", i32, dev, 1), _flat(ws, "ws", torch.uint8, dev),
+                               ws.numel(), _raw_stream(dev, stream))
     if code:
         raise QEError(code, "qe_kv_extend")
     if check:
@@ -597,7 +601,7 @@ def kv_append(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Te
             raise ValueError("a rotation needs positions")
         rows, half = cos.shape
     if out is None:
-        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
+        out = _on(stream, lambda: torch.empty_like(Q))
     qt, qh = _heads(Q, "Q", shape, dtype, dev)
     kt, kh = _heads(K, "K", (n, kv, dim), dtype, dev)
     vt, vh = _heads(V, "V", (n, kv, dim), dtype, dev)
@@ -618,15 +622,17 @@ def kv_attn_workspace_size(total: int, batch: int, max_q: int, heads: int, kv_he
     return int(load().qe_kv_attn_workspace_size(total, batch, max_q, heads, kv_heads, dim))
 
 
-def _attn_queries(Q, pages, table, group, q_start, max_q):
-    """What kv_attn and kv_attn_shared check first: (total, heads, dim, batch, width, max_q, cache)."""
-    if len(Q.shape) != 3 or Q.dtype not in _DTYPES:
+def _attn(Q, pages, table, lengths, group, q_start, max_q, scale, causal, window, sinks, slopes, out, lse, ws, check, stream, groups,
+          shared):
+    """kv_attn, and kv_attn_shared where `shared` is given."""
+    shape, dtype = Q.shape, Q.dtype
+    if len(shape) != 3 or dtype not in _DTYPES:
         _bad("Q", Q, "total x heads x dim in float32, float16 or bfloat16")
     if table.dim() != 2:
         _bad("table", table, "sequences x pages")
-    total, heads, dim = Q.shape
+    total, heads, dim = shape
     batch, width = table.shape
-    cache = _pages(pages, dim, group)
+    num, page, kv, dev = _pages(pages, dim, group)
     if q_start is None:
         if max_q is None:
             max_q = total // batch if batch else 0
@@ -634,7 +640,38 @@ def _attn_queries(Q, pages, table, group, q_start, max_q):
             raise ValueError(f"{total} queries are not {max_q} for each of {batch} sequences: give q_start")
     elif max_q is None:
         raise ValueError("q_start needs max_q, the largest number of queries of a sequence")
-    return total, heads, dim, batch, width, max_q, cache
+    shape = (total, heads, dim)
+    if not -0x80000000 <= window <= 0x7fffffff:      # (a C int would take its low bits: 2^32 as no window)
+        window = 0x7fffffff if window > 0 else -1
+    if out is None:
+        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
+    qt, qh = _heads(Q, "Q", shape, dtype, dev)
+    ot, oh = _heads(out, "out", shape, dtype, dev)
+    if ws is None:
+        need = (kv_attn_workspace_size(total, batch, max_q, heads, kv, dim) if shared is None else
+                kv_attn_shared_workspace_size(total, batch, max_q, heads, kv, dim, shared.numel()))
+        ws = _on(stream, lambda: workspace(need, pages.device))
+    queries = (Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
+               None if q_start is None else _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
+               num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
+               _flat(lengths, "lengths", torch.int32, dev, batch))
+    scale = dim ** -0.5 if scale is None else scale
+    rest = (None if slopes is None else _flat(slopes, "slopes", torch.float32, dev, heads), out.data_ptr(), ot, oh,
+            None if lse is None else _flat(lse, "lse", torch.float32, dev, total * heads),
+            _flat(ws, "ws", torch.uint8, dev), ws.numel(), _raw_stream(dev, stream))
+    if shared is not None:
+        code = load().qe_kv_attn_shared(*queries, _flat(groups, "groups", torch.int32, dev, shared.numel() + 1),
+                                        _flat(shared, "shared", torch.int32, dev), shared.numel(), scale, 1 if causal else 0, *rest)
+    elif sinks:
+        sinks = min(max(sinks, -1), 0x7fffffff)
+        code = load().qe_kv_attn_sinks(*queries, scale, 1 if causal else 0, window, sinks, *rest)
+    else:
+        code = load().qe_kv_attn(*queries, scale, 1 if causal else 0, window, *rest)
+    if code:
+        raise QEError(code, "qe_kv_attn" if shared is None else "qe_kv_attn_shared")
+    if check:
+        _finish(ws, check, "qe_kv_attn" if shared is None else "qe_kv_attn_shared", stream)
+    return out
 
 
 def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
@@ -654,34 +691,8 @@ def kv_attn(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: 
     a tensor of `stream`; rows of it that are no sequence's are not written.  The kernels cut their work for
     sequences that fill the table, so a table much wider than they are costs time.  No gradient:
     the output has no graph."""
-    total, heads, dim, batch, width, max_q, (num, page, kv, dev) = _attn_queries(Q, pages, table, group, q_start, max_q)
-    shape, dtype = (total, heads, dim), Q.dtype
-    if not -0x80000000 <= window <= 0x7fffffff:      # (a C int would take its low bits: 2^32 as no window)
-        window = 0x7fffffff if window > 0 else -1
-    if not -0x80000000 <= sinks <= 0x7fffffff:
-        sinks = 0x7fffffff if sinks > 0 else -1
-    if out is None:
-        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
-    qt, qh = _heads(Q, "Q", shape, dtype, dev)
-    ot, oh = _heads(out, "out", shape, dtype, dev)
-    if ws is None:
-        need = kv_attn_workspace_size(total, batch, max_q, heads, kv, dim)
-        ws = _on(stream, lambda: workspace(need, pages.device))
-    masks = (1 if causal else 0, window, sinks) if sinks else (1 if causal else 0, window)
-    code = (load().qe_kv_attn_sinks if sinks else load().qe_kv_attn)(
-        Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
-        _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
-        num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
-        _flat(lengths, "lengths", torch.int32, dev, batch),
-        dim ** -0.5 if scale is None else scale, *masks,
-        _flat(slopes, "slopes", torch.float32, dev, heads), out.data_ptr(), ot, oh,
-        _flat(lse, "lse", torch.float32, dev, total * heads),
-        _flat(ws, "ws", torch.uint8, dev), ws.numel(), _raw_stream(dev, stream))
-    if code:
-        raise QEError(code, "qe_kv_attn")
-    if check:
-        _finish(ws, check, "qe_kv_attn", stream)
-    return out
+    return _attn(Q, pages, table, lengths, group, q_start, max_q, scale, causal, window, sinks, slopes, out, lse, ws, check, stream, None,
+                 None)
 
 
 def kv_attn_sinks(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, window: int,
@@ -706,27 +717,4 @@ def kv_attn_shared(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, le
     The sequences groups[g] .. groups[g + 1] - 1 (int32, groups + 1 ascending entries) have the same first shared[g]
     (int32) entries in their rows of table; a row's lengths count the shared tokens.  The result is kv_attn's up to
     the rounding of sums.  The other arguments are kv_attn's; kv_attn_shared_workspace_size gives the workspace."""
-    total, heads, dim, batch, width, max_q, (num, page, kv, dev) = _attn_queries(Q, pages, table, group, q_start, max_q)
-    shape, dtype = (total, heads, dim), Q.dtype
-    n = shared.numel()
-    if out is None:
-        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
-    qt, qh = _heads(Q, "Q", shape, dtype, dev)
-    ot, oh = _heads(out, "out", shape, dtype, dev)
-    if ws is None:
-        need = kv_attn_shared_workspace_size(total, batch, max_q, heads, kv, dim, n)
-        ws = _on(stream, lambda: workspace(need, pages.device))
-    code = load().qe_kv_attn_shared(
-        Q.data_ptr(), _DTYPES[dtype], total, heads, dim, qt, qh,
-        _flat(q_start, "q_start", torch.int32, dev, batch + 1), batch, max_q, pages.data_ptr(),
-        num, page, kv, group, _flat(table, "table", torch.int32, dev), width,
-        _flat(lengths, "lengths", torch.int32, dev, batch), _flat(groups, "groups", torch.int32, dev, n + 1),
-        _flat(shared, "shared", torch.int32, dev), n, dim ** -0.5 if scale is None else scale, 1 if causal else 0,
-        _flat(slopes, "slopes", torch.float32, dev, heads), out.data_ptr(), ot, oh,
-        _flat(lse, "lse", torch.float32, dev, total * heads),
-        _flat(ws, "ws", torch.uint8, dev), ws.numel(), _raw_stream(dev, stream))
-    if code:
-        raise QEError(code, "qe_kv_attn_shared")
-    if check:
-        _finish(ws, check, "qe_kv_attn_shared", stream)
-    return out
+    return _attn(Q, pages, table, lengths, group, q_start, max_q, scale, causal, 0, 0, slopes, out, lse, ws, check, stream, groups, shared)

@@ -8,6 +8,7 @@ from test_stream_buffers import Stream, calls  # noqa: F401
 
 def test_step_calls(calls, monkeypatch):  # noqa: F811
     monkeypatch.setattr(Q, "_gpu", lambda t, name: t.get_device())
+    monkeypatch.setattr(torch.Tensor, "new_empty", lambda t, *shape, **kw: torch.empty(*shape, **kw))    # (recorded)
     s = Stream()
     i32 = lambda *shape: torch.ones(shape, dtype=torch.int32)  # noqa: E731
     q, k, pages = torch.ones((3, 4, 64)), torch.ones((3, 2, 64)), torch.ones((4, 2, 2, 64), dtype=torch.uint8)
