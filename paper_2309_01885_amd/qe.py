@@ -457,6 +457,11 @@ def _gpu(t: torch.Tensor, name: str) -> int:
     return t.get_device()
 
 
+def _elsewhere(dev: int) -> bool:
+    """Whether a call's tensors lie on another GPU than the current one: the call is then made with theirs as the current one."""
+    return dev >= 0 and dev != torch._C._cuda_getDevice()
+
+
 def _raw_stream(dev: int, stream):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
@@ -545,6 +550,10 @@ def kv_extend(counts: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, 
         _bad("table", table, "sequences x pages")
     batch, width = table.shape
     dev = _gpu(table, "table")
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return kv_extend(counts, table, lengths, free, free_count, page, total, keep, slots, positions, q_start, lacking, ws, check,
+                             stream)
     i32 = torch.int32
 
     def made(t, name, dtype, n):
@@ -591,6 +600,9 @@ def kv_append(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Te
         _bad("Q", Q, "tokens x heads x dim in float32, float16 or bfloat16")
     n, heads, dim = shape
     num, page, kv, dev = _pages(pages, dim, group)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return kv_append(Q, K, V, slots, pages, group, positions, cos, sin, interleaved, q_weight, k_weight, eps, out, status, stream)
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin come together")
     rows = half = 0
@@ -633,6 +645,10 @@ def _attn(Q, pages, table, lengths, group, q_start, max_q, scale, causal, window
     total, heads, dim = shape
     batch, width = table.shape
     num, page, kv, dev = _pages(pages, dim, group)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return _attn(Q, pages, table, lengths, group, q_start, max_q, scale, causal, window, sinks, slopes, out, lse, ws, check,
+                         stream, groups, shared)
     if q_start is None:
         if max_q is None:
             max_q = total // batch if batch else 0
