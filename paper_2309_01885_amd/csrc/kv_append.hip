@@ -323,6 +323,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 3 : 4) void kv_append_kernel(
         k[p].get(x);
         v[p].get(y);
         if (a.n.k) norm<OP>(x, w, a.n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = mine ? x[e] : 0.f;        // (0 times an infinite root)
         if (a.r.cos) rotate<1>(x, t, a.r, o, 0, true, turn[row]);
         uint32_t kw, vw;
         const uint32_t k8 = quantize8<LANES>(x, kw), v8 = quantize8<LANES>(y, vw);

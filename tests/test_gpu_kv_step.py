@@ -353,6 +353,18 @@ def test_append_special_values(qe, dtype):
         assert np.array_equal(host(pages), want_pages)
 
 
+@pytest.mark.parametrize("dim,group", [(8, 32), (40, 64), (72, 32), (136, 32), (200, 32)])
+def test_append_keeps_padding(qe, dim, group):
+    """Rows whose norm is infinite or NaN: the record's channels past dim hold 0 all the same."""
+    x = f64(draw((4, 1, dim), 3, "f32"))
+    x[1], x[2, 0, 3], x[3, 0, 5] = 0.0, np.nan, np.inf
+    x = rounded(x, "f32").cuda()
+    w = np.linspace(0.5, 2.0, dim, dtype=np.float32)
+    pages = qe.kv_pages(1, 1, dim, group, 32)
+    _, _, want_pages, _ = append(qe, x, x, x, np.arange(4), pages, group, qw=w, kw=w, eps=0.0, dtype="f32")
+    assert np.array_equal(host(pages), want_pages)
+
+
 def test_append_of_nothing(qe):
     pages = qe.kv_pages(1, 1, 64, 64, 32)
     e = torch.empty(0, 2, 64, device="cuda")
