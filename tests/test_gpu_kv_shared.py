@@ -335,3 +335,39 @@ def test_shared_where_it_gains(qe):
     """Through the public call, at a size that takes the lists by its own rule, and one that does not."""
     attend(qe, [(128, [8200 + 37 * y for y in range(24)])], [1] * 24, 8, 2, 64, 64, 64, "bf16", seed=1)
     attend(qe, [(1, [70, 90])], [1, 1], 8, 2, 64, 64, 64, "bf16", seed=2)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_shared_what_a_row_does_not_see(listed, dtype):
+    """NaN and huge values in one sequence's own part touch that sequence alone; NaN in the shared part every row of the
+    key head that sees it, in every sequence."""
+    pages, table, lens, held, groups, shared = family(listed, [(3, [140, 120, 97, 99])], 2, 64, 64, 32, dtype, seed=8)
+    q = draw((4, 4, 64), 1, dtype).cuda()
+    args = (q, pages, dev(table), i32(lens), i32(groups), i32(shared))
+
+    def put(b, t, value):
+        x = torch.full((1, 2, 64), value, dtype=DT[dtype], device="cuda")
+        x[:, 0] = 0.5                                       # (the second key head alone)
+        listed.kv_write(x, x, dev(np.array([int(table[b, t // 32]) * 32 + t % 32])), pages)
+
+    def seen():
+        out = []
+        for b, n in enumerate(lens):
+            t = np.arange(n)
+            out.append(tuple(f64(x) for x in listed.kv_read(pages, dev(table[b][t // 32].astype(np.int64) * 32 + t % 32), 64)))
+        return out
+
+    put(0, 110, float("nan"))
+    put(1, 119, 3.0e4 if dtype == "f16" else 1.0e30)
+    out = listed.kv_attn_shared(*args, check=True)
+    now = seen()
+    assert bool(torch.isnan(out[0, 2:]).all()) and bool(torch.isfinite(out[0, :2]).all())
+    for b in (2, 3):
+        check(out[b:b + 1], None, q[b:b + 1], [now[b]], [1], 0.125, dtype)
+    check(out[1:2, :2], None, q[1:2, :2], [tuple(x[:, :1] for x in now[1])], [1], 0.125, dtype)
+    put(2, 50, float("nan"))                                # (one page for all)
+    out = listed.kv_attn_shared(*args, check=True)
+    assert bool(torch.isnan(out[:, 2:]).all()) and bool(torch.isfinite(out[:, :2]).all())
+    # a sequence that ends before it does not see it, and keeps the others from sharing it
+    out = listed.kv_attn_shared(q, pages, dev(table), i32([140, 120, 97, 50]), i32(groups), i32(shared), check=True)
+    assert bool(torch.isnan(out[:3, 2:]).all()) and bool(torch.isfinite(out[3]).all())
