@@ -612,12 +612,14 @@ def kv_append(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Te
         if positions is None:
             raise ValueError("a rotation needs positions")
         rows, half = cos.shape
-    if out is None:
-        out = _on(stream, lambda: torch.empty_like(Q))
     qt, qh = _heads(Q, "Q", shape, dtype, dev)
     kt, kh = _heads(K, "K", (n, kv, dim), dtype, dev)
     vt, vh = _heads(V, "V", (n, kv, dim), dtype, dev)
-    ot, oh = _heads(out, "out", shape, dtype, dev)
+    if out is None:
+        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
+        ot, oh = heads * dim, dim
+    else:
+        ot, oh = _heads(out, "out", shape, dtype, dev)
     f32 = torch.float32
     code = load().qe_kv_append(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _DTYPES[dtype], n, heads, kv, dim, qt, qh, kt, kh, vt, vh,
                                _flat(q_weight, "q_weight", f32, dev, dim), _flat(k_weight, "k_weight", f32, dev, dim), eps,
@@ -659,10 +661,12 @@ def _attn(Q, pages, table, lengths, group, q_start, max_q, scale, causal, window
     shape = (total, heads, dim)
     if not -0x80000000 <= window <= 0x7fffffff:      # (a C int would take its low bits: 2^32 as no window)
         window = 0x7fffffff if window > 0 else -1
+    qt, qh = _heads(Q, "Q", shape, dtype, dev)
     if out is None:
         out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
-    qt, qh = _heads(Q, "Q", shape, dtype, dev)
-    ot, oh = _heads(out, "out", shape, dtype, dev)
+        ot, oh = heads * dim, dim
+    else:
+        ot, oh = _heads(out, "out", shape, dtype, dev)
     if ws is None:
         need = (kv_attn_workspace_size(total, batch, max_q, heads, kv, dim) if shared is None else
                 kv_attn_shared_workspace_size(total, batch, max_q, heads, kv, dim, shared.numel()))
