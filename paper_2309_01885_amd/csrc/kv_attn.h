@@ -759,7 +759,7 @@ constexpr int kv_few_occupancy(int dp, int group, int nt, int parts)
     return 2;
 }
 
-
+// What a few-row workgroup keeps in LDS: its waves' words, later their sums and the rows' maxima and masses.
 template <int DP, int GROUP, int NT> struct KvFewLds {
     static constexpr int NG = KvTiles<DP, GROUP>::NG;
     struct Words {

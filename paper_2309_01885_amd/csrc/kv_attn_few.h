@@ -1,4 +1,5 @@
-// Body of kv_few_kernel and kv_few_mode_kernel (kv_attn.h); DP, GROUP, NT, PARTS and MODE are theirs.
+// Body of kv_few_kernel, kv_few_mode_kernel (kv_attn.h) and kv_pair_kernel (kv_attn_modes.h); DP, GROUP, NT, PARTS, MODE
+// and lds (a KvFewLds) are theirs.
     using R = KvRec<DP, GROUP>;
     using T = KvTiles<DP, GROUP>;
     constexpr int NC = T::NC, NG = T::NG, UT = T::UT, CL = T::CL;

@@ -616,7 +616,7 @@ def kv_append(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Te
     kt, kh = _heads(K, "K", (n, kv, dim), dtype, dev)
     vt, vh = _heads(V, "V", (n, kv, dim), dtype, dev)
     if out is None:
-        out = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=pages.device))
+        out = _on(stream, lambda: Q.new_empty(shape))
         ot, oh = heads * dim, dim
     else:
         ot, oh = _heads(out, "out", shape, dtype, dev)
@@ -626,7 +626,7 @@ def kv_append(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Te
                                _flat(positions, "positions", torch.int32, dev, n), _flat(cos, "cos", f32, dev),
                                _flat(sin, "sin", f32, dev), rows, 2 * half, 1 if interleaved else 0,
                                _flat(slots, "slots", torch.int64, dev, n), group, pages.data_ptr(), num, page, out.data_ptr(),
-                               ot, oh, _flat(status, "status", torch.int32, dev, 1), _raw_stream(dev, stream))
+                               ot, oh, None if status is None else _flat(status, "status", torch.int32, dev, 1), _raw_stream(dev, stream))
     if code:
         raise QEError(code, "qe_kv_append")
     return out
