@@ -77,8 +77,10 @@ def i32(x):
 
 
 def attend(qe, parts, nqs, heads, kv, dim, group, page, dtype, seed=0, kscale=1.0, slopes=False, give_lse=True, causal=True,
-           scale=None, compare=True):
+           scale=None, compare=True, wide=0):
+    """wide: the table's width (its other entries are no pages), which decides the forms."""
     pages, table, lens, held, groups, shared = family(qe, parts, kv, dim, group, page, dtype, seed, kscale)
+    table = np.pad(table, ((0, 0), (0, max(0, wide - table.shape[1]))), constant_values=-1)
     total = sum(nqs)
     q = draw((total, heads, dim), seed + 7, dtype).cuda()
     scale = 1.0 / dim ** 0.5 if scale is None else scale
@@ -140,6 +142,16 @@ def test_shared_chunks(listed, dtype):
     """Chunks whose own part takes the many-row form or tiles of 32 rows."""
     attend(listed, [(4, [300, 290])], [150, 140], 3, 1, 64, 64, 64, dtype, seed=1)
     attend(listed, [(2, [300, 128 + 64])], [130, 64], 64, 64, 64, 64, 64, dtype, seed=2, give_lse=False)
+
+
+@pytest.mark.parametrize("dim,group", [(64, 64), (64, 32), (96, 64), (128, 128), (128, 32), (192, 64), (256, 128), (256, 32)])
+@pytest.mark.parametrize("dtype", list(DT))
+def test_shared_many_rows(listed, dtype, dim, group):
+    """The shared part in the many-row form, beside an own part in the few rows' and in the same; tiles that end inside a group,
+    entries of less than a stage, several groups."""
+    attend(listed, [(3, [100, 130, 97, 99, 96]), (2, [70, 64, 65])], [3, 1, 3, 2, 1, 3, 1, 2], 32, 1, dim, group, 32, dtype, seed=dim,
+           wide=30000)
+    attend(listed, [(5, [300, 290])], [70, 90], 4, 2, dim, group, 32, dtype, seed=dim + 1, slopes=True, wide=30000)
 
 
 def test_shared_many_sequences(listed):
