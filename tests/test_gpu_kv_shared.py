@@ -154,6 +154,15 @@ def test_shared_many_rows(listed, dtype, dim, group):
     attend(listed, [(5, [300, 290])], [70, 90], 4, 2, dim, group, 32, dtype, seed=dim + 1, slopes=True, wide=30000)
 
 
+@pytest.mark.parametrize("dim,group", [(64, 32), (64, 64), (80, 32), (96, 64), (96, 128), (128, 32), (128, 64), (128, 128), (200, 64)])
+@pytest.mark.parametrize("dtype", list(DT))
+def test_shared_single_tokens(listed, dtype, dim, group):
+    """Many sequences of a token each: shared tiles of 32 rows beside own ones of 16 in one launch, where the width has both."""
+    lens = [130 + 7 * y for y in range(12)]
+    attend(listed, [(4, lens), (1, [40, 33, 32, 50])], [1] * 16, 12, 2, dim, group, 32, dtype, seed=dim, slopes=group == 64)
+    attend(listed, [(30, [n + 960 for n in lens])], [1, 2] * 6, 8, 1, dim, group, 32, dtype, seed=dim + 1)
+
+
 def test_shared_many_sequences(listed):
     """More sequences than a thread each has, groups of all sizes."""
     r = np.random.default_rng(3)

@@ -279,6 +279,28 @@ def test_append_counts(qe, tokens, dtype):
     assert np.array_equal(host(pages), want_pages) and np.array_equal(bits(got), bits(want))
 
 
+@pytest.mark.parametrize("tokens,heads,dim,rot,interleaved", [(1100, 31, 128, 128, False), (2100, 25, 128, 36, False),
+                                                              (4100, 13, 96, 96, True), (1500, 19, 256, 128, False)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_runs_of_heads(qe, tokens, heads, dim, rot, interleaved, dtype):
+    """Enough tokens and heads that a workgroup goes through two to four heads, the last one through fewer; tokens without
+    a position among them, in place."""
+    q, k = draw((tokens, heads, dim), 1, dtype).cuda(), draw((tokens, 1, dim), 2, dtype).cuda()
+    cos, sin = tables(tokens + 9, rot)
+    w = np.linspace(0.5, 2.0, dim, dtype=np.float32)
+    positions = i32(np.arange(tokens) + 9)
+    positions[::7] = -1
+    pages = qe.kv_pages(-(-tokens // 128), 1, dim, 128, 128)
+    before = q.clone()
+    got, want, want_pages, _ = append(qe, q, k, k, np.arange(tokens), pages, 128, positions, cos, sin, interleaved, w, w, out=q,
+                                      dtype=dtype)
+    # (append's reference reads q after the call where it is the output: the rows are formed again from the copy)
+    want = rounded(okv.norm_rotate(f64(before), w, 1e-6, np.maximum(positions, 0), cos, sin, interleaved), dtype)
+    skipped = torch.from_numpy(positions < 0)
+    want[skipped] = before.cpu()[skipped]
+    assert got is q and np.array_equal(bits(q), bits(want)) and np.array_equal(host(pages), want_pages)
+
+
 @pytest.mark.parametrize("shift", [0, 1])
 @pytest.mark.parametrize("dtype", list(DT))
 def test_append_strided(qe, dtype, shift):
