@@ -411,7 +411,8 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  *  - then the pages j = held .. want - 1 are taken from the top in the same order, so that a call with
  *    the opposite counts restores table, lengths and stack.  A sequence gets all its pages or none: those that want any
  *    get them as long as the pages wanted up to and including theirs are there, those that want none need none.
- *    A sequence without its pages keeps its length, and its tokens get the slot -1;
+ *    A sequence without its pages keeps its length, and its tokens get the slot -1 (attention with this call's q_start
+ *    takes its rows for its last tokens: they mean nothing);
  *  - lengths[b] = new.  keep (NULL: 0): so many of the row's first entries are the caller's, for instance a prefix that
  *    several sequences share.  They are neither pushed, nor taken, nor changed.
  * Out, all on the device: q_start[b] = the sum of max(counts, 0) before b (batch + 1 entries, cut off at

@@ -572,8 +572,8 @@ qe_status qe_kv_attn_shared(const void* Q, int dtype, int64_t total, int heads, 
                                    o_head_stride, lse, ws);
     if (st != QE_OK || empty) return st;
     if (ngroups > 0 && (!groups || !shared)) return QE_ERR_ARG;
-    if (!ws || ws_bytes < qe_kv_attn_shared_workspace_size(total, batch, max_q, heads, kv_heads, dim, ngroups)) return QE_ERR_WORKSPACE;
-    return launch_kv_attn_shared(a, groups, shared, ngroups, ws, false, as_stream(stream));
+    if (!ws) return QE_ERR_WORKSPACE;
+    return launch_kv_attn_shared(a, groups, shared, ngroups, ws, ws_bytes, false, as_stream(stream));
 }
 
 // qe_kv_attn_shared by its lists also where kv_attn itself would be faster, and its workspace: not part of the ABI, for tests
@@ -599,8 +599,8 @@ qe_status qei_kv_attn_listed(const void* Q, int dtype, int64_t total, int heads,
                                    o_head_stride, lse, ws);
     if (st != QE_OK || empty) return st;
     if (ngroups > 0 && (!groups || !shared)) return QE_ERR_ARG;
-    if (!ws || ws_bytes < qei_kv_attn_listed_workspace_size(total, batch, max_q, heads, kv_heads, dim, ngroups)) return QE_ERR_WORKSPACE;
-    return launch_kv_attn_shared(a, groups, shared, ngroups, ws, true, as_stream(stream));
+    if (!ws) return QE_ERR_WORKSPACE;
+    return launch_kv_attn_shared(a, groups, shared, ngroups, ws, ws_bytes, true, as_stream(stream));
 }
 
 }  // extern "C"

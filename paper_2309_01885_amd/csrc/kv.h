@@ -185,8 +185,8 @@ size_t kv_attn_ws_bytes(int64_t batch, int64_t max_q, int heads, int kv_heads, i
 qe_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t s);
 bool kv_attn_many(const KvAttn& a);               // whether the call takes the many-row form
 size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads, int dim, int64_t ngroups, bool always);
-qe_status launch_kv_attn_shared(const KvAttn& a, const int32_t* groups, const int32_t* shared, int64_t ngroups, void* ws, bool always,
-                                hipStream_t s);   // always: also where kv_attn is faster
+qe_status launch_kv_attn_shared(const KvAttn& a, const int32_t* groups, const int32_t* shared, int64_t ngroups, void* ws, size_t ws_bytes,
+                                bool always, hipStream_t s);   // always: also where kv_attn is faster
 qe_status launch_kv_write(const void* K, const void* V, int dtype, const int64_t* strides, const int64_t* slots,
                           int64_t tokens, const KvCache& c, int group, int* status, hipStream_t s);
 qe_status launch_kv_read(const KvCache& c, int group, const int64_t* slots, int64_t tokens, void* K, void* V,

@@ -382,14 +382,21 @@ size_t kv_attn_shared_ws_bytes(int64_t total, int64_t batch, int64_t max_q, int 
     return need;
 }
 
-qe_status launch_kv_attn_shared(const KvAttn& call, const int32_t* groups, const int32_t* shared, int64_t ngroups, void* ws, bool always, hipStream_t s)
+// (The workspace is checked for what this call takes: the size for any group, type and width, as the caller has asked for it, is a
+// dozen lists' layouts, 2 us.)
+qe_status launch_kv_attn_shared(const KvAttn& call, const int32_t* groups, const int32_t* shared, int64_t ngroups, void* ws, size_t ws_bytes,
+                                bool always, hipStream_t s)
 {
     KvAttn a = call;
     const int dp = kv_dp(a.c.dim);
     Lists z = lists_of(a.total, a.batch, a.max_q, a.heads, a.c.heads, a.c.dim, a.group, a.dtype == QE_F32, ngroups, a.width * a.c.per);
-    if (!listed(z, a.total, a.batch, a.max_q, a.heads, a.c.heads) || !(always || gains(z, a))) return launch_kv_attn(a, ws, s);
-    kv_attn_vec(a);
+    if (!listed(z, a.total, a.batch, a.max_q, a.heads, a.c.heads) || !(always || gains(z, a))) {
+        if (ws_bytes < kv_attn_ws_bytes(a.batch, a.max_q, a.heads, a.c.heads, a.c.dim)) return QE_ERR_WORKSPACE;
+        return launch_kv_attn(a, ws, s);
+    }
     const Layout l = layout_of(z, a.batch, dp);
+    if (ws_bytes < l.end) return QE_ERR_WORKSPACE;
+    kv_attn_vec(a);
     char* const base = static_cast<char*>(ws);
     KvShared& sh = z.sh;
     sh.groups = groups;
