@@ -420,10 +420,14 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  * sequence with q_start[b] <= i < q_start[b + 1], positions[i] = that token and slots[i] = table page * page + token %
  * page.  Rows from q_start[batch] on, which a graph recorded for `total` rows may have, get -1 in both.
  * lacking (NULL, or one int): the pages that were wanted and not there, 0 where every sequence has its own.
- * Lengths below 0 or past width * page before or after the call, keep outside of 0 .. width, a stack outside
- * of 0 .. num_pages, page numbers outside of the cache that are taken and rows past `total` set QE_ERR_ARG in the workspace's status
- * word (never cleared here).  Such a sequence stays as it is and its rows get -1; a sequence whose rows
- * pass `total` gets no pages.  batch up to 2^20 (QE_ERR_UNSUPPORTED beyond).  No two rows of table may be the same memory. */
+ * QE_ERR_ARG in the workspace's status word (never cleared here) says that the call met
+ *  - lengths below 0 or past width * page before or after the call, or keep outside of 0 .. width: such a sequence stays as it
+ *    is, and its rows get -1;
+ *  - rows past `total`: a sequence that has one stays as it is, its rows before `total` get positions but no slots (a sequence
+ *    without new tokens has no rows, wherever it stands);
+ *  - a stack outside of 0 .. num_pages, which is cut off, or page numbers outside of the cache that were taken: their tokens get no
+ *    slots.
+ * batch up to 2^20 (QE_ERR_UNSUPPORTED beyond).  No two rows of table may be the same memory. */
 size_t qe_kv_extend_workspace_size(int64_t batch);
 qe_status qe_kv_extend(const int32_t* counts, int64_t batch, int32_t* table, int64_t width, int32_t* lengths,
                        const int32_t* keep, int32_t* free_pages, int64_t num_pages, int32_t* free_count, int page,

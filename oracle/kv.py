@@ -149,7 +149,7 @@ def extend(counts, table, lengths, free, free_count, page, total, keep=None):
     for b, (old, new, held, want, wrong) in enumerate(plan):
         n, need = max(int(counts[b]), 0), max(want - held, 0)
         needed += need
-        got = not wrong and (need == 0 or needed <= have) and row + n <= total
+        got = not wrong and (need == 0 or needed <= have) and (n == 0 or row + n <= total)
         if got:
             for j in range(need):
                 at = top - 1 - (needed - need + j)

@@ -150,8 +150,9 @@ __global__ __launch_bounds__(kScanThreads) void kv_extend_kernel(KvExtend a, boo
     for (int64_t b = b0; b < b1; ++b) {
         if (per > 1) c = change_of(a, b, false);
         const int64_t end = token + c.tokens, last = needed + c.need;
-        // (past the rows of this call nothing is written: the sequence stays as it is, its tokens are nobody's)
-        const bool got = !c.wrong && (c.need == 0 || last <= have) && end <= a.total;
+        // (past the rows of this call nothing is written: the sequence stays as it is, its tokens are nobody's.  One without rows
+        // is none of those, whatever came before it: its pages may have gone back already)
+        const bool got = !c.wrong && (c.need == 0 || last <= have) && (c.tokens == 0 || end <= a.total);
         KvExtendSeq s;
         s.old = c.old;
         s.held = c.held;
