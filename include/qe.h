@@ -505,10 +505,10 @@ qe_status qe_kv_attn_sinks(const void* Q, int dtype, int64_t total, int heads, i
 /* qe_kv_attn without a window for sequences that begin with the same pages (one system prompt, the branches of a request):
  * the sequences groups[g] .. groups[g + 1] - 1 (device, ngroups + 1 ascending entries from 0 to batch; sequences outside of
  * them share nothing) have the same first shared[g] page numbers in their rows of table.  The result is qe_kv_attn's,
- * up to the rounding of sums: the tokens of these pages that every query of the group sees (the whole records of 32 of them;
- * sequences without queries do not count) are read through the row of the group's first sequence, once for the
- * queries of all of them, the others sequence by sequence.  So the shared pages may be filled in part, or be
- * longer than a sequence.  A group of one sequence shares nothing, and a call that cannot gain is qe_kv_attn itself.
+ * up to the rounding of sums: the tokens of these pages that every query of the group sees (the whole records of 32 of them)
+ * are read through the row of the group's first sequence that has queries, once for the queries of all of them, the others sequence
+ * by sequence.  So the shared pages may be filled in part, or be longer than a sequence; sequences without queries do not
+ * count, and their rows may hold anything.  A group of one sequence shares nothing, and a call that cannot gain is qe_kv_attn itself.
  * Beside what qe_kv_attn checks, groups that do not ascend or leave 0 .. batch (then nothing is shared) and
  * shared[g] outside of 0 .. width set QE_ERR_ARG in the workspace's status word.  That the pages are the same is not
  * checked.  The queries of a sequence with a bad range in q_start are not computed. */

@@ -108,7 +108,7 @@ struct KvItem { int32_t first, b, kvh, tile_row, rows, len, pos0, rec0, rec1, sl
 
 // What the plan of kv_attn_shared knows of a group and of a sequence.
 struct KvGroup {
-    int32_t first_seq, first, tokens;      // its first sequence; first row of Q, rows
+    int32_t reader, first, tokens;         // the sequence whose pages are read; first row of Q, rows
     int32_t records;                       // shared records, 0: none
     int32_t tiles, splits, item;           // tiles and splits of the shared part, its first entry of list 0
     int32_t pad;

@@ -50,6 +50,7 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
     __shared__ ScanLds<2> lds2;
     __shared__ int32_t bound[kMaxGroups + 1];            // first sequences
     __shared__ int32_t sees[kMaxGroups], first[kMaxGroups], active[kMaxGroups], records[kMaxGroups], item[kMaxGroups + 1];
+    __shared__ int32_t reader[kMaxGroups];               // the first sequence with queries: its row of the table names the shared pages
     __shared__ unsigned long long tokens[kMaxGroups];
     __shared__ KvGroup group[kMaxGroups];
     __shared__ KvSequence seq[kScanThreads];              // (of more sequences than threads: in memory alone)
@@ -68,6 +69,7 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
     if (tid < ngroups) {
         shared_pages = sh.shared[tid];
         sees[tid] = 0x7fffffff;
+        reader[tid] = 0x7fffffff;
         first[tid] = 0;
         active[tid] = 0;
         tokens[tid] = 0;
@@ -112,6 +114,7 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
         if (s.nq < 0) atomicMin(&sees[g], 0);            // (its rows are not where the group's are)
         if (s.nq <= 0) continue;
         atomicMin(&sees[g], max(0, a.causal ? (int32_t)max((int64_t)s.len - s.nq + 1, (int64_t)0) : s.len));
+        atomicMin(&reader[g], (int32_t)b);
         atomicAdd(&active[g], 1);
         atomicAdd(&tokens[g], (unsigned long long)s.nq);
     }
@@ -123,7 +126,7 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
         if (shared_pages < 0 || shared_pages > a.width) set_status(a.status, QE_ERR_ARG);
         const int64_t most = max((int64_t)0, min((int64_t)shared_pages, a.width)) * a.c.per;
         const bool gains = !none && active[tid] > 1 && tokens[tid] <= (unsigned long long)a.total;
-        gr.first_seq = bound[tid];
+        gr.reader = reader[tid];
         gr.first = first[tid];
         gr.tokens = gains ? (int32_t)tokens[tid] : 0;
         gr.records = gains ? (int32_t)min(most, (int64_t)(sees[tid] / kKvTok)) : 0;
@@ -211,7 +214,7 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
         const int32_t split = (int32_t)(rest % (uint32_t)q.splits), kvh = (int32_t)(rest / (uint32_t)q.splits);
         KvItem it = {};
         it.first = q.first;
-        it.b = q.first_seq;
+        it.b = q.reader;
         it.kvh = kvh;
         it.tile_row = (int32_t)tile * sh.rows[0];
         it.rows = q.tokens * per;
