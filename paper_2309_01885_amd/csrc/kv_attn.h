@@ -316,6 +316,8 @@ template <int NC, int NT, int PARTS, KvMode MODE> struct KvRows {
     __device__ void load(const KvAttn& a, const KvUnit& u, int row0)
     {
         const int i = threadIdx.x & 15, j = (threadIdx.x & 63) >> 4;
+        // (a shared part's rows see all of it, and have no positions in it)
+        const bool causal = a.causal && (MODE != kKvListed || u.ref < 0);
         // all loads first (each with its conversion would wait for the one before)
         constexpr int E = PARTS == 2 ? 4 : 2;                // bytes of a channel
         u32x4 raw[NT][NC][E / 2];
@@ -395,14 +397,14 @@ template <int NC, int NT, int PARTS, KvMode MODE> struct KvRows {
                 if constexpr (PARTS == 2) q[1][n][k] = kv_frag(m[0], m[1], m[2], m[3]);
             }
             const int64_t pos = u.pos0 + qi[n];
-            hi[n] = have && a.causal ? (int)max((int64_t)0, pos + 1) : u.len;
+            hi[n] = have && causal ? (int)max((int64_t)0, pos + 1) : u.len;
             lo[n] = have && a.window ? (int)max((int64_t)0, pos - a.window + 1) : 0;
         }
         all_lo = 0;
         all_hi = u.len;
         if constexpr (MODE == kKvSinks) sinks = a.sinks;
         if constexpr (MODE == kKvListed) ref = u.ref;
-        if (a.causal) {
+        if (causal) {
             // the first and the last row bound the others
             const int64_t p0 = u.pos0 + row0 / u.per, p1 = u.pos0 + (min(u.rows, row0 + 16 * NT) - 1) / u.per;
             all_hi = (int)max((int64_t)0, p0 + 1);

@@ -27,8 +27,8 @@ extern template void kv_listed_width<256>(const KvAttn&, const KvPlan&, const Kv
 
 namespace {
 
-// Position of query 0 of a shared part: behind every token (and so that a position stays an int).
-constexpr int32_t kBehind = 1 << 29;
+// Rows of a call that the lists take (all heads of a key head; so that rows and what is added to them stay ints).
+constexpr int32_t kMostRows = 1 << 29;
 constexpr int kMaxGroups = kScanThreads;                 // a thread a group
 
 __device__ inline int32_t div_up(int32_t a, int32_t b) { return (int32_t)(((uint32_t)a + (uint32_t)b - 1) / (uint32_t)b); }
@@ -219,7 +219,6 @@ __global__ __launch_bounds__(kScanThreads) void kv_shared_plan_kernel(KvAttn a, 
         it.tile_row = (int32_t)tile * sh.rows[0];
         it.rows = q.tokens * per;
         it.len = q.records * kKvTok;
-        it.pos0 = kBehind;
         it.rec0 = piece(q.records, q.splits, split);
         it.rec1 = piece(q.records, q.splits, split + 1);
         it.slot = (q.item + (kvh * q.tiles + (int32_t)tile) * q.splits + split) * sh.rows[0];
@@ -320,7 +319,7 @@ Lists lists_of(int64_t total, int64_t batch, int64_t max_q, int heads, int kv_he
 bool listed(const Lists& z, int64_t total, int64_t batch, int64_t max_q, int heads, int kv_heads)
 {
     const int64_t per = heads / kv_heads, most = int64_t(1) << 23;
-    return batch > 1 && z.sh.ngroups > 0 && z.sh.ngroups <= kMaxGroups && total * per < kBehind && z.slots < (int64_t(1) << 31) &&
+    return batch > 1 && z.sh.ngroups > 0 && z.sh.ngroups <= kMaxGroups && total * per < kMostRows && z.slots < (int64_t(1) << 31) &&
            (int64_t)z.sh.room[0] + z.sh.room[1] < most && batch * kv_heads * cdiv(max_q * per, 8) < most;
 }
 
