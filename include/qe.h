@@ -408,13 +408,16 @@ qe_status qe_kv_read(const void* pages, int64_t num_pages, int page, const int64
  * want = max(ceil(new / page), keep[b]):
  *  - first the pages j = want .. held - 1 of all sequences go back onto the stack, the r-th of them (sequences and
  *    pages in ascending order) to the place r below the new top, and their table entries become -1;
- *  - then the pages j = held .. want - 1 are taken from the top in the same order, so that a call with
- *    the opposite counts restores table, lengths and stack.  A sequence gets all its pages or none: those that want any
- *    get them as long as the pages wanted up to and including theirs are there, those that want none need none.
- *    A sequence without its pages keeps its length, and its tokens get the slot -1 (attention with this call's q_start
+ *  - then the pages j = held .. want - 1 are taken from the top in the same order.  A sequence gets all its pages or none:
+ *    those that want any get them as long as the pages wanted up to and including theirs are there, those that want none need
+ *    none.  A sequence without its pages keeps its length, and its tokens get the slot -1 (attention with this call's q_start
  *    takes its rows for its last tokens: they mean nothing);
  *  - lengths[b] = new.  keep (NULL: 0): so many of the row's first entries are the caller's, for instance a prefix that
  *    several sequences share.  They are neither pushed, nor taken, nor changed.
+ * A next call whose counts are the lengths before this one less those after it restores table, lengths and stack: the
+ * opposite counts, but 0 for a sequence that was refused (its pages were not there, its rows passed `total`, its arguments were
+ * bad), which has no new tokens to take back and would lose as many of its old ones, and no more than a sequence had
+ * where a count took it down to none.
  * Out, all on the device: q_start[b] = the sum of max(counts, 0) before b (batch + 1 entries, cut off at
  * `total`); for row i of the call, which is token lengths[b] + i - q_start[b] (the length before the call) of the
  * sequence with q_start[b] <= i < q_start[b + 1], positions[i] = that token and slots[i] = table page * page + token %

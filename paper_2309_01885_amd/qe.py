@@ -544,8 +544,10 @@ def kv_extend(counts: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, 
     Returns slots (int64) and positions (int32) of the call's `total` rows, -1 for rows that are no token's,
     and q_start (int32, sequences + 1), into the tensors given or new ones of `stream`.  keep (int32): so many of each
     sequence's first pages are the caller's.  lacking: None or int32 of one element, the pages that were
-    not there; a sequence without its pages stays as it is and its slots are -1.  The call does not wait for
-    the device; check=True does, and raises if it met lengths that do not fit the table."""
+    not there; a sequence without its pages stays as it is and its slots are -1.  To take a step back, give the next call the
+    lengths before it less those after it (two tensors of the device, no wait): the opposite counts would take tokens from a
+    sequence that was refused its own.  The call does not wait for the device; check=True does, and raises if it met lengths that do
+    not fit the table."""
     if table.dim() != 2:
         _bad("table", table, "sequences x pages")
     batch, width = table.shape

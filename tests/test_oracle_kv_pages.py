@@ -60,3 +60,36 @@ def test_rows_past_total(batch):
         left = okv.extend(counts, table, lengths, free, 30, 32, total)[3]
         owned(table, lengths, free, left, 32)
         assert np.all(lengths[counts <= 0] == np.maximum(before + counts, 0)[counts <= 0])
+
+
+def test_taken_back_after_a_refusal():
+    """10 tokens, 40 more refused.  By the lengths nothing is taken back; the opposite count would take the 10."""
+    lengths, table, free = i32([10, 3]), i32([[1, -1], [0, -1]]), i32([-1, -1])
+    before = lengths.copy()
+    slots, _, _, left, lacking, bad = okv.extend([40, 2], table, lengths, free, 0, 32, 42)
+    assert not bad and lacking == 1 and lengths.tolist() == [10, 5] and np.all(slots[:40] == -1)
+    back = before - lengths
+    assert back.tolist() == [0, -2]
+    left = okv.extend(back, table, lengths, free, left, 32, 0)[3]
+    assert lengths.tolist() == [10, 3] and table.tolist() == [[1, -1], [0, -1]] and left == 0
+    left = okv.extend([-40, 0], table, lengths, free, left, 32, 0)[3]
+    assert lengths.tolist() == [0, 3] and table[0].tolist() == [-1, -1] and free[:left].tolist() == [1]
+
+
+@pytest.mark.parametrize("batch", [3, 40])
+def test_steps_that_refuse_taken_back(batch):
+    """Any mixture of new tokens, tokens that go back, pages that run out and rows past the total."""
+    for seed in range(40):
+        lengths, counts, total = rows_past_total(batch, seed)
+        if seed % 2:
+            total = int(np.maximum(counts, 0).sum())
+        spare = seed % 7
+        table, free = pool(lengths, 32, 9, spare, seed)
+        first = [x.copy() for x in (table, lengths, free[:spare])]
+        left = okv.extend(counts, table, lengths, free, spare, 32, total)[3]
+        owned(table, lengths, free, left, 32)
+        back = first[1] - lengths
+        left = okv.extend(back, table, lengths, free, left, 32, int(np.maximum(back, 0).sum()))[3]
+        assert left == spare
+        for a, b in zip(first, (table, lengths, free[:spare])):
+            assert np.array_equal(a, b)
