@@ -511,7 +511,10 @@ qe_status qe_kv_attn_sinks(const void* Q, int dtype, int64_t total, int heads, i
  * up to the rounding of sums: the tokens of these pages that every query of the group sees (the whole records of 32 of them)
  * are read through the row of the group's first sequence that has queries, once for the queries of all of them, the others sequence
  * by sequence.  So the shared pages may be filled in part, or be longer than a sequence; sequences without queries do not
- * count, and their rows may hold anything.  A group of one sequence shares nothing, and a call that cannot gain is qe_kv_attn itself.
+ * count, and their rows may hold anything.  A group of one sequence shares nothing.  A call that cannot gain by the sizes that the host
+ * knows, rows, heads and the table's width, and one of more than 1024 groups, is qe_kv_attn itself.  Lengths and shared
+ * pages are the device's: in a table much wider than the sequences are, or behind short prefixes, the call can be slower than
+ * qe_kv_attn (5 to 20 us on an MI355X), and a program that knows them calls that.
  * Beside what qe_kv_attn checks, groups that do not ascend or leave 0 .. batch (then nothing is shared) and
  * shared[g] outside of 0 .. width set QE_ERR_ARG in the workspace's status word.  That the pages are the same is not
  * checked.  The queries of a sequence with a bad range in q_start are not computed. */

@@ -278,6 +278,9 @@ constexpr int64_t kManyRows = 128, kManyRecords = 48 * 512;
 // Records of 16-row tiles that sharing has to save before it is taken: what its two more launches cost.  One query each, us of
 // kv_attn / the lists: 4 sequences behind 1000 tokens, 20 heads on 5 of 80, fp32 (saves 1000) 13.8 / 20.1; 32 heads on 8 of
 // 128: 16 behind 4096 (15000) 25.4 / 25.4, 8 behind 16384 (26000) 35.6 / 32.9, 64 behind 8192 (106000) 103 / 54.
+// The host knows the table's width alone, and takes sequences and prefixes to fill it.  Where they do not, the lists lose: in a table for
+// 131072 tokens, 8 of 500 tokens behind 64 12.0 / 18.9, 64 of 500 behind 64 18.3 / 35.1, 64 of 4000 behind 64 66 / 83, behind 3840
+// 54 / 51; 8 of 16584 behind 16384 34.2 / 30.7.
 constexpr int64_t kSaves = 20000;
 
 // The forms of the shared and the own part, and the sizes of their lists.

@@ -738,5 +738,7 @@ def kv_attn_shared(Q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, le
 
     The sequences groups[g] .. groups[g + 1] - 1 (int32, groups + 1 ascending entries) have the same first shared[g]
     (int32) entries in their rows of table; a row's lengths count the shared tokens.  The result is kv_attn's up to
-    the rounding of sums.  The other arguments are kv_attn's; kv_attn_shared_workspace_size gives the workspace."""
+    the rounding of sums.  Worth it behind long prefixes; in a table much wider than the sequences are, kv_attn is the faster
+    call for short ones (its own rule only sees the table's width).  Up to 1024 groups; more are kv_attn's.  The other arguments are
+    kv_attn's; kv_attn_shared_workspace_size gives the workspace."""
     return _attn(Q, pages, table, lengths, group, q_start, max_q, scale, causal, 0, 0, slopes, out, lse, ws, check, stream, groups, shared)
