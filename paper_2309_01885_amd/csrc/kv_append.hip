@@ -1,8 +1,8 @@
 // Norm of each head's query and key, rotation by their positions, and the write into the 4-bit cache, in one pass (qe.h).
 //
 // Every step is one correctly rounded fp32 operation (the compiler must not fuse them), so that the codes, which are
-// integers, are a function of the row's values alone; the norm's sum of squares and its root are in 64 bits, where no order
-// of the sum shows after the rounding to fp32:
+// integers, are a function of the row's values alone; the norm's sum of squares and its root are in 64 bits, where another order
+// of the sum or another root differs by some 2^-50 and moves the rounding to fp32 in one row of about 2^25:
 //   r = fp32(1 / sqrt(sum x^2 / dim + eps)), y = fp32(fp32(x r) w),
 //   a' = fp32(fp32(a c) - fp32(b s)), b' = fp32(fp32(b c) + fp32(a s)).
 // A channel's partner in the rotation comes through the row's own stretch of LDS, where any number of rotated channels is
